@@ -390,6 +390,105 @@ moe_status moe_plan_host(const moe_handle* h, double w_comp, double w_dispatch,
  * narrower tiles). */
 moe_status moe_tile_geometry(const moe_handle* h, int32_t* bm, int32_t* nt0, int32_t* nt1);
 
+/* ---- feed-forward blocks over row groups ------------------------------------
+ *
+ * The block of section 2.1 (gate and up projection, activation times up, down
+ * projection) on rows that are already ordered by group, with the weights as
+ * they are (not packed: in training they change every step), its backward
+ * pass, and the same products in 8-bit integers for serving.  A group is an
+ * expert (rows in the order of the layer's slots: group_off is then the `off`
+ * region of moe_ws_layout), or the one block of a dense layer.
+ *
+ * group_off: int32 [n_groups + 1]; group g has rows [group_off[g],
+ * group_off[g + 1]).  NULL where n_groups = 1: every row.  Offsets ascend in
+ * [0, rows]; groups may be empty, and rows before the first or behind the last
+ * group are neither read nor written.  (An offset outside that range or below
+ * an earlier one counts as the nearest that is not: no row has two groups and
+ * nothing outside the tensors is touched.)
+ *
+ * These calls need no handle.  They run on the current device, whose memory
+ * every argument is; pointers start on 16-byte boundaries (the workspace on
+ * 256 bytes), else MOE_ERR_INVALID_ARG.  A workspace holds scratch only: it
+ * needs no initialisation, keeps nothing from one call for the next, and may
+ * serve any calls that run one after the other, but not two that overlap.  No
+ * call allocates, waits, or adds in an order that changes from run to run, and
+ * all can be captured into a graph.  Outputs must not overlap inputs.
+ */
+typedef enum {
+  MOE_ACT_NONE = 0,
+  MOE_ACT_SILU = 1, /* v / (1 + e^-v) */
+  MOE_ACT_GELU = 2  /* tanh form: v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2 */
+} moe_act;
+
+#define MOE_MAX_GROUPS 512
+
+typedef struct {
+  int32_t rows;     /* T, 0..2^22 */
+  int32_t hidden;   /* H, multiple of 64, <= 16384 */
+  int32_t ffn;      /* F, multiple of 64, <= 32768 */
+  int32_t n_groups; /* G, 1..MOE_MAX_GROUPS */
+  int32_t act;      /* MOE_ACT_SILU or MOE_ACT_GELU */
+} moe_ffn_config;
+
+/* Workspace of moe_ffn_forward (backward = 0) or moe_ffn_backward (1). */
+moe_status moe_ffn_workspace_size(const moe_ffn_config* cfg, int32_t backward, size_t* bytes);
+
+/* y = (act(x W1) * (x W3)) W2 for the rows of each group.  x, y: bf16 [T][H];
+ * w1, w3: bf16 [G][H][F] (gate, up); w2: bf16 [G][F][H] (down).  gate, up:
+ * bf16 [T][F], x W1 and x W3 for moe_ffn_backward, or both NULL.  Products are
+ * summed in fp32; act(.) * up is rounded to bf16 once, for the second product. */
+moe_status moe_ffn_forward(const moe_ffn_config* cfg, const uint16_t* x, const int32_t* group_off,
+                           const uint16_t* w1, const uint16_t* w3, const uint16_t* w2, uint16_t* gate, uint16_t* up,
+                           uint16_t* y, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradients of moe_ffn_forward from dy (bf16 [T][H]), its inputs and the
+ * gate and up it kept: dx bf16 [T][H] (NULL: not wanted), dw1, dw3 bf16
+ * [G][H][F] and dw2 bf16 [G][F][H] (all, or all NULL).  The gradients of an
+ * empty group's weights are 0.  Sums are in fp32; the gradients of gate and up
+ * and act(gate) * up are rounded to bf16 once, for the products that take them. */
+moe_status moe_ffn_backward(const moe_ffn_config* cfg, const uint16_t* dy, const uint16_t* x,
+                            const int32_t* group_off, const uint16_t* w1, const uint16_t* w3, const uint16_t* w2,
+                            const uint16_t* gate, const uint16_t* up, uint16_t* dx, uint16_t* dw1, uint16_t* dw3,
+                            uint16_t* dw2, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows in 8 bits: scale[t] = max |x[t][.]| / 127 in fp32, q[t][c] = x[t][c] /
+ * scale[t] in fp32, rounded to the nearest whole number (halves to even), in
+ * [-127, 127].  A row of zeros has scale 0 and q = 0.  A row that holds an
+ * infinity or a NaN has scale NaN and q = 0, so that its products are NaN.
+ * x: bf16 [rows][cols], q: int8 [rows][cols], scale: fp32 [rows]; rows in
+ * [0, 2^22], cols a multiple of 64 up to 32768. */
+moe_status moe_quantize_rows_i8(int32_t rows, int32_t cols, const uint16_t* x, int8_t* q, float* scale, void* stream);
+
+/* Weights in 8 bits, a scale for each output channel: w bf16
+ * [n_groups][depth][channels] (the layout of w1, w3 and w2) becomes wq int8
+ * [n_groups][q_channels][depth], of which rows [first, first + channels) are
+ * written, and scale fp32 [n_groups][q_channels]; scales and rounding as
+ * moe_quantize_rows_i8's along the depth.  Two calls with q_channels = 2 F,
+ * first = 0 and F put gate and up into one operand.  depth and channels:
+ * multiples of 64, depth up to 32768, q_channels up to 65536. */
+moe_status moe_quantize_weights_i8(int32_t n_groups, int32_t depth, int32_t channels, int32_t q_channels,
+                                   int32_t first, const uint16_t* w, int8_t* wq, float* scale, void* stream);
+
+typedef struct {
+  int32_t rows;     /* T, 0..2^22 */
+  int32_t depth;    /* K, multiple of 64, <= 32768 */
+  int32_t channels; /* N, multiple of 8 (gated: of 16), <= 65536 */
+  int32_t n_groups; /* G, 1..MOE_MAX_GROUPS */
+  int32_t act;      /* MOE_ACT_NONE, or the activation of a gated product */
+} moe_gemm_i8_config;
+
+moe_status moe_gemm_i8_workspace_size(const moe_gemm_i8_config* cfg, size_t* bytes);
+
+/* v[t][n] = (sum_k xq[t][k] wq[g][n][k]) * x_scale[t] * w_scale[g][n] for the
+ * rows t of group g: the sum exact in 32-bit integers (any int8 values), the
+ * scales fp32.  act = MOE_ACT_NONE: y bf16 [T][N] is v.  Else channels [0, N/2)
+ * are gates and the rest their ups: y bf16 [T][N/2] = act(v[t][f]) *
+ * v[t][N/2 + f], v unrounded.  xq: int8 [T][K], x_scale: fp32 [T], wq: int8
+ * [G][N][K], w_scale: fp32 [G][N]. */
+moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const float* x_scale,
+                       const int32_t* group_off, const int8_t* wq, const float* w_scale, uint16_t* y, void* ws,
+                       size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -36,6 +36,11 @@ MOE_MODE_STATIC = 1
 MOE_MODE_SERIAL = 2
 MODES = {"dynamic": MOE_MODE_DYNAMIC, "static": MOE_MODE_STATIC, "serial": MOE_MODE_SERIAL}
 
+MOE_ACT_NONE = 0
+MOE_ACT_SILU = 1
+MOE_ACT_GELU = 2
+ACTS = {"none": MOE_ACT_NONE, "silu": MOE_ACT_SILU, "gelu": MOE_ACT_GELU}
+
 CALIB_MAX_C = 32
 CALIB_MAX_K = 4
 
@@ -69,6 +74,14 @@ class moe_ws_layout(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in (
         "total", "slot", "inv", "first_slot", "off", "sub_off", "row_off", "cnt_rank", "uniq", "stats", "plan",
         "err", "A", "Hbuf", "O")]
+
+
+class moe_ffn_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "hidden", "ffn", "n_groups", "act")]
+
+
+class moe_gemm_i8_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "depth", "channels", "n_groups", "act")]
 
 
 class MoeError(RuntimeError):
@@ -109,6 +122,13 @@ _SIGS = {
     "moe_sync_status": ([_H, _P], C.c_int),
     "moe_plan_host": ([_H, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_int64), C.POINTER(moe_plan)], C.c_int),
     "moe_tile_geometry": ([_H, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32)], C.c_int),
+    "moe_ffn_workspace_size": ([C.POINTER(moe_ffn_config), C.c_int32, C.POINTER(C.c_size_t)], C.c_int),
+    "moe_ffn_forward": ([C.POINTER(moe_ffn_config)] + [_P] * 9 + [C.c_size_t, _P], C.c_int),
+    "moe_ffn_backward": ([C.POINTER(moe_ffn_config)] + [_P] * 13 + [C.c_size_t, _P], C.c_int),
+    "moe_quantize_rows_i8": ([C.c_int32, C.c_int32, _P, _P, _P, _P], C.c_int),
+    "moe_quantize_weights_i8": ([C.c_int32] * 5 + [_P, _P, _P, _P], C.c_int),
+    "moe_gemm_i8_workspace_size": ([C.POINTER(moe_gemm_i8_config), C.POINTER(C.c_size_t)], C.c_int),
+    "moe_gemm_i8": ([C.POINTER(moe_gemm_i8_config)] + [_P] * 7 + [C.c_size_t, _P], C.c_int),
 }
 for _name, (_args, _res) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -307,6 +327,111 @@ def moe_tile_geometry(h: int):
     bm, n0, n1 = C.c_int32(), C.c_int32(), C.c_int32()
     _check("moe_tile_geometry", _lib.moe_tile_geometry(h, C.byref(bm), C.byref(n0), C.byref(n1)))
     return bm.value, n0.value, n1.value
+
+
+# The calls over row groups take no handle, so nothing else knows the sizes of
+# their tensors: each is checked here against the config, and the call runs on
+# the tensors' own device.
+
+class _Operands:
+    """Pointers of a call's tensors, checked to be dense, of the given type and size, and on one device."""
+
+    def __init__(self, first: torch.Tensor, name: str):
+        if first is None or not first.is_cuda:
+            raise ValueError(f"{name} must be in GPU memory")
+        self.device = first.device
+
+    def __call__(self, name: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, optional: bool = False):
+        if t is None:
+            if not optional:
+                raise ValueError(f"{name} is missing")
+            return None
+        if t.dtype != dtype or t.numel() != numel or t.device != self.device:
+            raise ValueError(f"{name} must be {dtype} with {numel} elements on {self.device}, "
+                             f"not {t.dtype} with {t.numel()} on {t.device}")
+        return _ptr(t)
+
+    def off(self, t: Optional[torch.Tensor], n_groups: int):
+        return self("group_off", t, torch.int32, n_groups + 1, optional=n_groups == 1)
+
+    def ws(self, t: torch.Tensor):
+        if t is None:
+            raise ValueError("ws is missing")
+        nbytes = t.numel() * t.element_size()
+        return self("ws", t, t.dtype, t.numel()), nbytes
+
+    def stream(self, stream):
+        """The given stream, or the device's current one."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device)
+        elif stream.device != self.device:
+            raise ValueError(f"the stream is of {stream.device}, the tensors are on {self.device}")
+        return C.c_void_p(stream.cuda_stream)
+
+
+def moe_ffn_workspace_size(cfg: moe_ffn_config, backward: bool = False) -> int:
+    n = C.c_size_t()
+    _check("moe_ffn_workspace_size", _lib.moe_ffn_workspace_size(C.byref(cfg), int(backward), C.byref(n)))
+    return n.value
+
+
+def moe_ffn_forward(cfg: moe_ffn_config, x, group_off, w1, w3, w2, gate, up, y, ws, stream=None) -> None:
+    o, bf = _Operands(x, "x"), torch.bfloat16
+    T, H, F, G = cfg.rows, cfg.hidden, cfg.ffn, cfg.n_groups
+    args = [o("x", x, bf, T * H), o.off(group_off, G), o("w1", w1, bf, G * H * F), o("w3", w3, bf, G * H * F),
+            o("w2", w2, bf, G * F * H), o("gate", gate, bf, T * F, True), o("up", up, bf, T * F, True),
+            o("y", y, bf, T * H), *o.ws(ws)]
+    with torch.cuda.device(o.device):
+        _check("moe_ffn_forward", _lib.moe_ffn_forward(C.byref(cfg), *args, o.stream(stream)))
+
+
+def moe_ffn_backward(cfg: moe_ffn_config, dy, x, group_off, w1, w3, w2, gate, up, dx, dw1, dw3, dw2, ws,
+                     stream=None) -> None:
+    o, bf = _Operands(dy, "dy"), torch.bfloat16
+    T, H, F, G = cfg.rows, cfg.hidden, cfg.ffn, cfg.n_groups
+    args = [o("dy", dy, bf, T * H), o("x", x, bf, T * H), o.off(group_off, G), o("w1", w1, bf, G * H * F),
+            o("w3", w3, bf, G * H * F), o("w2", w2, bf, G * F * H), o("gate", gate, bf, T * F),
+            o("up", up, bf, T * F), o("dx", dx, bf, T * H, True), o("dw1", dw1, bf, G * H * F, True),
+            o("dw3", dw3, bf, G * H * F, True), o("dw2", dw2, bf, G * F * H, True), *o.ws(ws)]
+    with torch.cuda.device(o.device):
+        _check("moe_ffn_backward", _lib.moe_ffn_backward(C.byref(cfg), *args, o.stream(stream)))
+
+
+def moe_quantize_rows_i8(rows: int, cols: int, x, q, scale, stream=None) -> None:
+    o = _Operands(x, "x")
+    args = [o("x", x, torch.bfloat16, rows * cols), o("q", q, torch.int8, rows * cols),
+            o("scale", scale, torch.float32, rows)]
+    with torch.cuda.device(o.device):
+        _check("moe_quantize_rows_i8", _lib.moe_quantize_rows_i8(int(rows), int(cols), *args, o.stream(stream)))
+
+
+def moe_quantize_weights_i8(n_groups: int, depth: int, channels: int, q_channels: int, first: int, w, wq, scale,
+                            stream=None) -> None:
+    o = _Operands(w, "w")
+    args = [o("w", w, torch.bfloat16, n_groups * depth * channels),
+            o("wq", wq, torch.int8, n_groups * q_channels * depth),
+            o("scale", scale, torch.float32, n_groups * q_channels)]
+    with torch.cuda.device(o.device):
+        _check("moe_quantize_weights_i8",
+               _lib.moe_quantize_weights_i8(int(n_groups), int(depth), int(channels), int(q_channels), int(first),
+                                            *args, o.stream(stream)))
+
+
+def moe_gemm_i8_workspace_size(cfg: moe_gemm_i8_config) -> int:
+    n = C.c_size_t()
+    _check("moe_gemm_i8_workspace_size", _lib.moe_gemm_i8_workspace_size(C.byref(cfg), C.byref(n)))
+    return n.value
+
+
+def moe_gemm_i8(cfg: moe_gemm_i8_config, xq, x_scale, group_off, wq, w_scale, y, ws, stream=None) -> None:
+    o = _Operands(xq, "xq")
+    T, K, N, G = cfg.rows, cfg.depth, cfg.channels, cfg.n_groups
+    out = N if cfg.act == MOE_ACT_NONE else N // 2
+    args = [o("xq", xq, torch.int8, T * K), o("x_scale", x_scale, torch.float32, T), o.off(group_off, G),
+            o("wq", wq, torch.int8, G * N * K), o("w_scale", w_scale, torch.float32, G * N),
+            o("y", y, torch.bfloat16, T * out), *o.ws(ws)]
+    with torch.cuda.device(o.device):
+        _check("moe_gemm_i8", _lib.moe_gemm_i8(C.byref(cfg), *args, o.stream(stream)))
 
 
 # ---- convenience --------------------------------------------------------------

@@ -9,15 +9,16 @@
 #include <string>
 
 #include "common.h"
+#include "host.h"
 #include "kernels.h"
 
 using namespace moe;
 
 namespace {
-
 thread_local std::string g_err;
+}
 
-moe_status fail(moe_status st, const char* fmt, ...) {
+moe_status moe::fail(moe_status st, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -26,16 +27,6 @@ moe_status fail(moe_status st, const char* fmt, ...) {
   g_err = buf;
   return st;
 }
-
-#define HIP_TRY(expr)                                                                   \
-  do {                                                                                  \
-    hipError_t e_ = (expr);                                                             \
-    if (e_ != hipSuccess) return fail(MOE_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
-
-size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-}  // namespace
 
 namespace {
 

@@ -1,0 +1,130 @@
+// What the products over row groups share: the groups' rows, the activations
+// of the gated block, and the host's checks (ffn.hip, int8.hip).
+#pragma once
+
+#include "common.h"
+#include "host.h"
+
+namespace moe {
+
+// ---- row groups -------------------------------------------------------------
+// Offsets are the caller's device data and are not trusted: offset i counts as
+// the running maximum of the offsets up to i, each clamped to [0, T], so that
+// groups never overlap and stay inside the tensors whatever the array holds.
+
+struct RowTile {
+  int group, begin, end;  // the tile's rows: [begin, end) of its group
+};
+
+__device__ __forceinline__ int clamp_off(int v, int T) { return v < 0 ? 0 : (v > T ? T : v); }
+
+// The rows of group g (every lane of the wavefront calls it and gets the same).
+__device__ __forceinline__ void group_rows(const int32_t* off, int T, int g, int* begin, int* end) {
+  if (!off) {
+    *begin = 0;
+    *end = T;
+    return;
+  }
+  int m = 0;
+  for (int i = threadIdx.x & 63; i <= g; i += 64) m = max(m, clamp_off(off[i], T));
+#pragma unroll
+  for (int d = 32; d; d >>= 1) m = max(m, __shfl_xor(m, d));
+  *begin = __builtin_amdgcn_readfirstlane(m);
+  *end = __builtin_amdgcn_readfirstlane(max(m, clamp_off(off[g + 1], T)));
+}
+
+// Row tile t of the list of all groups' tiles of `bm` rows, in group order (an
+// empty group has none); false past its end.  Every lane of the wavefront
+// calls it and gets the same; *total receives the length of the list.  Each
+// lane takes up to 8 consecutive groups (MOE_MAX_GROUPS / 64).
+__device__ __forceinline__ bool row_tile(const int32_t* off, int G, int T, int bm, int t, RowTile* out, int* total) {
+  if (!off) {
+    *total = ceil_div(T, bm);
+    *out = {0, min(t * bm, T), min((t + 1) * bm, T)};
+    return t < *total;
+  }
+  const int lane = threadIdx.x & 63;
+  const int per = ceil_div(G, 64), g0 = lane * per, g1 = min(g0 + per, G);
+  // running maximum of the offsets 0 .. g0
+  int m = 0;
+  for (int g = g0; g < g1; ++g) m = max(m, clamp_off(off[g], T));
+  const int own_first = g0 < G ? clamp_off(off[g0], T) : 0;
+  int pre = m;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(pre, d);
+    if (lane >= d) pre = max(pre, o);
+  }
+  pre = __shfl_up(pre, 1);
+  const int first = max(lane ? pre : 0, own_first);
+  int n = 0, at = first;
+  for (int g = g0; g < g1; ++g) {
+    const int e = max(at, clamp_off(off[g + 1], T));
+    n += ceil_div(e - at, bm);
+    at = e;
+  }
+  int incl = n;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(incl, d);
+    if (lane >= d) incl += o;
+  }
+  *total = __builtin_amdgcn_readlane(incl, 63);
+  if (t >= *total) return false;
+  const int before = incl - n;
+  int group = 0, begin = 0, end = 0, left = t - before;
+  const bool mine = left >= 0 && left < n;
+  if (mine) {
+    at = first;
+    for (int g = g0; g < g1; ++g) {
+      const int e = max(at, clamp_off(off[g + 1], T)), k = ceil_div(e - at, bm);
+      if (left >= 0 && left < k) {
+        group = g;
+        begin = at + left * bm;
+        end = min(begin + bm, e);
+      }
+      left -= k;
+      at = e;
+    }
+  }
+  const int src = __ffsll((unsigned long long)__ballot(mine)) - 1;
+  *out = {__builtin_amdgcn_readlane(group, src), __builtin_amdgcn_readlane(begin, src),
+          __builtin_amdgcn_readlane(end, src)};
+  return true;
+}
+
+// most row tiles a list can have
+__host__ __device__ inline int max_row_tiles(int T, int G, int bm) {
+  const int full = T / bm + G;  // every group ends in a partial tile
+  return full < T ? full : T;
+}
+
+// ---- the gated block's activation ---------------------------------------------
+// Both forms are v * s(z), s the logistic function: z = v for SiLU, and for
+// the tanh form z = 2 c (v + 0.044715 v^3), c = sqrt(2/pi), since
+// (1 + tanh(u)) / 2 = s(2u).  The hardware exponential and reciprocal are
+// within about 2 ulp of fp32; every result is rounded to bf16 next.
+constexpr float GELU_2C = 1.5957691216057308f, GELU_A = 0.044715f;
+
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+
+__device__ __forceinline__ float act_of(float v, int act) {
+  const float z = act == MOE_ACT_GELU ? GELU_2C * (v + GELU_A * v * v * v) : v;
+  return v * logistic(z);
+}
+
+// d/dv [v s(z)] = s + v s (1 - s) z'
+__device__ __forceinline__ void act_grad(float v, int act, float* a, float* da) {
+  const bool gelu = act == MOE_ACT_GELU;
+  const float z = gelu ? GELU_2C * (v + GELU_A * v * v * v) : v;
+  const float s = logistic(z), t = s * (1.0f - s);
+  const float dz = gelu ? GELU_2C * (1.0f + 3.0f * GELU_A * v * v) : 1.0f;
+  *a = v * s;
+  // (t is 0 where s is 0 or 1, and dz may be infinite there)
+  *da = t == 0.0f ? s : s + v * t * dz;
+}
+
+// ---- host checks ----------------------------------------------------------------
+inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+}  // namespace moe

@@ -1,0 +1,156 @@
+"""CPU tests of the operators over row groups: what the entry points refuse before anything is launched, what the
+binding refuses, and the oracle's gradients against differences.  No kernel is launched here."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from tests import blocks as K
+
+B = pytest.importorskip("paper_2609_21483_amd.binding", reason="libmoe.so not built")
+P = C.c_void_p
+AT = 1 << 20  # an aligned address that is never read: every call here is refused
+
+
+def ffn(call="moe_ffn_forward", cfg=(8, 64, 64, 1, 1), off=None, ws_bytes=1 << 30, **ptr):
+    """Status of a forward or backward call on made-up addresses."""
+    c = B.moe_ffn_config(*cfg)
+    names = ["x", "off", "w1", "w3", "w2", "gate", "up", "y"] if call == "moe_ffn_forward" else \
+        ["dy", "x", "off", "w1", "w3", "w2", "gate", "up", "dx", "dw1", "dw3", "dw2"]
+    at = dict({n: AT for n in names}, off=off, ws=AT)
+    at.update(ptr)
+    return getattr(B.library(), call)(C.byref(c), *[P(at[n]) for n in names], P(at["ws"]), ws_bytes, P(0))
+
+
+def gemm(cfg=(8, 64, 64, 1, 0), off=None, ws_bytes=1 << 20, **ptr):
+    c = B.moe_gemm_i8_config(*cfg)
+    names = ["xq", "sx", "off", "wq", "sw", "y", "ws"]
+    at = dict({n: AT for n in names}, off=off)
+    at.update(ptr)
+    return B.library().moe_gemm_i8(C.byref(c), *[P(at[n]) for n in names], ws_bytes, P(0))
+
+
+BAD_FFN = [(-1, 64, 64, 1, 1), ((1 << 22) + 1, 64, 64, 1, 1), (8, 0, 64, 1, 1), (8, 96, 64, 1, 1), (8, 16448, 64, 1, 1),
+           (8, 64, 32, 1, 1), (8, 64, 32832, 1, 1), (8, 64, 64, 0, 1), (8, 64, 64, 513, 1), (8, 64, 64, 1, 0),
+           (8, 64, 64, 1, 3)]
+
+
+@pytest.mark.parametrize("cfg", BAD_FFN)
+def test_ffn_refuses_bad_config(cfg):
+    n = C.c_size_t()
+    c = B.moe_ffn_config(*cfg)
+    assert B.library().moe_ffn_workspace_size(C.byref(c), 0, C.byref(n)) == B.MOE_ERR_INVALID_ARG
+    for call in ("moe_ffn_forward", "moe_ffn_backward"):
+        assert ffn(call, cfg, off=AT) == B.MOE_ERR_INVALID_ARG
+        assert B.moe_last_error()
+
+
+@pytest.mark.parametrize("call", ["moe_ffn_forward", "moe_ffn_backward"])
+@pytest.mark.parametrize("bad", [dict(x=0), dict(w1=0), dict(w3=0), dict(w2=0), dict(up=0), dict(x=AT + 2), dict(w2=AT + 8),
+                                 dict(gate=AT + 4), dict(ws=0), dict(ws=AT + 128), dict(ws_bytes=256),
+                                 dict(cfg=(8, 64, 64, 2, 1))])
+def test_ffn_refuses_bad_arguments(call, bad):
+    assert ffn(call, **bad) == B.MOE_ERR_INVALID_ARG, bad
+    assert B.moe_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(dy=0), dict(gate=0), dict(dw1=0), dict(dw3=0), dict(dw2=0), dict(dw1=0, dw3=0),
+                                 dict(dx=AT + 2), dict(dw2=AT + 2)])
+def test_backward_refuses_bad_arguments(bad):
+    assert ffn("moe_ffn_backward", **bad) == B.MOE_ERR_INVALID_ARG, bad
+
+
+def test_forward_of_no_rows_is_nothing():
+    assert ffn(cfg=(0, 64, 64, 1, 1), x=0, y=0, gate=0, up=0) == B.MOE_OK
+    assert gemm((0, 64, 64, 1, 0), xq=0, y=0) == B.MOE_OK
+    assert B.library().moe_quantize_rows_i8(0, 64, None, None, None, None) == B.MOE_OK
+
+
+@pytest.mark.parametrize("cfg", [(-1, 64, 64, 1, 0), (8, 0, 64, 1, 0), (8, 80, 64, 1, 0), (8, 32832, 64, 1, 0),
+                                 (8, 64, 0, 1, 0), (8, 64, 12, 1, 0), (8, 64, 24, 1, 1), (8, 64, 65544, 1, 0),
+                                 (8, 64, 64, 0, 0), (8, 64, 64, 513, 0), (8, 64, 64, 1, 3), (8, 64, 64, 1, -1)])
+def test_gemm_i8_refuses_bad_config(cfg):
+    n = C.c_size_t()
+    c = B.moe_gemm_i8_config(*cfg)
+    assert B.library().moe_gemm_i8_workspace_size(C.byref(c), C.byref(n)) == B.MOE_ERR_INVALID_ARG
+    assert gemm(cfg, off=AT) == B.MOE_ERR_INVALID_ARG
+    assert B.moe_last_error()
+
+
+@pytest.mark.parametrize("bad", [dict(xq=0), dict(sx=0), dict(wq=0), dict(sw=0), dict(y=0), dict(ws=0), dict(ws=AT + 64),
+                                 dict(ws_bytes=0), dict(xq=AT + 4), dict(wq=AT + 8), dict(y=AT + 2), dict(sx=AT + 4),
+                                 dict(cfg=(8, 64, 64, 2, 0))])
+def test_gemm_i8_refuses_bad_arguments(bad):
+    assert gemm(**bad) == B.MOE_ERR_INVALID_ARG, bad
+
+
+def test_quantisers_refuse_bad_arguments():
+    lib, bad = B.library(), B.MOE_ERR_INVALID_ARG
+    for rows, cols in [(-1, 64), ((1 << 22) + 1, 64), (8, 0), (8, 72), (8, 32832)]:
+        assert lib.moe_quantize_rows_i8(rows, cols, P(AT), P(AT), P(AT), None) == bad
+    for a in [(0, AT, AT), (AT, 0, AT), (AT, AT, 0), (AT + 2, AT, AT), (AT, AT + 1, AT), (AT, AT, AT + 4)]:
+        assert lib.moe_quantize_rows_i8(8, 64, *map(P, a), None) == bad
+        assert lib.moe_quantize_weights_i8(1, 64, 64, 64, 0, *map(P, a), None) == bad
+    for g, k, n, nq, first in [(0, 64, 64, 64, 0), (513, 64, 64, 64, 0), (1, 32, 64, 64, 0), (1, 64, 32, 64, 0),
+                               (1, 64, 128, 64, 0), (1, 64, 64, 128, 65), (1, 64, 64, 128, -1), (1, 64, 64, 65600, 0),
+                               (1, 32832, 64, 64, 0)]:
+        assert lib.moe_quantize_weights_i8(g, k, n, nq, first, P(AT), P(AT), P(AT), None) == bad, (g, k, n, nq, first)
+
+
+def test_workspace_sizes_grow_with_rows():
+    a = B.moe_ffn_workspace_size(B.moe_ffn_config(100, 64, 128, 1, 1))
+    b = B.moe_ffn_workspace_size(B.moe_ffn_config(100, 64, 128, 1, 1), True)
+    assert a >= 100 * 128 * 2 and b >= 3 * 100 * 128 * 2
+    assert B.moe_gemm_i8_workspace_size(B.moe_gemm_i8_config(100, 64, 128, 1, 0)) > 0
+
+
+def test_binding_refuses_host_memory():
+    c = B.moe_ffn_config(8, 64, 64, 1, 1)
+    t = torch.zeros(8, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="GPU memory"):
+        B.moe_ffn_forward(c, t, None, t, t, t, None, None, t, t)
+    with pytest.raises(ValueError, match="GPU memory"):
+        B.moe_ffn_backward(c, t, t, None, t, t, t, t, t, t, t, t, t, t)
+    with pytest.raises(ValueError, match="GPU memory"):
+        B.moe_gemm_i8(B.moe_gemm_i8_config(8, 64, 64, 1, 0), t, t, None, t, t, t, t)
+    with pytest.raises(ValueError, match="GPU memory"):
+        B.moe_quantize_rows_i8(8, 64, t, t, t)
+    with pytest.raises(ValueError, match="GPU memory"):
+        B.moe_quantize_weights_i8(1, 64, 64, 64, 0, t, t, t)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_oracle_gradients_match_differences(name):
+    """Central differences in 64 bits: with a step of 1e-5, off by about 1e-10 of the gradients' size."""
+    rng = np.random.default_rng(5)
+    T, H, F, G, off = 9, 6, 10, 3, [0, 4, 4, 8]
+    p = dict(x=rng.normal(size=(T, H)), w1=rng.normal(size=(G, H, F)), w3=rng.normal(size=(G, H, F)),
+             w2=rng.normal(size=(G, F, H)))
+    dy = rng.normal(size=(T, H))
+
+    def loss(q):
+        (y, _, _), _ = K.forward(q["x"], off, q["w1"], q["w3"], q["w2"], name, T)
+        return np.nansum(y * dy)
+
+    (_, gate, up), _ = K.forward(p["x"], off, p["w1"], p["w3"], p["w2"], name, T)
+    grads, _ = K.backward(dy, p["x"], off, p["w1"], p["w3"], p["w2"], gate, up, name)
+    for key, g in zip(("x", "w1", "w3", "w2"), grads):
+        g = np.nan_to_num(g)
+        for i in np.ndindex(*p[key].shape):
+            q = {k: v.copy() for k, v in p.items()}
+            q[key][i] += 1e-5
+            up_ = loss(q)
+            q[key][i] -= 2e-5
+            assert abs((up_ - loss(q)) / 2e-5 - g[i]) <= 1e-7 * max(1.0, np.abs(g).max()), (key, i)
+
+
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_oracle_derivative_of_the_activation(name):
+    v = np.linspace(-12, 12, 481)
+    a, da, _, _ = K.act(v, name)
+    num = (K.act(v + 1e-5, name)[0] - K.act(v - 1e-5, name)[0]) / 2e-5
+    assert np.max(np.abs(num - da)) <= 1e-8
+    t = torch.from_numpy(v)
+    ref = torch.nn.functional.silu(t) if name == "silu" else torch.nn.functional.gelu(t, approximate="tanh")
+    assert np.max(np.abs(ref.numpy() - a)) <= 1e-12

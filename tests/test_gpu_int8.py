@@ -1,0 +1,211 @@
+"""GPU tests of the quantisers and of the 8-bit integer product over row groups: whole numbers and scales equal the
+IEEE definition, products are off by their one rounding to bf16."""
+import numpy as np
+import pytest
+import torch
+
+from tests import blocks as K
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2609_21483_amd import binding
+    return binding
+
+
+def rows_bf16(T, C, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, C, generator=g) * torch.exp(3 * torch.randn(T, 1, generator=g))
+    return x.to(torch.bfloat16)
+
+
+@pytest.mark.parametrize("T,C", [(1, 64), (3, 128), (65, 192), (257, 1408), (5, 4096), (2, 14336), (3, 32768), (9, 2112)])
+def test_rows_are_quantised_as_defined(B, T, C):
+    x = rows_bf16(T, C, T + C)
+    q = torch.full((T * C + 64,), 99, dtype=torch.int8, device="cuda")
+    s = torch.full((T + 16,), 99.0, device="cuda")
+    B.moe_quantize_rows_i8(T, C, x.cuda(), q[:T * C], s[:T])
+    eq, es = K.quantize_rows(x.float().numpy())
+    assert np.array_equal(s[:T].cpu().numpy(), es)
+    assert np.array_equal(q[:T * C].view(T, C).cpu().numpy(), eq)
+    assert (q[T * C:] == 99).all() and (s[T:] == 99.0).all()
+
+
+def test_rows_of_special_values(B):
+    x = rows_bf16(10, 128, 1)
+    x[0] = 0.0
+    x[1] = -0.0
+    x[2, 5] = float("inf")
+    x[3, 127] = float("nan")
+    x[4] = torch.tensor([9.2e-41] * 128)           # the smallest subnormal of bf16
+    x[5] = x[5].float().sign() * 3.0e38
+    x[6] = 0.0
+    x[6, 64] = -2.0e-40
+    x[7] = torch.arange(128).to(torch.bfloat16)      # whole numbers and halves of the step
+    x[8, 0] = float("-inf")
+    x[9] = 1.0e-38
+    x[9, 3] = 1.2e-36                               # a scale below the smallest normal fp32
+    q, s = torch.empty(10, 128, dtype=torch.int8, device="cuda"), torch.empty(10, device="cuda")
+    B.moe_quantize_rows_i8(10, 128, x.cuda(), q, s)
+    eq, es = K.quantize_rows(x.float().numpy())
+    assert np.array_equal(q.cpu().numpy(), eq)
+    assert np.array_equal(s.cpu().numpy(), es, equal_nan=True)
+    assert np.isnan(es[[2, 3, 8]]).all() and not eq[[0, 1, 2, 3, 8]].any()
+    # the product of such a row is NaN, and only its own
+    wq, sw = torch.ones(1, 72, 128, dtype=torch.int8, device="cuda"), torch.ones(1, 72, device="cuda")
+    y = torch.empty(10, 72, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(B.moe_gemm_i8_workspace_size(B.moe_gemm_i8_config(10, 128, 72, 1, 0)), dtype=torch.uint8, device="cuda")
+    B.moe_gemm_i8(B.moe_gemm_i8_config(10, 128, 72, 1, 0), q, s, None, wq, sw, y, ws)
+    bad = torch.isnan(y).all(1).cpu().numpy()
+    assert np.array_equal(np.nonzero(bad)[0], [2, 3, 8])
+    # row 5 adds +-3e38 128 times: its product is net * 3e38, beyond bf16's 3.39e38 for a net count of 2 and more
+    with np.errstate(invalid="ignore"):
+        fits = np.abs(eq.astype(np.float64).sum(1) * es.astype(np.float64)) < 3.38e38
+    assert fits.sum() >= 6
+    assert torch.isfinite(y[torch.from_numpy(fits).cuda()]).all()
+
+
+@pytest.mark.parametrize("G,D,N,NQ,first", [(1, 64, 64, 64, 0), (3, 192, 128, 128, 0), (2, 128, 192, 384, 192),
+                                            (2, 1408, 64, 200, 100), (1, 4096, 320, 320, 0)])
+def test_weights_are_quantised_by_output_channel(B, G, D, N, NQ, first):
+    w = rows_bf16(G * D, N, G + D).view(G, D, N)
+    w *= 0.02
+    w[0, :, 3] = 0.0
+    w[G - 1, D - 1, 5] = float("inf")
+    wq = torch.full((G, NQ, D), 99, dtype=torch.int8, device="cuda")
+    s = torch.full((G, NQ), 99.0, device="cuda")
+    B.moe_quantize_weights_i8(G, D, N, NQ, first, w.cuda(), wq, s)
+    eq, es = K.quantize_rows(w.float().transpose(1, 2).numpy())
+    mine = slice(first, first + N)
+    assert np.array_equal(wq[:, mine].cpu().numpy(), eq)
+    assert np.array_equal(s[:, mine].cpu().numpy(), es, equal_nan=True)
+    rest = torch.ones(NQ, dtype=torch.bool)
+    rest[mine] = False
+    assert (wq[:, rest.cuda()] == 99).all() and (s[:, rest.cuda()] == 99.0).all()
+
+
+class Gemm:
+    def __init__(self, B, T, D, N, G, off, act, seed=0, full=False):
+        rng = np.random.default_rng(seed + T)
+        self.B, self.T, self.N, self.act, self.off = B, T, N, act, off
+        self.cfg = B.moe_gemm_i8_config(T, D, N, G, B.ACTS[act])
+        lo, hi = (-128, -127) if full else (-128, 128)
+        self.xq, self.wq = rng.integers(lo, hi, (T, D), dtype=np.int8), rng.integers(lo, hi, (G, N, D), dtype=np.int8)
+        # products of a few units, so that the activation bends
+        self.sx = (rng.uniform(0.5, 2.0, T) / 5000 / D ** 0.5).astype(np.float32)
+        self.sw = rng.uniform(-1.0, 2.0, (G, N)).astype(np.float32)
+        self.d = [torch.from_numpy(v).cuda() for v in (self.xq, self.sx, self.wq, self.sw)]
+        self.doff = None if off is None else torch.tensor(off, dtype=torch.int32, device="cuda")
+        self.ws = torch.empty(B.moe_gemm_i8_workspace_size(self.cfg), dtype=torch.uint8, device="cuda")
+        self.out = N if act == "none" else N // 2
+
+    def run(self, stream=None):
+        whole = torch.full((self.T * self.out + 64,), 0x4B4B, dtype=torch.int16, device="cuda").view(torch.bfloat16)
+        y = whole[:self.T * self.out].view(self.T, self.out)
+        self.B.moe_gemm_i8(self.cfg, self.d[0], self.d[1], self.doff, self.d[2], self.d[3], y, self.ws, stream)
+        return y, whole
+
+    def verify(self):
+        y, whole = self.run()
+        torch.cuda.synchronize()
+        ref, bound = K.gemm_i8(self.xq, self.sx, self.off, self.wq, self.sw, self.act)
+        K.check("y", y.float().cpu().numpy().astype(np.float64), ref, bound)
+        rest = torch.from_numpy(np.isnan(ref).all(1)).cuda()
+        assert (y.view(torch.int16)[rest] == 0x4B4B).all() and (whole.view(torch.int16)[-64:] == 0x4B4B).all()
+        return y
+
+
+@pytest.mark.parametrize("act", ["none", "silu", "gelu"])
+@pytest.mark.parametrize("T", [1, 2, 16, 31, 33, 64, 65, 129, 257, 600])
+def test_products_of_any_rows(B, T, act):
+    Gemm(B, T, 192, 320, 1, None, act).verify()
+
+
+@pytest.mark.parametrize("D", [64, 128, 192, 448, 1408, 4160])
+@pytest.mark.parametrize("N", [16, 48, 64, 144, 272, 528])
+@pytest.mark.parametrize("T", [5, 130])
+def test_products_of_any_width(B, D, N, T):
+    Gemm(B, T, D, N, 1, None, "silu", seed=1).verify()
+    Gemm(B, T, D, N - 8, 1, [0, T], "none", seed=2).verify()
+
+
+@pytest.mark.parametrize("off", [[0, 64, 128, 192, 256], [0, 1, 70, 71, 255], [0, 0, 129, 255, 255], [3, 40, 40, 41, 200],
+                                 [17, 17, 17, 17, 17], [0, 0, 0, 256, 256], [-5, 30, 400, 500, 1 << 30],
+                                 [200, 100, 256, 3, 0]], ids=str)
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_groups_of_any_rows(B, off, act):
+    Gemm(B, 256, 192, 144, 4, off, act, seed=3).verify()
+
+
+@pytest.mark.parametrize("G,T", [(37, 500), (64, 90), (65, 1100), (512, 700)])
+def test_many_groups(B, G, T):
+    cut = np.sort(np.random.default_rng(G).integers(0, T + 1, G - 1))
+    Gemm(B, T, 128, 96, G, [0, *cut.tolist(), T], "none", seed=4).verify()
+
+
+def test_large_groups(B):
+    Gemm(B, 1333, 704, 1296, 2, [0, 811, 1333], "silu", seed=5).verify()
+    Gemm(B, 1333, 704, 1288, 2, [0, 811, 1333], "none", seed=5).verify()
+
+
+@pytest.mark.parametrize("T", [3, 300])
+def test_largest_sums_are_exact(B, T):
+    """Every product -128 * -128 over the greatest depth: 2^29."""
+    Gemm(B, T, 32768, 64, 1, None, "none", seed=6, full=True).verify()
+
+
+def test_scales_of_zero_infinity_and_nan(B):
+    g = Gemm(B, 70, 128, 64, 1, None, "none", seed=7)
+    g.d[1][3], g.d[1][4], g.d[3][0, 5] = 0.0, float("nan"), float("inf")
+    y, _ = g.run()
+    acc = g.xq.astype(np.int64) @ g.wq[0].astype(np.int64).T
+    assert torch.isnan(y[4]).all()
+    row3 = np.delete(y[3].float().cpu().numpy(), 5)
+    assert (row3 == 0).all() and torch.isnan(y[3, 5])
+    some = np.array([r for r in range(70) if r not in (3, 4) and acc[r, 5] != 0])
+    assert torch.isinf(y[torch.from_numpy(some).cuda(), 5]).all()
+
+
+def test_same_bits_on_every_run_stream_and_replay(B):
+    g = Gemm(B, 333, 448, 320, 3, [0, 100, 101, 333], "silu", seed=8)
+    y, _ = g.run()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    y2, _ = g.run(s)
+    torch.cuda.synchronize()
+    assert torch.equal(y.view(torch.int16), y2.view(torch.int16))
+    x = rows_bf16(333, 448, 9).cuda()
+    cg = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(cg):
+        B.moe_quantize_rows_i8(333, 448, x, g.d[0], g.d[1])
+        yg, _ = g.run()
+    for turn in range(4):
+        x.copy_(rows_bf16(333, 448, turn))
+        g.doff.copy_(torch.tensor([0, 3 * turn, 90 * turn, 333], dtype=torch.int32))
+        yg.zero_()
+        cg.replay()
+        torch.cuda.synchronize()
+        got = yg.clone()
+        B.moe_quantize_rows_i8(333, 448, x, g.d[0], g.d[1])
+        ye, _ = g.run()
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int16), ye.view(torch.int16)), turn
+
+
+def test_binding_refuses_what_does_not_fit(B):
+    g = Gemm(B, 70, 128, 64, 2, [0, 30, 70], "none")
+    ok = list(g.d)
+    for i, t in [(0, ok[0][:69]), (0, ok[0].view(torch.uint8)), (1, ok[1].double()), (2, ok[2][:1]), (3, ok[3].t()),
+                 (3, None), (2, ok[2].cpu())]:
+        g.d = [*ok[:i], t, *ok[i + 1:]]
+        with pytest.raises(ValueError):
+            g.run()
+    g.d = ok
+    with pytest.raises(ValueError):
+        B.moe_quantize_rows_i8(70, 128, torch.empty(70, 128, dtype=torch.bfloat16, device="cuda"), ok[0], ok[1][:69])
+    with pytest.raises(ValueError):
+        B.moe_quantize_weights_i8(2, 128, 64, 64, 0, torch.empty(2, 128, 64, device="cuda"), ok[2], ok[3])
