@@ -33,65 +33,67 @@ __device__ __forceinline__ void group_rows(const int32_t* off, int T, int g, int
   *end = __builtin_amdgcn_readfirstlane(max(m, clamp_off(off[g + 1], T)));
 }
 
-// Row tile t of the list of all groups' tiles of `bm` rows, in group order (an
-// empty group has none); false past its end.  Every lane of the wavefront
-// calls it and gets the same; *total receives the length of the list.  Each
-// lane takes up to 8 consecutive groups (MOE_MAX_GROUPS / 64).
-__device__ __forceinline__ bool row_tile(const int32_t* off, int G, int T, int bm, int t, RowTile* out, int* total) {
-  if (!off) {
-    *total = ceil_div(T, bm);
-    *out = {0, min(t * bm, T), min((t + 1) * bm, T)};
-    return t < *total;
-  }
-  const int lane = threadIdx.x & 63;
-  const int per = ceil_div(G, 64), g0 = lane * per, g1 = min(g0 + per, G);
-  // running maximum of the offsets 0 .. g0
-  int m = 0;
-  for (int g = g0; g < g1; ++g) m = max(m, clamp_off(off[g], T));
-  const int own_first = g0 < G ? clamp_off(off[g0], T) : 0;
-  int pre = m;
+// The list of all groups' row tiles of `bm` rows, in group order (an empty
+// group has none).  Every lane of the wavefront takes part and gets the same
+// answers; each holds up to 8 consecutive groups (MOE_MAX_GROUPS / 64).
+struct RowTiles {
+  const int32_t* off;
+  int T, bm, g0, g1, first, incl, n;  // first: where this lane's groups start; n: their tiles, incl: and those before
+  int total;
+
+  __device__ __forceinline__ RowTiles(const int32_t* off_, int G, int T_, int bm_) : off(off_), T(T_), bm(bm_) {
+    if (!off) {
+      total = ceil_div(T, bm);
+      return;
+    }
+    const int lane = threadIdx.x & 63, per = ceil_div(G, 64);
+    g0 = min(lane * per, G), g1 = min(g0 + per, G);
+    int m = 0;  // the largest offset so far, over the lanes before and this lane's
+    for (int g = g0; g < g1; ++g) m = max(m, clamp_off(off[g], T));
+    const int own = g0 < G ? clamp_off(off[g0], T) : 0;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(pre, d);
-    if (lane >= d) pre = max(pre, o);
-  }
-  pre = __shfl_up(pre, 1);
-  const int first = max(lane ? pre : 0, own_first);
-  int n = 0, at = first;
-  for (int g = g0; g < g1; ++g) {
-    const int e = max(at, clamp_off(off[g + 1], T));
-    n += ceil_div(e - at, bm);
-    at = e;
-  }
-  int incl = n;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(incl, d);
-    if (lane >= d) incl += o;
-  }
-  *total = __builtin_amdgcn_readlane(incl, 63);
-  if (t >= *total) return false;
-  const int before = incl - n;
-  int group = 0, begin = 0, end = 0, left = t - before;
-  const bool mine = left >= 0 && left < n;
-  if (mine) {
-    at = first;
-    for (int g = g0; g < g1; ++g) {
-      const int e = max(at, clamp_off(off[g + 1], T)), k = ceil_div(e - at, bm);
-      if (left >= 0 && left < k) {
-        group = g;
-        begin = at + left * bm;
-        end = min(begin + bm, e);
-      }
-      left -= k;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(m, d);
+      if (lane >= d) m = max(m, o);
+    }
+    m = __shfl_up(m, 1);
+    first = max(lane ? m : 0, own);
+    n = 0;
+    for (int g = g0, at = first; g < g1; ++g) {
+      const int e = max(at, clamp_off(off[g + 1], T));
+      n += ceil_div(e - at, bm);
       at = e;
     }
+    incl = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    total = __builtin_amdgcn_readlane(incl, 63);
   }
-  const int src = __ffsll((unsigned long long)__ballot(mine)) - 1;
-  *out = {__builtin_amdgcn_readlane(group, src), __builtin_amdgcn_readlane(begin, src),
-          __builtin_amdgcn_readlane(end, src)};
-  return true;
-}
+
+  // tile t < total
+  __device__ __forceinline__ RowTile at(int t) const {
+    if (!off) return {0, t * bm, min((t + 1) * bm, T)};
+    int group = 0, begin = 0, end = 0, left = t - (incl - n);
+    const bool mine = left >= 0 && left < n;
+    if (mine)
+      for (int g = g0, a = first; g < g1; ++g) {
+        const int e = max(a, clamp_off(off[g + 1], T)), k = ceil_div(e - a, bm);
+        if (left >= 0 && left < k) {
+          group = g;
+          begin = a + left * bm;
+          end = min(begin + bm, e);
+        }
+        left -= k;
+        a = e;
+      }
+    const int src = __ffsll((unsigned long long)__ballot(mine)) - 1;
+    return {__builtin_amdgcn_readlane(group, src), __builtin_amdgcn_readlane(begin, src),
+            __builtin_amdgcn_readlane(end, src)};
+  }
+};
 
 // most row tiles a list can have
 __host__ __device__ inline int max_row_tiles(int T, int G, int bm) {

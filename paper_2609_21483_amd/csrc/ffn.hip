@@ -2,125 +2,189 @@
 #include <hip/hip_runtime.h>
 
 #include "blocks.h"
+#include "tile.h"
 
 using namespace moe;
 
 namespace {
 
-constexpr int TS = 64, KS = 16;  // tile and depth step
-
-// acc[i][j] += sum_k a(m0 + ty + 16 i, k) b(k, n0 + tx + 16 j) over [0, Kd)
-template <typename LA, typename LB>
-__device__ void product(float (&acc)[4][4], int Kd, LA&& la, LB&& lb) {
-  __shared__ float sa[KS][TS + 1], sb[KS][TS + 1];
-  const int t = threadIdx.x, tx = t % 16, ty = t / 16;
-  for (int k0 = 0; k0 < Kd; k0 += KS) {
-    __syncthreads();
-    for (int i = t; i < KS * TS; i += 256) {
-      sa[i / TS][i % TS] = k0 + i / TS < Kd ? la(i % TS, k0 + i / TS) : 0.0f;
-      sb[i / TS][i % TS] = k0 + i / TS < Kd ? lb(k0 + i / TS, i % TS) : 0.0f;
-    }
-    __syncthreads();
-    for (int k = 0; k < KS; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j) acc[i][j] += sa[k][ty + 16 * i] * sb[k][tx + 16 * j];
-  }
-}
-
-template <typename Fn>
-__device__ void each(int rows, int cols, Fn&& fn) {
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j)
-      if (ty + 16 * i < rows && tx + 16 * j < cols) fn(i, j, ty + 16 * i, tx + 16 * j);
-}
-
 struct FfnArgs {
   int T, H, F, G, act;
   const int32_t* off;
-  const uint16_t *x, *w1, *w3, *w2, *gate, *up, *dy, *h, *dgate, *dup;
-  uint16_t *o0, *o1, *o2;
+  const uint16_t *x, *w1, *w3, *w2, *gate, *up, *dy;
+  uint16_t *h, *dgate, *dup;       // workspace
+  uint16_t *kgate, *kup, *y;       // forward's outputs (kgate and kup may be NULL)
+  uint16_t *dx, *dw1, *dw3, *dw2;  // backward's (dx, or the three dw, may be NULL)
 };
 
-// h = act(x W1) * (x W3); o0 = h, o1, o2 = gate and up or NULL
-__global__ __launch_bounds__(256) void ffn_up_kernel(FfnArgs a) {
-  RowTile rt;
-  int total;
-  if (!row_tile(a.off, a.G, a.T, TS, blockIdx.y, &rt, &total)) return;
-  const int n0 = blockIdx.x * TS, rows = rt.end - rt.begin;
-  float g[4][4] = {}, u[4][4] = {};
-  auto la = [&](int m, int k) { return m < rows ? bf16_to_f32(a.x[(size_t)(rt.begin + m) * a.H + k]) : 0.0f; };
-  product(g, a.H, la, [&](int k, int n) { return bf16_to_f32(a.w1[((size_t)rt.group * a.H + k) * a.F + n0 + n]); });
-  product(u, a.H, la, [&](int k, int n) { return bf16_to_f32(a.w3[((size_t)rt.group * a.H + k) * a.F + n0 + n]); });
-  each(rows, a.F - n0, [&](int i, int j, int m, int n) {
-    const size_t at = (size_t)(rt.begin + m) * a.F + n0 + n;
-    a.o0[at] = f32_to_bf16(act_of(g[i][j], a.act) * u[i][j]);
-    if (a.o1) a.o1[at] = f32_to_bf16(g[i][j]), a.o2[at] = f32_to_bf16(u[i][j]);
+__device__ __forceinline__ const char* bytes(const uint16_t* p) { return reinterpret_cast<const char*>(p); }
+__device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
+  *reinterpret_cast<u32x4_t*>(p) = tile::pack8(v);
+}
+
+// Forms of the tile: x W (weights transposed), d W^T, and x^T d
+template <typename S>
+using XW = tile::Tile<S, false, false, true>;
+template <typename S>
+using XWT = tile::Tile<S, false, false, false>;
+template <typename S>
+using XTD = tile::Tile<S, false, true, true>;
+
+// h = act(x W1) * (x W3), and gate and up where they are kept
+template <typename Tl>
+__global__ __launch_bounds__(Tl::THREADS) void ffn_up_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const RowTiles list(a.off, a.G, a.T, Tl::BM);
+  constexpr int COLS = Tl::BN / 2;
+  int m, n;
+  if (!tile::pick(list.total, ceil_div(a.F, COLS), &m, &n)) return;
+  const RowTile rt = list.at(m);
+  const int n0 = n * COLS, rows = rt.end - rt.begin;
+  const size_t wo = (size_t)rt.group * a.H * a.F;
+  const tile::Operand A{bytes(a.x + (size_t)rt.begin * a.H), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
+  const tile::Operand B{bytes(a.w1 + wo), bytes(a.w3 + wo), (uint32_t)a.F * 2, 0, n0, a.F};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, a.H, A, B, 0);
+  Tl::template epilogue<true>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[16]) {
+    if (n0 + c >= a.F) return;
+    const size_t at = (size_t)(rt.begin + r) * a.F + n0 + c;
+    float g[8], u[8], h[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      g[i] = __uint_as_float(v[i]);
+      u[i] = __uint_as_float(v[8 + i]);
+      h[i] = act_of(g[i], a.act) * u[i];
+    }
+    store8(a.h + at, h);
+    if (a.kgate) {
+      store8(a.kgate + at, g);
+      store8(a.kup + at, u);
+    }
   });
 }
 
 // y = h W2
-__global__ __launch_bounds__(256) void ffn_down_kernel(FfnArgs a) {
-  RowTile rt;
-  int total;
-  if (!row_tile(a.off, a.G, a.T, TS, blockIdx.y, &rt, &total)) return;
-  const int n0 = blockIdx.x * TS, rows = rt.end - rt.begin;
-  float y[4][4] = {};
-  product(y, a.F, [&](int m, int k) { return m < rows ? bf16_to_f32(a.h[(size_t)(rt.begin + m) * a.F + k]) : 0.0f; },
-          [&](int k, int n) { return bf16_to_f32(a.w2[((size_t)rt.group * a.F + k) * a.H + n0 + n]); });
-  each(rows, a.H - n0, [&](int i, int j, int m, int n) {
-    a.o0[(size_t)(rt.begin + m) * a.H + n0 + n] = f32_to_bf16(y[i][j]);
+template <typename Tl>
+__global__ __launch_bounds__(Tl::THREADS) void ffn_down_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const RowTiles list(a.off, a.G, a.T, Tl::BM);
+  int m, n;
+  if (!tile::pick(list.total, ceil_div(a.H, Tl::BN), &m, &n)) return;
+  const RowTile rt = list.at(m);
+  const int n0 = n * Tl::BN, rows = rt.end - rt.begin;
+  const tile::Operand A{bytes(a.h + (size_t)rt.begin * a.F), nullptr, (uint32_t)a.F * 2, rows, 0, 0};
+  const tile::Operand B{bytes(a.w2 + (size_t)rt.group * a.F * a.H), nullptr, (uint32_t)a.H * 2, 0, n0, a.H};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, a.F, A, B, 0);
+  Tl::template epilogue<false>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[8]) {
+    if (n0 + c < a.H) store8(a.y + (size_t)(rt.begin + r) * a.H + n0 + c, __builtin_bit_cast(float[8], v));
   });
 }
 
-// dh = dy W2^T, and from it o0 = act(gate) * up, o1 = d gate, o2 = d up
-__global__ __launch_bounds__(256) void ffn_dh_kernel(FfnArgs a) {
-  RowTile rt;
-  int total;
-  if (!row_tile(a.off, a.G, a.T, TS, blockIdx.y, &rt, &total)) return;
-  const int n0 = blockIdx.x * TS, rows = rt.end - rt.begin;
-  float dh[4][4] = {};
-  product(dh, a.H, [&](int m, int k) { return m < rows ? bf16_to_f32(a.dy[(size_t)(rt.begin + m) * a.H + k]) : 0.0f; },
-          [&](int k, int n) { return bf16_to_f32(a.w2[((size_t)rt.group * a.F + n0 + n) * a.H + k]); });
-  each(rows, a.F - n0, [&](int i, int j, int m, int n) {
-    const size_t at = (size_t)(rt.begin + m) * a.F + n0 + n;
-    const float g = bf16_to_f32(a.gate[at]), u = bf16_to_f32(a.up[at]);
-    float v, dv;
-    act_grad(g, a.act, &v, &dv);
-    a.o0[at] = f32_to_bf16(v * u);
-    a.o1[at] = f32_to_bf16(dh[i][j] * u * dv);
-    a.o2[at] = f32_to_bf16(dh[i][j] * v);
+// dh = dy W2^T, and from it h = act(gate) * up again, d gate and d up
+template <typename Tl>
+__global__ __launch_bounds__(Tl::THREADS) void ffn_dh_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const RowTiles list(a.off, a.G, a.T, Tl::BM);
+  int m, n;
+  if (!tile::pick(list.total, ceil_div(a.F, Tl::BN), &m, &n)) return;
+  const RowTile rt = list.at(m);
+  const int n0 = n * Tl::BN, rows = rt.end - rt.begin;
+  const tile::Operand A{bytes(a.dy + (size_t)rt.begin * a.H), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
+  const tile::Operand B{bytes(a.w2 + ((size_t)rt.group * a.F + n0) * a.H), nullptr, (uint32_t)a.H * 2, a.F - n0, 0, 0};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, a.H, A, B, 0);
+  Tl::template epilogue<false>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[8]) {
+    if (n0 + c >= a.F) return;
+    const size_t at = (size_t)(rt.begin + r) * a.F + n0 + c;
+    float g[8], u[8], h[8];
+    tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.gate + at), g);
+    tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.up + at), u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float s, ds;
+      act_grad(g[i], a.act, &s, &ds);
+      const float d = __uint_as_float(v[i]);
+      h[i] = s * u[i];
+      g[i] = d * u[i] * ds;
+      u[i] = d * s;
+    }
+    store8(a.h + at, h);
+    store8(a.dgate + at, g);
+    store8(a.dup + at, u);
   });
 }
 
-// dx = dgate W1^T + dup W3^T
-__global__ __launch_bounds__(256) void ffn_dx_kernel(FfnArgs a) {
-  RowTile rt;
-  int total;
-  if (!row_tile(a.off, a.G, a.T, TS, blockIdx.y, &rt, &total)) return;
-  const int n0 = blockIdx.x * TS, rows = rt.end - rt.begin;
-  float dx[4][4] = {};
-  product(dx, a.F, [&](int m, int k) { return m < rows ? bf16_to_f32(a.dgate[(size_t)(rt.begin + m) * a.F + k]) : 0.0f; },
-          [&](int k, int n) { return bf16_to_f32(a.w1[((size_t)rt.group * a.H + n0 + n) * a.F + k]); });
-  product(dx, a.F, [&](int m, int k) { return m < rows ? bf16_to_f32(a.dup[(size_t)(rt.begin + m) * a.F + k]) : 0.0f; },
-          [&](int k, int n) { return bf16_to_f32(a.w3[((size_t)rt.group * a.H + n0 + n) * a.F + k]); });
-  each(rows, a.H - n0, [&](int i, int j, int m, int n) {
-    a.o0[(size_t)(rt.begin + m) * a.H + n0 + n] = f32_to_bf16(dx[i][j]);
+// dx = dgate W1^T + dup W3^T, one depth of 2 F
+template <typename Tl>
+__global__ __launch_bounds__(Tl::THREADS) void ffn_dx_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const RowTiles list(a.off, a.G, a.T, Tl::BM);
+  int m, n;
+  if (!tile::pick(list.total, ceil_div(a.H, Tl::BN), &m, &n)) return;
+  const RowTile rt = list.at(m);
+  const int n0 = n * Tl::BN, rows = rt.end - rt.begin;
+  const size_t ro = (size_t)rt.begin * a.F, wo = ((size_t)rt.group * a.H + n0) * a.F;
+  const uint32_t ld = (uint32_t)a.F * 2;
+  const tile::Operand A{bytes(a.dgate + ro), nullptr, ld, rows, 0, 0}, A2{bytes(a.dup + ro), nullptr, ld, rows, 0, 0};
+  const tile::Operand B{bytes(a.w1 + wo), nullptr, ld, a.H - n0, 0, 0}, B2{bytes(a.w3 + wo), nullptr, ld, a.H - n0, 0, 0};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, a.F, A2, B2, a.F);
+  Tl::template epilogue<false>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[8]) {
+    if (n0 + c < a.H) store8(a.dx + (size_t)(rt.begin + r) * a.H + n0 + c, __builtin_bit_cast(float[8], v));
   });
 }
 
-// out[g] = p^T q over the group's rows; p [T][M], q [T][N]
-__global__ __launch_bounds__(256) void ffn_dw_kernel(const int32_t* off, int T, const uint16_t* p, const uint16_t* q,
-                                                     uint16_t* out, int M, int N) {
-  const int g = blockIdx.z, m0 = blockIdx.y * TS, n0 = blockIdx.x * TS;
+// dW1 = x^T dgate, dW3 = x^T dup, dW2 = h^T dy, each group's
+template <typename Tl>
+__global__ __launch_bounds__(Tl::THREADS) void ffn_dw_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  // tiles of a group: those of dW1, of dW3, then of dW2
+  const int hm = ceil_div(a.H, Tl::BM), fn = ceil_div(a.F, Tl::BN), fm = ceil_div(a.F, Tl::BM), hn = ceil_div(a.H, Tl::BN);
+  const int t13 = hm * fn, per = 2 * t13 + fm * hn, chunk = gridDim.x / NXCD;
+  const int t = (blockIdx.x % NXCD) * chunk + blockIdx.x / NXCD;
+  if (t >= per * a.G) return;
+  const int g = t / per, i = t % per, which = i / t13 < 2 ? i / t13 : 2;
   int b, e;
-  group_rows(off, T, g, &b, &e);
-  float w[4][4] = {};
-  product(w, e - b, [&](int m, int k) { return bf16_to_f32(p[(size_t)(b + k) * M + m0 + m]); },
-          [&](int k, int n) { return bf16_to_f32(q[(size_t)(b + k) * N + n0 + n]); });
-  each(M - m0, N - n0, [&](int i, int j, int m, int n) {
-    out[((size_t)g * M + m0 + m) * N + n0 + n] = f32_to_bf16(w[i][j]);
+  group_rows(a.off, a.T, g, &b, &e);
+  const uint16_t *p = which == 2 ? a.h : a.x, *q = which == 0 ? a.dgate : which == 1 ? a.dup : a.dy;
+  const int M = which == 2 ? a.F : a.H, N = which == 2 ? a.H : a.F, mt = which == 2 ? fm : hm, nt = which == 2 ? hn : fn;
+  const int j = i - which * t13, band = j / (tile::NEAR * nt), first = band * tile::NEAR;
+  const int wide = min(tile::NEAR, mt - first), in = j - band * tile::NEAR * nt;
+  const int m0 = (first + in % wide) * Tl::BM, n0 = in / wide * Tl::BN;
+  const tile::Operand A{bytes(p + (size_t)b * M), nullptr, (uint32_t)M * 2, 0, m0, M};
+  const tile::Operand B{bytes(q + (size_t)b * N), nullptr, (uint32_t)N * 2, 0, n0, N};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, e - b, A, B, 0);
+  uint16_t* out = (which == 0 ? a.dw1 : which == 1 ? a.dw3 : a.dw2) + ((size_t)g * M + m0) * N + n0;
+  Tl::template epilogue<false>(acc, lds, min(Tl::BM, M - m0), [&](int r, int c, const uint32_t (&v)[8]) {
+    if (n0 + c < N) store8(out + (size_t)r * N + c, __builtin_bit_cast(float[8], v));
   });
+}
+
+// Launches on the most tiles that the groups can have
+#define LAUNCH(name, form, width)                                                                       \
+  template <typename S>                                                                                   \
+  void launch_##name(const FfnArgs& a, hipStream_t s) {                                                 \
+    using Tl = form<S>;                                                                              \
+    const int g = tile::grid_of(max_row_tiles(a.T, a.G, Tl::BM), width);                                \
+    ffn_##name##_kernel<Tl><<<g, Tl::THREADS, 0, s>>>(a);                                               \
+  }
+LAUNCH(up, XW, ceil_div(a.F, Tl::BN / 2))
+LAUNCH(down, XW, ceil_div(a.H, Tl::BN))
+LAUNCH(dh, XWT, ceil_div(a.F, Tl::BN))
+LAUNCH(dx, XWT, ceil_div(a.H, Tl::BN))
+#undef LAUNCH
+template <typename S>
+void launch_dw(const FfnArgs& a, hipStream_t s) {
+  using Tl = XTD<S>;
+  const int per = 2 * ceil_div(a.H, Tl::BM) * ceil_div(a.F, Tl::BN) + ceil_div(a.F, Tl::BM) * ceil_div(a.H, Tl::BN);
+  ffn_dw_kernel<Tl><<<tile::grid_of(a.G, per), Tl::THREADS, 0, s>>>(a);
 }
 
 moe_status check_cfg(const moe_ffn_config* c) {
@@ -178,12 +242,9 @@ moe_status moe_ffn_forward(const moe_ffn_config* cfg, const uint16_t* x, const i
   a.T = cfg->rows, a.H = cfg->hidden, a.F = cfg->ffn, a.G = cfg->n_groups, a.act = cfg->act;
   a.off = group_off;
   a.x = x, a.w1 = w1, a.w3 = w3, a.w2 = w2;
-  uint16_t* h = static_cast<uint16_t*>(ws);
-  a.h = h, a.o0 = h, a.o1 = gate, a.o2 = up;
-  const int mt = max_row_tiles(a.T, a.G, TS);
-  ffn_up_kernel<<<dim3(a.F / TS, mt), 256, 0, s>>>(a);
-  a.o0 = y;
-  ffn_down_kernel<<<dim3(a.H / TS, mt), 256, 0, s>>>(a);
+  a.h = static_cast<uint16_t*>(ws), a.kgate = gate, a.kup = up, a.y = y;
+  launch_up<tile::Wide>(a, s);
+  launch_down<tile::Wide>(a, s);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }
@@ -209,23 +270,15 @@ moe_status moe_ffn_backward(const moe_ffn_config* cfg, const uint16_t* dy, const
   a.off = group_off;
   a.x = x, a.w1 = w1, a.w3 = w3, a.w2 = w2, a.gate = gate, a.up = up, a.dy = dy;
   char* at = static_cast<char*>(ws);
-  uint16_t* h = reinterpret_cast<uint16_t*>(at);
-  uint16_t* dg = reinterpret_cast<uint16_t*>(at + plane(cfg));
-  uint16_t* du = reinterpret_cast<uint16_t*>(at + 2 * plane(cfg));
+  a.h = reinterpret_cast<uint16_t*>(at);
+  a.dgate = reinterpret_cast<uint16_t*>(at + plane(cfg));
+  a.dup = reinterpret_cast<uint16_t*>(at + 2 * plane(cfg));
+  a.dx = dx, a.dw1 = dw1, a.dw3 = dw3, a.dw2 = dw2;
   if (a.T > 0 && (dx || dw1)) {
-    const int mt = max_row_tiles(a.T, a.G, TS);
-    a.o0 = h, a.o1 = dg, a.o2 = du;
-    ffn_dh_kernel<<<dim3(a.F / TS, mt), 256, 0, s>>>(a);
-    if (dx) {
-      a.dgate = dg, a.dup = du, a.o0 = dx;
-      ffn_dx_kernel<<<dim3(a.H / TS, mt), 256, 0, s>>>(a);
-    }
+    launch_dh<tile::Wide>(a, s);
+    if (dx) launch_dx<tile::Wide>(a, s);
   }
-  if (dw1) {
-    ffn_dw_kernel<<<dim3(a.F / TS, a.H / TS, a.G), 256, 0, s>>>(a.off, a.T, x, dg, dw1, a.H, a.F);
-    ffn_dw_kernel<<<dim3(a.F / TS, a.H / TS, a.G), 256, 0, s>>>(a.off, a.T, x, du, dw3, a.H, a.F);
-    ffn_dw_kernel<<<dim3(a.H / TS, a.F / TS, a.G), 256, 0, s>>>(a.off, a.T, h, dy, dw2, a.F, a.H);
-  }
+  if (dw1) launch_dw<tile::Wide>(a, s);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include "blocks.h"
+#include "tile.h"
 
 using namespace moe;
 
@@ -62,27 +63,6 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(int K, int N, int
 }
 
 // ---- the product ----------------------------------------------------------------
-constexpr int TS = 64, KS = 64;
-
-__device__ void product(int (&acc)[4][4], const int8_t* a, int rows, const int8_t* b, int cols, int K) {
-  __shared__ int sa[TS][KS / 4 + 1], sb[TS][KS / 4 + 1];
-  const int t = threadIdx.x, tx = t % 16, ty = t / 16;
-  for (int k0 = 0; k0 < K; k0 += KS) {
-    __syncthreads();
-    for (int i = t; i < TS * (KS / 4); i += 256) {
-      const int r = i / (KS / 4), c = i % (KS / 4);
-      sa[r][c] = r < rows ? reinterpret_cast<const int*>(a + (size_t)r * K + k0)[c] : 0;
-      sb[r][c] = r < cols ? reinterpret_cast<const int*>(b + (size_t)r * K + k0)[c] : 0;
-    }
-    __syncthreads();
-    for (int k = 0; k < KS / 4; ++k)
-      for (int i = 0; i < 4; ++i)
-        for (int j = 0; j < 4; ++j)
-          for (int byte = 0; byte < 32; byte += 8)
-            acc[i][j] += (int)(int8_t)(sa[ty + 16 * i][k] >> byte) * (int)(int8_t)(sb[tx + 16 * j][k] >> byte);
-  }
-}
-
 struct I8Args {
   int T, K, N, G, act;
   const int32_t* off;
@@ -91,28 +71,46 @@ struct I8Args {
   uint16_t* y;
 };
 
-__global__ __launch_bounds__(256) void gemm_i8_kernel(I8Args a) {
-  RowTile rt;
-  int total;
-  if (!row_tile(a.off, a.G, a.T, TS, blockIdx.y, &rt, &total)) return;
-  const bool gated = a.act != MOE_ACT_NONE;
-  const int out = gated ? a.N / 2 : a.N, n0 = blockIdx.x * TS, rows = rt.end - rt.begin, cols = min(TS, out - n0);
-  const int8_t* x = a.x + (size_t)rt.begin * a.K;
-  const int8_t* w = a.w + ((size_t)rt.group * a.N + n0) * a.K;
+template <typename S>
+using I8 = tile::Tile<S, true, false, false>;
+
+template <typename Tl, bool GATED>
+__global__ __launch_bounds__(Tl::THREADS) void gemm_i8_kernel(I8Args a) {
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const RowTiles list(a.off, a.G, a.T, Tl::BM);
+  constexpr int COLS = GATED ? Tl::BN / 2 : Tl::BN;
+  const int out = GATED ? a.N / 2 : a.N;
+  int m, n;
+  if (!tile::pick(list.total, ceil_div(out, COLS), &m, &n)) return;
+  const RowTile rt = list.at(m);
+  const int n0 = n * COLS, rows = rt.end - rt.begin;
+  const char* w = reinterpret_cast<const char*>(a.w) + ((size_t)rt.group * a.N + n0) * a.K;
+  const tile::Operand A{reinterpret_cast<const char*>(a.x) + (size_t)rt.begin * a.K, nullptr, (uint32_t)a.K, rows, 0, 0};
+  const tile::Operand B{w, GATED ? w + (size_t)out * a.K : nullptr, (uint32_t)a.K, out - n0, 0, 0};
   const float* sw = a.sw + (size_t)rt.group * a.N + n0;
-  int v[4][4] = {}, u[4][4] = {};
-  product(v, x, rows, w, cols, a.K);
-  if (gated) product(u, x, rows, w + (size_t)out * a.K, cols, a.K);
-  const int tx = threadIdx.x % 16, ty = threadIdx.x / 16;
-  for (int i = 0; i < 4; ++i)
-    for (int j = 0; j < 4; ++j) {
-      const int m = ty + 16 * i, n = tx + 16 * j;
-      if (m >= rows || n >= cols) continue;
-      const float s = a.sx[rt.begin + m];
-      float r = (float)v[i][j] * (s * sw[n]);
-      if (gated) r = act_of(r, a.act) * ((float)u[i][j] * (s * sw[out + n]));
-      a.y[(size_t)(rt.begin + m) * out + n0 + n] = f32_to_bf16(r);
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, a.K, A, B, 0);
+  Tl::template epilogue<GATED>(acc, lds, rows, [&](int r, int c, const auto& v) {
+    if (n0 + c >= out) return;
+    const float sx = a.sx[rt.begin + r];
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      y[i] = (float)(int)v[i] * (sx * sw[c + i]);
+      if constexpr (GATED) y[i] = act_of(y[i], a.act) * ((float)(int)v[8 + i] * (sx * sw[out + c + i]));
     }
+    *reinterpret_cast<u32x4_t*>(a.y + (size_t)(rt.begin + r) * out + n0 + c) = tile::pack8(y);
+  });
+}
+
+template <typename S>
+void launch_gemm(const I8Args& a, hipStream_t s) {
+  using Tl = I8<S>;
+  const bool gated = a.act != MOE_ACT_NONE;
+  const int nt = gated ? ceil_div(a.N / 2, Tl::BN / 2) : ceil_div(a.N, Tl::BN);
+  const int g = tile::grid_of(max_row_tiles(a.T, a.G, Tl::BM), nt);
+  (gated ? gemm_i8_kernel<Tl, true> : gemm_i8_kernel<Tl, false>)<<<g, Tl::THREADS, 0, s>>>(a);
 }
 
 moe_status check_cfg(const moe_gemm_i8_config* c) {
@@ -188,8 +186,7 @@ moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const fl
     return fail(MOE_ERR_INVALID_ARG, "the workspace holds %zu of %zu bytes", ws ? ws_bytes : 0, ws_size(cfg));
   if (reinterpret_cast<uintptr_t>(ws) % 256) return fail(MOE_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
   I8Args a{cfg->rows, cfg->depth, cfg->channels, cfg->n_groups, cfg->act, group_off, xq, wq, x_scale, w_scale, y};
-  const int out = cfg->act == MOE_ACT_NONE ? cfg->channels : cfg->channels / 2;
-  gemm_i8_kernel<<<dim3(ceil_div(out, TS), max_row_tiles(a.T, a.G, TS)), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+  launch_gemm<tile::Wide>(a, reinterpret_cast<hipStream_t>(stream));
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }

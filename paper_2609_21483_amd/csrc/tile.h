@@ -1,0 +1,374 @@
+// Matrix-core tiles of the products over row groups (ffn.hip, int8.hip):
+// C[BM x BN] = A[BM x K] B[K x BN], bf16 or int8 operands read where they lie.
+//
+// An operand is k-contiguous (rows of the tile, each a run of the depth) or
+// transposed (rows of the depth, each a run of the tile's rows or columns):
+// weights [H][F] are the latter for x W and the former for d W^T, and both
+// operands of x^T d are.  No pass over the weights lays them out first.
+//
+// A stage of the depth is 128 bytes of it: 64 bf16 or 128 int8 values, BM * 128
+// and BN * 128 bytes, loaded straight into LDS (global_load_lds_dwordx4), two
+// stages in turn.  LDS images, in 16-byte granules:
+//  - k-contiguous: row r at r * 128 bytes, granule c at position c ^ (r & 7).
+//    A fragment (lane: row l % 32, 16 bytes of the depth) is one ds_read_b128,
+//    and eight consecutive lanes read eight different positions.
+//  - transposed (bf16): two panels of half the tile's width, each 64 depth rows
+//    of PW columns; granule c of row k at position c ^ swz(k).  A fragment is
+//    two ds_read_b64_tr_b16: 16 lanes address 4 depth rows x 16 columns, lane
+//    i at row i / 4, columns 4 (i % 4), and lane i receives column i of all 4.
+//    The swizzle puts the four rows' 64-byte pieces (32 columns) on different
+//    banks.
+// Panels also let a gated tile take half of its columns from each matrix: a
+// wave's first NB / 2 column blocks lie in panel 0 and the others, the same
+// columns, in panel 1.
+//
+// WM x WN waves, each MB x NB blocks of 32 x 32 (v_mfma_f32_32x32x16_bf16,
+// v_mfma_i32_32x32x32_i8).  Row block b of the tile belongs to wave row
+// b % WM.  B is the first operand of the instruction, so that a lane's
+// accumulators are 4 consecutive columns of one row: column 8 (r / 4) + 4 (l /
+// 32) + r % 4 of row l % 32 in register r.
+#pragma once
+
+#include "common.h"
+#include "gemm.h"
+
+namespace moe {
+namespace tile {
+
+using gemm::compiler_fence;
+using gemm::dma16;
+using gemm::lds_barrier;
+using gemm::lds_u32;
+using gemm::uniform_ptr;
+using gemm::wait_vm;
+
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((__vector_size__(4 * sizeof(short))));
+typedef short s16x8_t __attribute__((__vector_size__(8 * sizeof(short))));
+
+constexpr int DEPTH = 128;  // bytes of the depth per stage
+
+// One operand's matrix as a tile sees it: `p` and, for the second panel, `p2`
+// (the same matrix, or the up projection's) are the addresses of depth 0; ld
+// the bytes between rows.  k-contiguous: `valid` rows exist from p on, rows
+// from half the tile on are read at p2 (gated) or behind p (p2 = NULL).
+// Transposed: columns [col, cols) of the matrix exist, a panel starts at col
+// (+ PW in panel 1 unless p2 is given).
+struct Operand {
+  const char *p, *p2;
+  uint32_t ld;
+  int valid, col, cols;
+};
+
+template <int WM_, int WN_, int MB_, int NB_>
+struct Shape {
+  static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_;
+};
+using Wide = Shape<2, 4, 4, 2>;   // 256 x 256
+using Small = Shape<2, 2, 2, 2>;  // 128 x 128
+
+template <typename S, bool I8_, bool AT_, bool BT_>
+struct Tile {
+  static constexpr int WM = S::WM, WN = S::WN, MB = S::MB, NB = S::NB;
+  static constexpr bool I8 = I8_, AT = AT_, BT = BT_;
+  static constexpr int NW = WM * WN, BM = WM * MB * 32, BN = WN * NB * 32;
+  static constexpr int A_BYTES = BM * DEPTH, B_BYTES = BN * DEPTH, STAGE = A_BYTES + B_BYTES;
+  static constexpr int AI = BM / 8 / NW, BI = BN / 8 / NW, INSTR = AI + BI;  // DMA instructions of a wave per stage
+  static constexpr int THREADS = NW * 64;
+  static constexpr int EPI = WM * 32 * BN * 4;  // bytes of one staged set of row blocks (fp32)
+  static constexpr int LDS = 2 * STAGE > 2 * EPI ? 2 * STAGE : 2 * EPI;
+  static_assert(AI * NW * 8 == BM && BI * NW * 8 == BN && NB % 2 == 0, "tile shape");
+  static_assert(!I8 || (!AT && !BT), "int8 operands are k-contiguous");
+  using Acc1 = std::conditional_t<I8, i32x16_t, f32x16_t>;
+  typedef Acc1 Acc[MB][NB];
+  using Frag = std::conditional_t<I8, i32x4_t, bf16x8_t>;
+
+  template <bool TR, int ROWS, int N>
+  struct Offs {
+    uint32_t o[N];
+  };
+
+  // Byte offsets of a wave's DMA lanes from the operand's base; `last` the
+  // valid depth rows of the stage (transposed operands; 64 except in the end)
+  template <bool TR, int ROWS, int N>
+  static __device__ __forceinline__ void offsets(uint32_t (&o)[N], const Operand& m, int wave, int lane, int last) {
+    if constexpr (TR) {
+      constexpr int PW = ROWS / 2, RPI = 512 / PW, IPP = 64 / RPI, GR = PW / 8;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int j = wave * N + i, panel = j / IPP, k = (j % IPP) * RPI + lane / GR;
+        const int c = (lane % GR) ^ swz<PW>(k);
+        const int col = m.col + c * 8 + (m.p2 ? 0 : panel * PW);
+        o[i] = (uint32_t)min(k, last - 1) * m.ld + (uint32_t)min(col, m.cols - 8) * 2u;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int r = (wave * N + i) * 8 + (lane >> 3);
+        const int rr = m.p2 && r >= ROWS / 2 ? r - ROWS / 2 : r;
+        o[i] = (uint32_t)min(rr, m.valid - 1) * m.ld + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+      }
+    }
+  }
+  template <int PW>
+  static __device__ __forceinline__ int swz(int k) {
+    return PW == 128 ? 4 * (k & 3) : 4 * ((k >> 1) & 1);
+  }
+  // the base a wave's DMA reads from (its instructions are all of one panel)
+  template <int ROWS, int N>
+  static __device__ __forceinline__ const char* base_of(const Operand& m, int wave) {
+    static_assert((ROWS / 16) % N == 0, "a wave's DMA stays in one half");
+    return uniform_ptr(m.p2 && wave * N * 8 >= ROWS / 2 ? m.p2 : m.p);
+  }
+
+  struct FragOffs {
+    uint32_t a[AT ? MB : 4], b[BT ? NB : 4];
+  };
+  static __device__ __forceinline__ FragOffs frag_offsets(int wm, int wn, int lane) {
+    FragOffs f;
+    if constexpr (AT) {
+      constexpr int PW = BM / 2;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const int row = (mb * WM + wm) * 32;
+        f.a[mb] = tr_offset<PW>(row / PW, row % PW, lane);
+      }
+    } else {
+      const int r = wm * 32 + (lane & 31);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk) f.a[kk] = (uint32_t)(r * DEPTH + ((kk * 2 + (lane >> 5)) ^ (r & 7)) * 16);
+    }
+    if constexpr (BT) {
+      constexpr int PW = BN / 2;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+        f.b[nb] = A_BYTES + tr_offset<PW>(nb / (NB / 2), (wn * (NB / 2) + nb % (NB / 2)) * 32, lane);
+    } else {
+      const int r = wn * (NB / 2) * 32 + (lane & 31);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        f.b[kk] = (uint32_t)(A_BYTES + r * DEPTH + ((kk * 2 + (lane >> 5)) ^ (r & 7)) * 16);
+    }
+    return f;
+  }
+  template <int PW>
+  static __device__ __forceinline__ uint32_t tr_offset(int panel, int col, int lane) {
+    const int k = (lane >> 5) * 8 + ((lane & 15) >> 2);
+    const int c = (col >> 3) + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+    return (uint32_t)(panel * 64 * PW * 2 + k * PW * 2 + (c ^ swz<PW>(k)) * 16 + (lane & 1) * 8);
+  }
+  template <int PW>
+  static __device__ __forceinline__ Frag read_tr(const char* st, uint32_t off, int kk) {
+    typedef __attribute__((address_space(3))) s16x4_t* P;
+    const char* p = st + off + kk * 16 * PW * 2;
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p));
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 4 * PW * 2));
+    return __builtin_bit_cast(Frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  // byte distance of column block nb from a wave's first (k-contiguous B)
+  static constexpr int nb_bytes(int nb) { return (nb / (NB / 2) * (BN / 2) + nb % (NB / 2) * 32) * DEPTH; }
+
+  static __device__ __forceinline__ void load_frags(const char* st, int kk, const FragOffs& f, Frag (&a)[MB], Frag (&b)[NB]) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if constexpr (BT) b[nb] = read_tr<BN / 2>(st, f.b[nb], kk);
+      else b[nb] = *reinterpret_cast<const Frag*>(st + f.b[kk] + nb_bytes(nb));
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      if constexpr (AT) a[mb] = read_tr<BM / 2>(st, f.a[mb], kk);
+      else a[mb] = *reinterpret_cast<const Frag*>(st + f.a[kk] + mb * WM * 32 * DEPTH);
+    }
+  }
+  static __device__ __forceinline__ void multiply(Acc& acc, const Frag (&a)[MB], const Frag (&b)[NB]) {
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        if constexpr (I8) acc[mb][nb] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[nb], a[mb], acc[mb][nb], 0, 0, 0);
+        else acc[mb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[nb], a[mb], acc[mb][nb], 0, 0, 0);
+      }
+  }
+
+  // acc += A B over the depth in [0, n1), and of a second pair of operands
+  // (A2, B2: same shapes) over n2 more; depths in elements.  Depths are
+  // multiples of 64 (int8: the second half of a last stage is not multiplied)
+  // or, where both operands are transposed, any (the rows behind the end are
+  // cleared in LDS, so that whatever lies there, NaN too, adds nothing).
+  static __device__ __forceinline__ void run(Acc& acc, char* lds, const Operand& A, const Operand& B, int n1,
+                                             const Operand& A2, const Operand& B2, int n2) {
+    constexpr int KE = I8 ? 128 : 64;  // depth elements of a stage
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    const int half = (n1 + KE - 1) / KE, ns = half + (n2 + KE - 1) / KE;
+    if (ns == 0) return;
+    uint32_t oa[AI], ob[BI];
+    offsets<AT, BM, AI>(oa, A, wave, lane, 64);
+    offsets<BT, BN, BI>(ob, B, wave, lane, 64);
+    const char *pa = base_of<BM, AI>(A, wave), *pb = base_of<BN, BI>(B, wave);
+    const char *pa2 = n2 ? base_of<BM, AI>(A2, wave) : nullptr, *pb2 = n2 ? base_of<BN, BI>(B2, wave) : nullptr;
+    const size_t sa = AT ? (size_t)A.ld * 64 : DEPTH, sb = BT ? (size_t)B.ld * 64 : DEPTH;
+    const uint32_t la = lds_u32(lds) + wave * AI * 1024, lb = lds_u32(lds) + A_BYTES + wave * BI * 1024;
+    const int rest = n1 % KE;  // depth of the last stage, 0: whole (only without a second pair)
+    auto issue = [&](int s) {
+      const uint32_t so = (s & 1) * STAGE;
+      const char* a = s < half ? pa + s * sa : pa2 + (s - half) * sa;
+      const char* b = s < half ? pb + s * sb : pb2 + (s - half) * sb;
+      if ((AT && BT) && rest && s == ns - 1) {
+        uint32_t ta[AI], tb[BI];
+        offsets<AT, BM, AI>(ta, A, wave, lane, rest);
+        offsets<BT, BN, BI>(tb, B, wave, lane, rest);
+#pragma unroll
+        for (int i = 0; i < AI; ++i) dma16(a, ta[i], la + so + i * 1024);
+#pragma unroll
+        for (int i = 0; i < BI; ++i) dma16(b, tb[i], lb + so + i * 1024);
+        return;
+      }
+      // (int8: a last stage of 64 has no granules 4..7; they are read as 0..3)
+      const uint32_t back = I8 && rest && s == ns - 1 && (((lane & 7) ^ (lane >> 3)) & 4) ? 64 : 0;
+#pragma unroll
+      for (int i = 0; i < AI; ++i) dma16(a, oa[i] - back, la + so + i * 1024);
+#pragma unroll
+      for (int i = 0; i < BI; ++i) dma16(b, ob[i] - back, lb + so + i * 1024);
+    };
+    // clears the depth rows from `rest` on of a stage of transposed operands
+    auto clear = [&](char* st) {
+      if constexpr (AT && BT) {
+        for (int i = threadIdx.x; i < STAGE / 16; i += THREADS) {
+          constexpr int RA = BM / 2 * 2 / 16, RB = BN / 2 * 2 / 16;  // granules per depth row of a panel
+          const int k = i < A_BYTES / 16 ? i / RA % 64 : (i - A_BYTES / 16) / RB % 64;
+          if (k >= rest) *reinterpret_cast<u32x4_t*>(st + i * 16) = u32x4_t{0, 0, 0, 0};
+        }
+        lds_barrier();
+      }
+    };
+    const FragOffs f = frag_offsets(wm, wn, lane);
+    Frag a0[MB], b0[NB], a1[MB], b1[NB];
+    issue(0);
+    if (ns > 1) {
+      issue(1);
+      wait_vm<INSTR>();
+    } else {
+      wait_vm<0>();
+    }
+    __builtin_amdgcn_s_barrier();
+    compiler_fence();
+    if ((AT && BT) && rest && ns == 1) clear(lds);
+    load_frags(lds, 0, f, a0, b0);
+    const int whole = I8 && rest ? ns - 1 : ns;
+    for (int s = 0; s < whole; ++s) {
+      const char* st = lds + (s & 1) * STAGE;
+      char* nx = lds + (~s & 1) * STAGE;
+      load_frags(st, 1, f, a1, b1);
+      multiply(acc, a0, b0);
+      load_frags(st, 2, f, a0, b0);
+      multiply(acc, a1, b1);
+      load_frags(st, 3, f, a1, b1);
+      multiply(acc, a0, b0);
+      // this wave's reads of the stage have arrived and so has its part of the
+      // next one: after the barrier everyone's have, and the stage is free
+      compiler_fence();
+      __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0) lgkmcnt(0)
+      __builtin_amdgcn_s_barrier();
+      compiler_fence();
+      if (s + 2 < ns) issue(s + 2);
+      if (s + 1 < ns) {
+        if ((AT && BT) && rest && s + 2 == ns) clear(nx);
+        load_frags(nx, 0, f, a0, b0);
+      }
+      multiply(acc, a1, b1);
+    }
+    if (whole < ns) {
+      const char* st = lds + (whole & 1) * STAGE;
+      load_frags(st, 1, f, a1, b1);
+      multiply(acc, a0, b0);
+      multiply(acc, a1, b1);
+    }
+    lds_barrier();
+  }
+
+  static __device__ __forceinline__ void zero(Acc& acc) {
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[mb][nb][r] = 0;
+  }
+
+  // Hands out the tile by rows: fn(row, col, v) for every 8 consecutive
+  // columns of a row, row < rows.  col counts the tile's columns; GATED: the
+  // columns of panel 0, v[0..7] theirs and v[8..15] panel 1's.  Accumulators
+  // pass through LDS one set of WM row blocks at a time (two buffers, one
+  // barrier each), 16-byte granules at position c ^ (row & 15).
+  template <bool GATED, typename Fn>
+  static __device__ __forceinline__ void epilogue(const Acc& acc, char* lds, int rows, Fn&& fn) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM;
+    constexpr int SET = WM * 32, PPR = (GATED ? BN / 2 : BN) / 8;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+      if (mb * SET >= rows) break;
+      char* buf = lds + (mb & 1) * EPI;
+      const int sr = wm * 32 + (lane & 31);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = nb / (NB / 2) * (BN / 2) + (wn * (NB / 2) + nb % (NB / 2)) * 32 + q * 8 + (lane >> 5) * 4;
+          u32x4_t v;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            if constexpr (I8) v[r] = (uint32_t)acc[mb][nb][q * 4 + r];
+            else v[r] = __float_as_uint(acc[mb][nb][q * 4 + r]);
+          }
+          *reinterpret_cast<u32x4_t*>(buf + sr * BN * 4 + ((col / 4) ^ (sr & 15)) * 16) = v;
+        }
+      lds_barrier();
+#pragma unroll
+      for (int i = 0; i < SET * PPR / THREADS; ++i) {
+        const int piece = (int)threadIdx.x + i * THREADS, r = piece / PPR, c = piece % PPR * 8;
+        if (mb * SET + r < rows) {
+          uint32_t v[GATED ? 16 : 8];
+#pragma unroll
+          for (int p = 0; p < (GATED ? 4 : 2); ++p) {
+            const int g = (c + p / 2 * (BN / 2)) / 4 + p % 2;
+            *reinterpret_cast<u32x4_t*>(v + p * 4) =
+                *reinterpret_cast<const u32x4_t*>(buf + r * BN * 4 + (g ^ (r & 15)) * 16);
+          }
+          fn(mb * SET + r, c, v);
+        }
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ u32x4_t pack8(const float (&v)[8]) {
+  return u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void unpack8(u32x4_t w, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = bf16_lo(w[i]);
+    v[2 * i + 1] = bf16_hi(w[i]);
+  }
+}
+
+// The tile of this workgroup among mt row tiles x nt column tiles: workgroup i
+// runs on XCD i % 8, and each XCD takes a run of consecutive tiles, ordered so
+// that 8 row tiles share each column tile's operand while it is in the XCD's
+// L2.  False: no tile (the grid is sized for the most row tiles there can be).
+constexpr int NEAR = 8;
+__device__ __forceinline__ bool pick(int mt, int nt, int* m, int* n) {
+  const int total = mt * nt, chunk = ceil_div(total, NXCD), t = (blockIdx.x % NXCD) * chunk + blockIdx.x / NXCD;
+  if ((int)(blockIdx.x / NXCD) >= chunk || t >= total) return false;
+  const int band = t / (NEAR * nt), first = band * NEAR, wide = min(NEAR, mt - first), in = t - band * NEAR * nt;
+  *m = first + in % wide;
+  *n = in / wide;
+  return true;
+}
+inline int grid_of(long long mt, int nt) { return (int)((mt * nt + NXCD - 1) / NXCD * NXCD); }
+
+}  // namespace tile
+}  // namespace moe
