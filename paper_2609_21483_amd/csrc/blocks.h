@@ -95,6 +95,14 @@ struct RowTiles {
   }
 };
 
+// The rows that some group has: [begin, end).
+__device__ __forceinline__ void covered_rows(const int32_t* off, int G, int T, int* begin, int* end) {
+  int e;
+  group_rows(off, T, 0, begin, &e);
+  if (G > 1) group_rows(off, T, G - 1, &e, end);
+  else *end = e;
+}
+
 // most row tiles a list can have
 __host__ __device__ inline int max_row_tiles(int T, int G, int bm) {
   const int full = T / bm + G;  // every group ends in a partial tile

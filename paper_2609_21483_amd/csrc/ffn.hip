@@ -1,6 +1,8 @@
 // The gated feed-forward block over row groups and its backward pass (moe.h).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "blocks.h"
 #include "tile.h"
 
@@ -15,176 +17,265 @@ struct FfnArgs {
   uint16_t *h, *dgate, *dup;       // workspace
   uint16_t *kgate, *kup, *y;       // forward's outputs (kgate and kup may be NULL)
   uint16_t *dx, *dw1, *dw3, *dw2;  // backward's (dx, or the three dw, may be NULL)
+  float* part;                     // partial sums [split][T][width] of a split product
+  int split;
 };
 
 __device__ __forceinline__ const char* bytes(const uint16_t* p) { return reinterpret_cast<const char*>(p); }
+
+// The four products over rows.  UP: h = act(x W1) * (x W3), DOWN: y = h W2,
+// DH: dh = dy W2^T and what follows from it, DX: dx = dgate W1^T + dup W3^T
+// (one depth of 2 F).
+enum Op { UP, DOWN, DH, DX };
+
+template <Op OP>
+constexpr bool GATED = OP == UP;
+// columns of the output, depth, and columns of the partial sums
+template <Op OP>
+__host__ __device__ inline int cols_of(const FfnArgs& a) { return OP == UP || OP == DH ? a.F : a.H; }
+template <Op OP>
+__host__ __device__ inline int depth_of(const FfnArgs& a) { return OP == DOWN ? a.F : OP == DX ? 2 * a.F : a.H; }
+template <Op OP>
+__host__ __device__ inline int sums_of(const FfnArgs& a) { return OP == UP ? 2 * a.F : cols_of<OP>(a); }
+
 __device__ __forceinline__ void store8(uint16_t* p, const float (&v)[8]) {
   *reinterpret_cast<u32x4_t*>(p) = tile::pack8(v);
 }
 
-// Forms of the tile: x W (weights transposed), d W^T, and x^T d
-template <typename S>
-using XW = tile::Tile<S, false, false, true>;
-template <typename S>
-using XWT = tile::Tile<S, false, false, false>;
-template <typename S>
-using XTD = tile::Tile<S, false, true, true>;
-
-// h = act(x W1) * (x W3), and gate and up where they are kept
-template <typename Tl>
-__global__ __launch_bounds__(Tl::THREADS) void ffn_up_kernel(FfnArgs a) {
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-  const RowTiles list(a.off, a.G, a.T, Tl::BM);
-  constexpr int COLS = Tl::BN / 2;
-  int m, n;
-  if (!tile::pick(list.total, ceil_div(a.F, COLS), &m, &n)) return;
-  const RowTile rt = list.at(m);
-  const int n0 = n * COLS, rows = rt.end - rt.begin;
-  const size_t wo = (size_t)rt.group * a.H * a.F;
-  const tile::Operand A{bytes(a.x + (size_t)rt.begin * a.H), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
-  const tile::Operand B{bytes(a.w1 + wo), bytes(a.w3 + wo), (uint32_t)a.F * 2, 0, n0, a.F};
-  typename Tl::Acc acc;
-  Tl::zero(acc);
-  Tl::run(acc, lds, A, B, a.H, A, B, 0);
-  Tl::template epilogue<true>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[16]) {
-    if (n0 + c >= a.F) return;
-    const size_t at = (size_t)(rt.begin + r) * a.F + n0 + c;
-    float g[8], u[8], h[8];
+// 8 columns of a row from their fp32 sums (UP: v[8..15] the up projection's).
+// h, d gate and d up are rounded to bf16 for the matrix instructions that take
+// them: 2^-8 of each value at most, which their products' sums average out.
+template <Op OP>
+__device__ __forceinline__ void finish(const FfnArgs& a, size_t row, int col, const float* v) {
+  const size_t at = row * cols_of<OP>(a) + col;
+  float p[8], q[8], r[8];
+  if constexpr (OP == UP) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      g[i] = __uint_as_float(v[i]);
-      u[i] = __uint_as_float(v[8 + i]);
-      h[i] = act_of(g[i], a.act) * u[i];
+      p[i] = v[i];
+      q[i] = v[8 + i];
+      r[i] = act_of(p[i], a.act) * q[i];
     }
-    store8(a.h + at, h);
+    store8(a.h + at, r);
     if (a.kgate) {
-      store8(a.kgate + at, g);
-      store8(a.kup + at, u);
+      store8(a.kgate + at, p);
+      store8(a.kup + at, q);
     }
-  });
-}
-
-// y = h W2
-template <typename Tl>
-__global__ __launch_bounds__(Tl::THREADS) void ffn_down_kernel(FfnArgs a) {
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-  const RowTiles list(a.off, a.G, a.T, Tl::BM);
-  int m, n;
-  if (!tile::pick(list.total, ceil_div(a.H, Tl::BN), &m, &n)) return;
-  const RowTile rt = list.at(m);
-  const int n0 = n * Tl::BN, rows = rt.end - rt.begin;
-  const tile::Operand A{bytes(a.h + (size_t)rt.begin * a.F), nullptr, (uint32_t)a.F * 2, rows, 0, 0};
-  const tile::Operand B{bytes(a.w2 + (size_t)rt.group * a.F * a.H), nullptr, (uint32_t)a.H * 2, 0, n0, a.H};
-  typename Tl::Acc acc;
-  Tl::zero(acc);
-  Tl::run(acc, lds, A, B, a.F, A, B, 0);
-  Tl::template epilogue<false>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[8]) {
-    if (n0 + c < a.H) store8(a.y + (size_t)(rt.begin + r) * a.H + n0 + c, __builtin_bit_cast(float[8], v));
-  });
-}
-
-// dh = dy W2^T, and from it h = act(gate) * up again, d gate and d up
-template <typename Tl>
-__global__ __launch_bounds__(Tl::THREADS) void ffn_dh_kernel(FfnArgs a) {
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-  const RowTiles list(a.off, a.G, a.T, Tl::BM);
-  int m, n;
-  if (!tile::pick(list.total, ceil_div(a.F, Tl::BN), &m, &n)) return;
-  const RowTile rt = list.at(m);
-  const int n0 = n * Tl::BN, rows = rt.end - rt.begin;
-  const tile::Operand A{bytes(a.dy + (size_t)rt.begin * a.H), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
-  const tile::Operand B{bytes(a.w2 + ((size_t)rt.group * a.F + n0) * a.H), nullptr, (uint32_t)a.H * 2, a.F - n0, 0, 0};
-  typename Tl::Acc acc;
-  Tl::zero(acc);
-  Tl::run(acc, lds, A, B, a.H, A, B, 0);
-  Tl::template epilogue<false>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[8]) {
-    if (n0 + c >= a.F) return;
-    const size_t at = (size_t)(rt.begin + r) * a.F + n0 + c;
-    float g[8], u[8], h[8];
-    tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.gate + at), g);
-    tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.up + at), u);
+  } else if constexpr (OP == DH) {
+    tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.gate + at), p);
+    tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.up + at), q);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float s, ds;
-      act_grad(g[i], a.act, &s, &ds);
-      const float d = __uint_as_float(v[i]);
-      h[i] = s * u[i];
-      g[i] = d * u[i] * ds;
-      u[i] = d * s;
+      act_grad(p[i], a.act, &s, &ds);
+      r[i] = s * q[i];
+      p[i] = v[i] * q[i] * ds;
+      q[i] = v[i] * s;
     }
-    store8(a.h + at, h);
-    store8(a.dgate + at, g);
-    store8(a.dup + at, u);
-  });
+    store8(a.h + at, r);
+    store8(a.dgate + at, p);
+    store8(a.dup + at, q);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = v[i];
+    store8((OP == DOWN ? a.y : a.dx) + at, p);
+  }
 }
 
-// dx = dgate W1^T + dup W3^T, one depth of 2 F
-template <typename Tl>
-__global__ __launch_bounds__(Tl::THREADS) void ffn_dx_kernel(FfnArgs a) {
+// The same, or the partial sums where the product is split.
+template <Op OP>
+__device__ __forceinline__ void put(const FfnArgs& a, int part, size_t row, int col, const uint32_t* v) {
+  constexpr int N = GATED<OP> ? 16 : 8;
+  if (a.split > 1) {
+    float* p = a.part + ((size_t)part * a.T + row) * sums_of<OP>(a) + col;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i)
+      *reinterpret_cast<u32x4_t*>(p + i / 2 * a.F + i % 2 * 4) = u32x4_t{v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]};
+    return;
+  }
+  float f[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = __uint_as_float(v[i]);
+  finish<OP>(a, row, col, f);
+}
+
+// Operands of a tile: rows of A from depth k on (elements), and W's columns
+// from n0 on.  UP and DOWN read the weights transposed, DH and DX as they lie.
+template <Op OP>
+__device__ __forceinline__ tile::Operand rows_op(const FfnArgs& a, const RowTile& rt, int k) {
+  const uint16_t* p = OP == UP ? a.x : OP == DOWN ? a.h : OP == DH ? a.dy : k < a.F ? a.dgate : a.dup - a.F;
+  const int ld = OP == DX ? a.F : depth_of<OP>(a);
+  return {bytes(p + (size_t)rt.begin * ld + k), nullptr, (uint32_t)ld * 2, rt.end - rt.begin, 0, 0};
+}
+template <Op OP>
+__device__ __forceinline__ tile::Operand weights_op(const FfnArgs& a, const RowTile& rt, int k, int n0) {
+  const size_t wo = (size_t)rt.group * a.H * a.F;
+  if constexpr (OP == UP) {
+    const size_t at = wo + (size_t)k * a.F;
+    return {bytes(a.w1 + at), bytes(a.w3 + at), (uint32_t)a.F * 2, 0, n0, a.F};
+  } else if constexpr (OP == DOWN) {
+    return {bytes(a.w2 + wo + (size_t)k * a.H), nullptr, (uint32_t)a.H * 2, 0, n0, a.H};
+  } else if constexpr (OP == DH) {
+    return {bytes(a.w2 + wo + (size_t)n0 * a.H + k), nullptr, (uint32_t)a.H * 2, a.F - n0, 0, 0};
+  } else {
+    const uint16_t* w = k < a.F ? a.w1 : a.w3 - a.F;
+    return {bytes(w + wo + (size_t)n0 * a.F + k), nullptr, (uint32_t)a.F * 2, a.H - n0, 0, 0};
+  }
+}
+
+template <Op OP, typename S>
+__global__ __launch_bounds__(S::THREADS) void ffn_kernel(FfnArgs a) {
+  using Tl = tile::Tile<S, false, false, OP == UP || OP == DOWN>;
   __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
   const RowTiles list(a.off, a.G, a.T, Tl::BM);
+  constexpr int COLS = GATED<OP> ? Tl::BN / 2 : Tl::BN;
+  const int nt = ceil_div(cols_of<OP>(a), COLS), stages = depth_of<OP>(a) / 64;
   int m, n;
-  if (!tile::pick(list.total, ceil_div(a.H, Tl::BN), &m, &n)) return;
+  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
   const RowTile rt = list.at(m);
-  const int n0 = n * Tl::BN, rows = rt.end - rt.begin;
-  const size_t ro = (size_t)rt.begin * a.F, wo = ((size_t)rt.group * a.H + n0) * a.F;
-  const uint32_t ld = (uint32_t)a.F * 2;
-  const tile::Operand A{bytes(a.dgate + ro), nullptr, ld, rows, 0, 0}, A2{bytes(a.dup + ro), nullptr, ld, rows, 0, 0};
-  const tile::Operand B{bytes(a.w1 + wo), nullptr, ld, a.H - n0, 0, 0}, B2{bytes(a.w3 + wo), nullptr, ld, a.H - n0, 0, 0};
+  const int part = n / nt, n0 = n % nt * COLS, rows = rt.end - rt.begin;
+  const int k0 = stages * part / a.split * 64, k1 = stages * (part + 1) / a.split * 64;
+  // DX: the depth's second half is another pair of operands
+  const int mid = OP == DX ? min(max(k0, a.F), k1) : k1;
   typename Tl::Acc acc;
   Tl::zero(acc);
-  Tl::run(acc, lds, A, B, a.F, A2, B2, a.F);
-  Tl::template epilogue<false>(acc, lds, rows, [&](int r, int c, const uint32_t (&v)[8]) {
-    if (n0 + c < a.H) store8(a.dx + (size_t)(rt.begin + r) * a.H + n0 + c, __builtin_bit_cast(float[8], v));
+  Tl::run(acc, lds, rows_op<OP>(a, rt, k0), weights_op<OP>(a, rt, k0, n0), mid - k0, rows_op<OP>(a, rt, mid),
+          weights_op<OP>(a, rt, mid, n0), k1 - mid);
+  Tl::template epilogue<GATED<OP>>(acc, lds, rows, [&](int r, int c, const auto& v) {
+    if (n0 + c < cols_of<OP>(a)) put<OP>(a, part, rt.begin + r, n0 + c, v);
   });
 }
 
-// dW1 = x^T dgate, dW3 = x^T dup, dW2 = h^T dy, each group's
-template <typename Tl>
-__global__ __launch_bounds__(Tl::THREADS) void ffn_dw_kernel(FfnArgs a) {
+template <Op OP, int NW>
+using FewOf = tile::Few<NW, false, true, GATED<OP>>;
+
+template <Op OP, int NW>
+__global__ __launch_bounds__(NW * 64) void ffn_few_kernel(FfnArgs a) {
+  using Fw = FewOf<OP, NW>;
+  __shared__ __attribute__((aligned(1024))) char lds[Fw::LDS];
+  const RowTiles list(a.off, a.G, a.T, Fw::BM);
+  const int nt = cols_of<OP>(a) / Fw::COLS, steps = depth_of<OP>(a) / Fw::KE;
+  int m, n;
+  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
+  const RowTile rt = list.at(m);
+  const int part = n / nt, n0 = n % nt * Fw::COLS;
+  Fw::run(lds, rows_op<OP>(a, rt, 0), weights_op<OP>(a, rt, 0, n0), steps * part / a.split, steps * (part + 1) / a.split,
+          [&](int r, int c, const auto& v) { put<OP>(a, part, rt.begin + r, n0 + c, v); });
+}
+
+// The partial sums of a split product, added in order.
+template <Op OP>
+__global__ __launch_bounds__(256) void ffn_sum_kernel(FfnArgs a) {
+  int b, e;
+  covered_rows(a.off, a.G, a.T, &b, &e);
+  const int width = cols_of<OP>(a);
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8, row = i / width, c = i % width;
+  if (row < b || row >= e) return;
+  float v[GATED<OP> ? 16 : 8] = {};
+  for (int s = 0; s < a.split; ++s) {
+    const float* at = a.part + ((size_t)s * a.T + row) * sums_of<OP>(a) + c;
+#pragma unroll
+    for (int j = 0; j < (GATED<OP> ? 16 : 8); ++j) v[j] += at[j / 8 * a.F + j % 8];
+  }
+  finish<OP>(a, row, (int)c, v);
+}
+
+// dW1 = x^T dgate, dW3 = x^T dup, dW2 = h^T dy, each group's: its rows are the
+// depth, in stages of 64; a split takes runs of whole stages.
+template <typename S>
+__global__ __launch_bounds__(S::THREADS) void ffn_dw_kernel(FfnArgs a) {
+  using Tl = tile::Tile<S, false, true, true>;
   __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-  // tiles of a group: those of dW1, of dW3, then of dW2
+  // tiles of a group: those of dW1, of dW3, then of dW2 (each XCD takes an
+  // eighth of every group's: groups differ in depth)
   const int hm = ceil_div(a.H, Tl::BM), fn = ceil_div(a.F, Tl::BN), fm = ceil_div(a.F, Tl::BM), hn = ceil_div(a.H, Tl::BN);
-  const int t13 = hm * fn, per = 2 * t13 + fm * hn, chunk = gridDim.x / NXCD;
-  const int t = (blockIdx.x % NXCD) * chunk + blockIdx.x / NXCD;
-  if (t >= per * a.G) return;
-  const int g = t / per, i = t % per, which = i / t13 < 2 ? i / t13 : 2;
+  const int t13 = hm * fn, per = 2 * t13 + fm * hn, run = ceil_div(per * a.split, NXCD);
+  const int slot = blockIdx.x / NXCD, g = slot / run, w = (blockIdx.x % NXCD) * run + slot % run;
+  if (w >= per * a.split) return;
+  const int part = w / per, i = w % per, which = i / t13 < 2 ? i / t13 : 2;
   int b, e;
   group_rows(a.off, a.T, g, &b, &e);
+  const int stages = ceil_div(e - b, 64), k0 = stages * part / a.split * 64, k1 = min(stages * (part + 1) / a.split * 64, e - b);
   const uint16_t *p = which == 2 ? a.h : a.x, *q = which == 0 ? a.dgate : which == 1 ? a.dup : a.dy;
   const int M = which == 2 ? a.F : a.H, N = which == 2 ? a.H : a.F, mt = which == 2 ? fm : hm, nt = which == 2 ? hn : fn;
   const int j = i - which * t13, band = j / (tile::NEAR * nt), first = band * tile::NEAR;
   const int wide = min(tile::NEAR, mt - first), in = j - band * tile::NEAR * nt;
   const int m0 = (first + in % wide) * Tl::BM, n0 = in / wide * Tl::BN;
-  const tile::Operand A{bytes(p + (size_t)b * M), nullptr, (uint32_t)M * 2, 0, m0, M};
-  const tile::Operand B{bytes(q + (size_t)b * N), nullptr, (uint32_t)N * 2, 0, n0, N};
+  const tile::Operand A{bytes(p + (size_t)(b + k0) * M), nullptr, (uint32_t)M * 2, 0, m0, M};
+  const tile::Operand B{bytes(q + (size_t)(b + k0) * N), nullptr, (uint32_t)N * 2, 0, n0, N};
   typename Tl::Acc acc;
   Tl::zero(acc);
-  Tl::run(acc, lds, A, B, e - b, A, B, 0);
-  uint16_t* out = (which == 0 ? a.dw1 : which == 1 ? a.dw3 : a.dw2) + ((size_t)g * M + m0) * N + n0;
+  Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
+  const size_t at = ((size_t)g * M + m0) * N + n0, all = (size_t)a.G * a.H * a.F;
+  uint16_t* out = (which == 0 ? a.dw1 : which == 1 ? a.dw3 : a.dw2) + at;
+  float* sums = a.part + (part * 3 + which) * all + at;
   Tl::template epilogue<false>(acc, lds, min(Tl::BM, M - m0), [&](int r, int c, const uint32_t (&v)[8]) {
-    if (n0 + c < N) store8(out + (size_t)r * N + c, __builtin_bit_cast(float[8], v));
+    if (n0 + c >= N) return;
+    if (a.split > 1) {
+      u32x4_t* o = reinterpret_cast<u32x4_t*>(sums + (size_t)r * N + c);
+      o[0] = u32x4_t{v[0], v[1], v[2], v[3]};
+      o[1] = u32x4_t{v[4], v[5], v[6], v[7]};
+      return;
+    }
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[j]);
+    store8(out + (size_t)r * N + c, f);
   });
 }
 
-// Launches on the most tiles that the groups can have
-#define LAUNCH(name, form, width)                                                                       \
-  template <typename S>                                                                                   \
-  void launch_##name(const FfnArgs& a, hipStream_t s) {                                                 \
-    using Tl = form<S>;                                                                              \
-    const int g = tile::grid_of(max_row_tiles(a.T, a.G, Tl::BM), width);                                \
-    ffn_##name##_kernel<Tl><<<g, Tl::THREADS, 0, s>>>(a);                                               \
-  }
-LAUNCH(up, XW, ceil_div(a.F, Tl::BN / 2))
-LAUNCH(down, XW, ceil_div(a.H, Tl::BN))
-LAUNCH(dh, XWT, ceil_div(a.F, Tl::BN))
-LAUNCH(dx, XWT, ceil_div(a.H, Tl::BN))
-#undef LAUNCH
+__global__ __launch_bounds__(256) void ffn_dw_sum_kernel(FfnArgs a) {
+  const size_t all = (size_t)a.G * a.H * a.F, i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8;
+  if (i >= 3 * all) return;
+  float f[8] = {};
+  for (int s = 0; s < a.split; ++s)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] += a.part[s * 3 * all + i + j];
+  store8((i < all ? a.dw1 : i < 2 * all ? a.dw3 : a.dw2) + i % all, f);
+}
+
+// ---- host ---------------------------------------------------------------------
+template <Op OP>
+tile::Plan plan(const FfnArgs& a) {
+  return tile::plan_of(a.T, a.G, cols_of<OP>(a), GATED<OP> ? 2 : 1, depth_of<OP>(a) / 64, OP == UP || OP == DOWN);
+}
 template <typename S>
-void launch_dw(const FfnArgs& a, hipStream_t s) {
-  using Tl = XTD<S>;
-  const int per = 2 * ceil_div(a.H, Tl::BM) * ceil_div(a.F, Tl::BN) + ceil_div(a.F, Tl::BM) * ceil_div(a.H, Tl::BN);
-  ffn_dw_kernel<Tl><<<tile::grid_of(a.G, per), Tl::THREADS, 0, s>>>(a);
+int dw_tiles(const FfnArgs& a) {  // of a group
+  return 2 * ceil_div(a.H, S::BM) * ceil_div(a.F, S::BN) + ceil_div(a.F, S::BM) * ceil_div(a.H, S::BN);
+}
+tile::Plan dw_plan(const FfnArgs& a) {
+  return tile::tile_plan((double)a.G * dw_tiles<tile::Wide>(a), (double)a.G * dw_tiles<tile::Small>(a),
+                         ceil_div(ceil_div(a.T, a.G), 64), 12.0 * a.G * a.H * a.F);
+}
+
+// Launches are for the most tiles that the groups can have.
+template <Op OP>
+void launch(FfnArgs a, hipStream_t s) {
+  const tile::Plan p = plan<OP>(a);
+  a.split = p.split;
+  const auto go = [&](auto kernel, int bm, int cols, int threads) {
+    kernel<<<tile::grid_of(max_row_tiles(a.T, a.G, bm), ceil_div(cols_of<OP>(a), cols) * a.split), threads, 0, s>>>(a);
+  };
+  constexpr int per = GATED<OP> ? 2 : 1;
+  if constexpr (OP == UP || OP == DOWN) {
+    if (p.kind == tile::Plan::FEW4) go(ffn_few_kernel<OP, 4>, FewOf<OP, 4>::BM, FewOf<OP, 4>::COLS, FewOf<OP, 4>::THREADS);
+    if (p.kind == tile::Plan::FEW8) go(ffn_few_kernel<OP, 8>, FewOf<OP, 8>::BM, FewOf<OP, 8>::COLS, FewOf<OP, 8>::THREADS);
+  }
+  using tile::Small, tile::Wide;
+  if (p.kind == tile::Plan::SMALL) go(ffn_kernel<OP, Small>, Small::BM, Small::BN / per, Small::THREADS);
+  if (p.kind == tile::Plan::WIDE) go(ffn_kernel<OP, Wide>, Wide::BM, Wide::BN / per, Wide::THREADS);
+  if (a.split > 1) ffn_sum_kernel<OP><<<(int)(((long long)a.T * cols_of<OP>(a) / 8 + 255) / 256), 256, 0, s>>>(a);
+}
+
+void launch_dw(FfnArgs a, hipStream_t s) {
+  const tile::Plan p = dw_plan(a);
+  a.split = p.split;
+  const auto go = [&](auto kernel, int tiles, int threads) {
+    kernel<<<a.G * ceil_div(tiles * a.split, NXCD) * NXCD, threads, 0, s>>>(a);
+  };
+  if (p.kind == tile::Plan::SMALL) go(ffn_dw_kernel<tile::Small>, dw_tiles<tile::Small>(a), tile::Small::THREADS);
+  else go(ffn_dw_kernel<tile::Wide>, dw_tiles<tile::Wide>(a), tile::Wide::THREADS);
+  if (a.split > 1) ffn_dw_sum_kernel<<<(int)((3LL * a.G * a.H * a.F / 8 + 255) / 256), 256, 0, s>>>(a);
 }
 
 moe_status check_cfg(const moe_ffn_config* c) {
@@ -201,9 +292,28 @@ moe_status check_cfg(const moe_ffn_config* c) {
   return MOE_OK;
 }
 
-// Workspace: bf16 [T][F] each of h (forward), or h, dgate and dup (backward).
+FfnArgs args_of(const moe_ffn_config* c, const int32_t* off) {
+  FfnArgs a{};
+  a.T = c->rows, a.H = c->hidden, a.F = c->ffn, a.G = c->n_groups, a.act = c->act;
+  a.off = off;
+  return a;
+}
+
+// Workspace: bf16 [T][F] each of h (forward), or h, dgate and dup (backward);
+// then the partial sums of the products that are split, one after the other.
 size_t plane(const moe_ffn_config* c) { return align_up(sizeof(uint16_t) * (size_t)c->rows * c->ffn, 256); }
-size_t ws_size(const moe_ffn_config* c, bool backward) { return 256 + plane(c) * (backward ? 3 : 1); }
+template <Op OP>
+size_t part_bytes(const FfnArgs& a) {
+  const int s = plan<OP>(a).split;
+  return s > 1 ? sizeof(float) * (size_t)s * a.T * sums_of<OP>(a) : 0;
+}
+size_t ws_size(const moe_ffn_config* c, bool backward) {
+  const FfnArgs a = args_of(c, nullptr);
+  if (!backward) return 256 + plane(c) + std::max(part_bytes<UP>(a), part_bytes<DOWN>(a));
+  const int s = dw_plan(a).split;
+  const size_t dw = s > 1 ? 3 * sizeof(float) * (size_t)s * a.G * a.H * a.F : 0;
+  return 256 + 3 * plane(c) + std::max(dw, std::max(part_bytes<DH>(a), part_bytes<DX>(a)));
+}
 
 moe_status check_ws(const moe_ffn_config* c, bool backward, const void* ws, size_t bytes) {
   const size_t need = ws_size(c, backward);
@@ -238,13 +348,12 @@ moe_status moe_ffn_forward(const moe_ffn_config* cfg, const uint16_t* x, const i
     if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
   if ((st = check_ws(cfg, false, ws, ws_bytes)) != MOE_OK) return st;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  FfnArgs a{};
-  a.T = cfg->rows, a.H = cfg->hidden, a.F = cfg->ffn, a.G = cfg->n_groups, a.act = cfg->act;
-  a.off = group_off;
+  FfnArgs a = args_of(cfg, group_off);
   a.x = x, a.w1 = w1, a.w3 = w3, a.w2 = w2;
   a.h = static_cast<uint16_t*>(ws), a.kgate = gate, a.kup = up, a.y = y;
-  launch_up<tile::Wide>(a, s);
-  launch_down<tile::Wide>(a, s);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + plane(cfg));
+  launch<UP>(a, s);
+  launch<DOWN>(a, s);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }
@@ -265,20 +374,19 @@ moe_status moe_ffn_backward(const moe_ffn_config* cfg, const uint16_t* dy, const
     if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
   if ((st = check_ws(cfg, true, ws, ws_bytes)) != MOE_OK) return st;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  FfnArgs a{};
-  a.T = cfg->rows, a.H = cfg->hidden, a.F = cfg->ffn, a.G = cfg->n_groups, a.act = cfg->act;
-  a.off = group_off;
+  FfnArgs a = args_of(cfg, group_off);
   a.x = x, a.w1 = w1, a.w3 = w3, a.w2 = w2, a.gate = gate, a.up = up, a.dy = dy;
   char* at = static_cast<char*>(ws);
   a.h = reinterpret_cast<uint16_t*>(at);
   a.dgate = reinterpret_cast<uint16_t*>(at + plane(cfg));
   a.dup = reinterpret_cast<uint16_t*>(at + 2 * plane(cfg));
+  a.part = reinterpret_cast<float*>(at + 3 * plane(cfg));
   a.dx = dx, a.dw1 = dw1, a.dw3 = dw3, a.dw2 = dw2;
   if (a.T > 0 && (dx || dw1)) {
-    launch_dh<tile::Wide>(a, s);
-    if (dx) launch_dx<tile::Wide>(a, s);
+    launch<DH>(a, s);
+    if (dx) launch<DX>(a, s);
   }
-  if (dw1) launch_dw<tile::Wide>(a, s);
+  if (dw1) launch_dw(a, s);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }

@@ -25,18 +25,67 @@ __device__ __forceinline__ int quantize(uint16_t v, float scale) {
   return (int)fminf(fmaxf(rintf(bf16_to_f32(v) / scale), -127.0f), 127.0f);
 }
 
-__global__ __launch_bounds__(256) void quantize_rows_kernel(int cols, const uint16_t* x, int8_t* q, float* scale) {
+// The quotient of a value by its row's scale, rounded to a whole number as the
+// IEEE quotient would be.  The value times the hardware reciprocal is within
+// 127 * 3 * 2^-24 < 3e-5 of it, so only where that lies within 1e-4 of a half
+// does the division itself decide (about 1 value in 5000).
+struct Quantizer {
+  float scale, inv;
+  bool slow;
+  __device__ __forceinline__ explicit Quantizer(float s) : scale(s), inv(__builtin_amdgcn_rcpf(s)), slow(s < 0x1p-100f) {}
+  __device__ __forceinline__ int operator()(float v) const {
+    float q = v * inv, r = rintf(q);
+    if (slow || fabsf(q - r) > 0.4999f) r = rintf(v / scale);
+    return (int)fminf(fmaxf(r, -127.0f), 127.0f);
+  }
+};
+
+// One row a workgroup of WAVES waves, held in registers: each thread takes LOADS pieces of
+// 8 values.  Reads 2 and writes 1 byte a value once.
+template <int THREADS, int LOADS>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(int rows, int cols, const uint16_t* x, int8_t* q, float* scale) {
+  constexpr int PER = 256 / THREADS;  // rows of a workgroup
   __shared__ uint32_t red[4];
-  const size_t row = blockIdx.x;
+  const int t = threadIdx.x % THREADS, row = blockIdx.x * PER + threadIdx.x / THREADS;
+  const bool some = row < rows;
+  const uint16_t* xr = x + (size_t)row * cols;
+  u32x4_t v[LOADS];
   uint32_t m = 0;
-  for (int c = threadIdx.x; c < cols; c += 256) m = max(m, x[row * cols + c] & 0x7fffu);
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int c = (t + i * THREADS) * 8;
+    v[i] = some && c < cols ? *reinterpret_cast<const u32x4_t*>(xr + c) : u32x4_t{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) m = max(m, max(v[i][j] & 0x7fffu, (v[i][j] >> 16) & 0x7fffu));
+#pragma unroll
   for (int d = 32; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = m;
-  __syncthreads();
-  m = max(max(red[0], red[1]), max(red[2], red[3]));
+  if constexpr (THREADS > 64) {
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = m;
+    __syncthreads();
+    m = max(max(red[0], red[1]), max(red[2], red[3]));
+  }
+  if (!some) return;
   const float s = scale_of(m);
-  if (threadIdx.x == 0) scale[row] = s;
-  for (int c = threadIdx.x; c < cols; c += 256) q[row * cols + c] = (int8_t)quantize(x[row * cols + c], s);
+  if (t == 0) scale[row] = s;
+  const bool zero = !(s > 0.0f);
+  const Quantizer quant(s);
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int c = (t + i * THREADS) * 8;
+    if (c >= cols) break;
+    uint32_t w[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t lo = v[i][2 * j], hi = v[i][2 * j + 1];
+      w[j] = zero ? 0u
+                  : (uint32_t)(quant(bf16_lo(lo)) & 255) | (uint32_t)(quant(bf16_hi(lo)) & 255) << 8 |
+                        (uint32_t)(quant(bf16_lo(hi)) & 255) << 16 | (uint32_t)quant(bf16_hi(hi)) << 24;
+    }
+    *reinterpret_cast<uint2*>(q + (size_t)row * cols + c) = uint2{w[0], w[1]};
+  }
 }
 
 // a workgroup takes 64 channels of a group: the largest magnitudes, then the
@@ -69,48 +118,130 @@ struct I8Args {
   const int8_t *x, *w;
   const float *sx, *sw;
   uint16_t* y;
+  int32_t* part;  // few rows: partial sums [split][T][N] of a split product
+  int split;
 };
 
-template <typename S>
-using I8 = tile::Tile<S, true, false, false>;
+// 8 columns of y from their sums (gated: v[8..15] the ups'): n the column of y
+template <bool GATED>
+__device__ __forceinline__ void finish(const I8Args& a, size_t row, int group, int n, const uint32_t* v) {
+  const int out = GATED ? a.N / 2 : a.N;
+  const float sx = a.sx[row];
+  const float* sw = a.sw + (size_t)group * a.N + n;
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    y[i] = (float)(int)v[i] * (sx * sw[i]);
+    if constexpr (GATED) y[i] = act_of(y[i], a.act) * ((float)(int)v[8 + i] * (sx * sw[out + i]));
+  }
+  *reinterpret_cast<u32x4_t*>(a.y + row * out + n) = tile::pack8(y);
+}
 
-template <typename Tl, bool GATED>
-__global__ __launch_bounds__(Tl::THREADS) void gemm_i8_kernel(I8Args a) {
+// The same, or the partial sums where the product is split.
+template <bool GATED>
+__device__ __forceinline__ void put(const I8Args& a, int part, size_t row, int group, int n, const uint32_t* v) {
+  if (a.split == 1) {
+    finish<GATED>(a, row, group, n, v);
+    return;
+  }
+  int32_t* p = a.part + ((size_t)part * a.T + row) * a.N + n;
+#pragma unroll
+  for (int i = 0; i < (GATED ? 4 : 2); ++i)
+    *reinterpret_cast<u32x4_t*>(p + i / 2 * (a.N / 2) + i % 2 * 4) = u32x4_t{v[i * 4], v[i * 4 + 1], v[i * 4 + 2], v[i * 4 + 3]};
+}
+
+// Operands of a tile from depth k and column n0 on
+template <bool GATED>
+__device__ __forceinline__ tile::Operand rows_op(const I8Args& a, const RowTile& rt, int k) {
+  return {reinterpret_cast<const char*>(a.x) + (size_t)rt.begin * a.K + k, nullptr, (uint32_t)a.K, rt.end - rt.begin, 0, 0};
+}
+template <bool GATED>
+__device__ __forceinline__ tile::Operand weights_op(const I8Args& a, const RowTile& rt, int k, int n0) {
+  const int out = GATED ? a.N / 2 : a.N;
+  const char* w = reinterpret_cast<const char*>(a.w) + ((size_t)rt.group * a.N + n0) * a.K + k;
+  return {w, GATED ? w + (size_t)out * a.K : nullptr, (uint32_t)a.K, out - n0, 0, 0};
+}
+
+template <typename S, bool GATED>
+__global__ __launch_bounds__(S::THREADS) void gemm_i8_kernel(I8Args a) {
+  using Tl = tile::Tile<S, true, false, false>;
   __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
   const RowTiles list(a.off, a.G, a.T, Tl::BM);
   constexpr int COLS = GATED ? Tl::BN / 2 : Tl::BN;
-  const int out = GATED ? a.N / 2 : a.N;
+  const int out = GATED ? a.N / 2 : a.N, nt = ceil_div(out, COLS), stages = ceil_div(a.K, 128);
   int m, n;
-  if (!tile::pick(list.total, ceil_div(out, COLS), &m, &n)) return;
+  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
   const RowTile rt = list.at(m);
-  const int n0 = n * COLS, rows = rt.end - rt.begin;
-  const char* w = reinterpret_cast<const char*>(a.w) + ((size_t)rt.group * a.N + n0) * a.K;
-  const tile::Operand A{reinterpret_cast<const char*>(a.x) + (size_t)rt.begin * a.K, nullptr, (uint32_t)a.K, rows, 0, 0};
-  const tile::Operand B{w, GATED ? w + (size_t)out * a.K : nullptr, (uint32_t)a.K, out - n0, 0, 0};
-  const float* sw = a.sw + (size_t)rt.group * a.N + n0;
+  const int part = n / nt, n0 = n % nt * COLS, rows = rt.end - rt.begin;
+  const int k0 = stages * part / a.split * 128, k1 = min(stages * (part + 1) / a.split * 128, a.K);
+  const tile::Operand A = rows_op<GATED>(a, rt, k0), B = weights_op<GATED>(a, rt, k0, n0);
   typename Tl::Acc acc;
   Tl::zero(acc);
-  Tl::run(acc, lds, A, B, a.K, A, B, 0);
+  Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
   Tl::template epilogue<GATED>(acc, lds, rows, [&](int r, int c, const auto& v) {
-    if (n0 + c >= out) return;
-    const float sx = a.sx[rt.begin + r];
-    float y[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      y[i] = (float)(int)v[i] * (sx * sw[c + i]);
-      if constexpr (GATED) y[i] = act_of(y[i], a.act) * ((float)(int)v[8 + i] * (sx * sw[out + c + i]));
-    }
-    *reinterpret_cast<u32x4_t*>(a.y + (size_t)(rt.begin + r) * out + n0 + c) = tile::pack8(y);
+    if (n0 + c < out) put<GATED>(a, part, rt.begin + r, rt.group, n0 + c, v);
   });
 }
 
-template <typename S>
-void launch_gemm(const I8Args& a, hipStream_t s) {
-  using Tl = I8<S>;
+template <int NW, bool GATED>
+__global__ __launch_bounds__(NW * 64) void gemm_i8_few_kernel(I8Args a) {
+  using Fw = tile::Few<NW, true, false, GATED>;
+  __shared__ __attribute__((aligned(1024))) char lds[Fw::LDS];
+  const RowTiles list(a.off, a.G, a.T, Fw::BM);
+  const int out = GATED ? a.N / 2 : a.N, nt = ceil_div(out, Fw::COLS), steps = a.K / Fw::KE;
+  int m, n;
+  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
+  const RowTile rt = list.at(m);
+  const int part = n / nt, n0 = n % nt * Fw::COLS;
+  Fw::run(lds, rows_op<GATED>(a, rt, 0), weights_op<GATED>(a, rt, 0, n0), steps * part / a.split,
+          steps * (part + 1) / a.split, [&](int r, int c, const auto& v) {
+            if (n0 + c < out) put<GATED>(a, part, rt.begin + r, rt.group, n0 + c, v);
+          });
+}
+
+// y from the partial sums of a split product
+template <bool GATED>
+__global__ __launch_bounds__(256) void gemm_i8_sum_kernel(I8Args a) {
+  const int out = GATED ? a.N / 2 : a.N;
+  const RowTiles list(a.off, a.G, a.T, 1);
+  if ((int)blockIdx.x >= list.total) return;
+  const RowTile rt = list.at(blockIdx.x);
+  if (const int c = (blockIdx.y * 256 + threadIdx.x) * 8; c < out) {
+    uint32_t v[GATED ? 16 : 8] = {};
+    for (int s = 0; s < a.split; ++s) {
+      const int32_t* p = a.part + ((size_t)s * a.T + rt.begin) * a.N + c;
+#pragma unroll
+      for (int j = 0; j < (GATED ? 16 : 8); ++j) v[j] += (uint32_t)p[j / 8 * out + j % 8];
+    }
+    finish<GATED>(a, rt.begin, rt.group, c, v);
+  }
+}
+
+tile::Plan plan(const I8Args& a) {
   const bool gated = a.act != MOE_ACT_NONE;
-  const int nt = gated ? ceil_div(a.N / 2, Tl::BN / 2) : ceil_div(a.N, Tl::BN);
-  const int g = tile::grid_of(max_row_tiles(a.T, a.G, Tl::BM), nt);
-  (gated ? gemm_i8_kernel<Tl, true> : gemm_i8_kernel<Tl, false>)<<<g, Tl::THREADS, 0, s>>>(a);
+  return tile::plan_of(a.T, a.G, gated ? a.N / 2 : a.N, gated ? 2 : 1, ceil_div(a.K, 128), true);
+}
+
+// Launches are for the most tiles that the groups can have.
+template <bool GATED>
+void launch(I8Args a, hipStream_t s) {
+  const tile::Plan p = plan(a);
+  a.split = p.split;
+  const int out = GATED ? a.N / 2 : a.N;
+  constexpr int per = GATED ? 2 : 1;
+  const auto go = [&](auto kernel, int bm, int cols, int threads) {
+    kernel<<<tile::grid_of(max_row_tiles(a.T, a.G, bm), ceil_div(out, cols) * a.split), threads, 0, s>>>(a);
+  };
+  using tile::Small, tile::Wide;
+  using F4 = tile::Few<4, true, false, GATED>;
+  using F8 = tile::Few<8, true, false, GATED>;
+  switch (p.kind) {
+    case tile::Plan::FEW4: go(gemm_i8_few_kernel<4, GATED>, F4::BM, F4::COLS, F4::THREADS); break;
+    case tile::Plan::FEW8: go(gemm_i8_few_kernel<8, GATED>, F8::BM, F8::COLS, F8::THREADS); break;
+    case tile::Plan::SMALL: go(gemm_i8_kernel<Small, GATED>, Small::BM, Small::BN / per, Small::THREADS); break;
+    case tile::Plan::WIDE: go(gemm_i8_kernel<Wide, GATED>, Wide::BM, Wide::BN / per, Wide::THREADS); break;
+  }
+  if (a.split > 1) gemm_i8_sum_kernel<GATED><<<dim3(a.T, ceil_div(out, 2048)), 256, 0, s>>>(a);
 }
 
 moe_status check_cfg(const moe_gemm_i8_config* c) {
@@ -128,7 +259,17 @@ moe_status check_cfg(const moe_gemm_i8_config* c) {
   return MOE_OK;
 }
 
-size_t ws_size(const moe_gemm_i8_config*) { return 256; }
+I8Args args_of(const moe_gemm_i8_config* c) {
+  I8Args a{};
+  a.T = c->rows, a.K = c->depth, a.N = c->channels, a.G = c->n_groups, a.act = c->act;
+  return a;
+}
+
+// Workspace: the partial sums of a split product, int32 [split][T][N].
+size_t ws_size(const moe_gemm_i8_config* c) {
+  const int s = plan(args_of(c)).split;
+  return 256 + (s > 1 ? sizeof(int32_t) * (size_t)s * c->rows * c->channels : 0);
+}
 
 }  // namespace
 
@@ -142,7 +283,16 @@ moe_status moe_quantize_rows_i8(int32_t rows, int32_t cols, const uint16_t* x, i
   if (!x || !q || !scale) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
   if (!aligned16(x) || !aligned16(q) || !aligned16(scale))
     return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
-  quantize_rows_kernel<<<rows, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(cols, x, q, scale);
+  // rows of up to 1024 values are a wavefront's each, four to a workgroup
+  const auto kernel = cols <= 512     ? quantize_rows_kernel<64, 1>
+                      : cols <= 1024  ? quantize_rows_kernel<64, 2>
+                      : cols <= 2048  ? quantize_rows_kernel<256, 1>
+                      : cols <= 4096  ? quantize_rows_kernel<256, 2>
+                      : cols <= 8192  ? quantize_rows_kernel<256, 4>
+                      : cols <= 16384 ? quantize_rows_kernel<256, 8>
+                                      : quantize_rows_kernel<256, 16>;
+  const int per = cols <= 1024 ? 4 : 1;
+  kernel<<<ceil_div(rows, per), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(rows, cols, x, q, scale);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }
@@ -185,8 +335,12 @@ moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const fl
   if (!ws || ws_bytes < ws_size(cfg))
     return fail(MOE_ERR_INVALID_ARG, "the workspace holds %zu of %zu bytes", ws ? ws_bytes : 0, ws_size(cfg));
   if (reinterpret_cast<uintptr_t>(ws) % 256) return fail(MOE_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
-  I8Args a{cfg->rows, cfg->depth, cfg->channels, cfg->n_groups, cfg->act, group_off, xq, wq, x_scale, w_scale, y};
-  launch_gemm<tile::Wide>(a, reinterpret_cast<hipStream_t>(stream));
+  I8Args a = args_of(cfg);
+  a.off = group_off;
+  a.x = xq, a.w = wq, a.sx = x_scale, a.sw = w_scale, a.y = y;
+  a.part = static_cast<int32_t*>(ws);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  a.act == MOE_ACT_NONE ? launch<false>(a, s) : launch<true>(a, s);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }

@@ -29,6 +29,10 @@
 // 32) + r % 4 of row l % 32 in register r.
 #pragma once
 
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
 #include "common.h"
 #include "gemm.h"
 
@@ -64,6 +68,7 @@ struct Operand {
 template <int WM_, int WN_, int MB_, int NB_>
 struct Shape {
   static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_;
+  static constexpr int BM = WM * MB * 32, BN = WN * NB * 32, THREADS = WM * WN * 64;
 };
 using Wide = Shape<2, 4, 4, 2>;   // 256 x 256
 using Small = Shape<2, 2, 2, 2>;  // 128 x 128
@@ -169,26 +174,40 @@ struct Tile {
   // byte distance of column block nb from a wave's first (k-contiguous B)
   static constexpr int nb_bytes(int nb) { return (nb / (NB / 2) * (BN / 2) + nb % (NB / 2) * 32) * DEPTH; }
 
-  static __device__ __forceinline__ void load_frags(const char* st, int kk, const FragOffs& f, Frag (&a)[MB], Frag (&b)[NB]) {
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      if constexpr (BT) b[nb] = read_tr<BN / 2>(st, f.b[nb], kk);
-      else b[nb] = *reinterpret_cast<const Frag*>(st + f.b[kk] + nb_bytes(nb));
-    }
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
+  // fragment u of slice kk: B's blocks, then A's
+  static constexpr int FRAGS = NB + MB;
+  static __device__ __forceinline__ void load_frag(int u, const char* st, int kk, const FragOffs& f, Frag (&a)[MB], Frag (&b)[NB]) {
+    if (u < NB) {
+      if constexpr (BT) b[u] = read_tr<BN / 2>(st, f.b[u], kk);
+      else b[u] = *reinterpret_cast<const Frag*>(st + f.b[kk] + nb_bytes(u));
+    } else {
+      const int mb = u - NB;
       if constexpr (AT) a[mb] = read_tr<BM / 2>(st, f.a[mb], kk);
       else a[mb] = *reinterpret_cast<const Frag*>(st + f.a[kk] + mb * WM * 32 * DEPTH);
     }
   }
-  static __device__ __forceinline__ void multiply(Acc& acc, const Frag (&a)[MB], const Frag (&b)[NB]) {
+  static __device__ __forceinline__ void load_frags(const char* st, int kk, const FragOffs& f, Frag (&a)[MB], Frag (&b)[NB]) {
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
+    for (int u = 0; u < FRAGS; ++u) load_frag(u, st, kk, f, a, b);
+  }
+  // The products of one slice, with next(u) for u in [0, FRAGS), the loads of
+  // the next slice's fragments, and dma(i) for i in [0, INSTR) between them,
+  // in this order: left to itself the compiler loads each fragment right
+  // before the product that takes it, and every product waits for LDS.
+  template <typename Next, typename Dma>
+  static __device__ __forceinline__ void multiply(Acc& acc, const Frag (&a)[MB], const Frag (&b)[NB], Next&& next, Dma&& dma) {
+    constexpr int P = MB * NB;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        if constexpr (I8) acc[mb][nb] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[nb], a[mb], acc[mb][nb], 0, 0, 0);
-        else acc[mb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[nb], a[mb], acc[mb][nb], 0, 0, 0);
-      }
+    for (int i = 0; i < P; ++i) {
+      const int mb = i / NB, nb = i % NB;
+      if constexpr (I8) acc[mb][nb] = __builtin_amdgcn_mfma_i32_32x32x32_i8(b[nb], a[mb], acc[mb][nb], 0, 0, 0);
+      else acc[mb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b[nb], a[mb], acc[mb][nb], 0, 0, 0);
+#pragma unroll
+      for (int u = i * FRAGS / P; u < (i + 1) * FRAGS / P; ++u) next(u);
+#pragma unroll
+      for (int j = i * INSTR / P; j < (i + 1) * INSTR / P; ++j) dma(j);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 
   // acc += A B over the depth in [0, n1), and of a second pair of operands
@@ -211,10 +230,20 @@ struct Tile {
     const size_t sa = AT ? (size_t)A.ld * 64 : DEPTH, sb = BT ? (size_t)B.ld * 64 : DEPTH;
     const uint32_t la = lds_u32(lds) + wave * AI * 1024, lb = lds_u32(lds) + A_BYTES + wave * BI * 1024;
     const int rest = n1 % KE;  // depth of the last stage, 0: whole (only without a second pair)
+    // instruction i of stage s (its operands' addresses at, its offsets and LDS)
+    auto issue_one = [&](int i, const char* a, const char* b, uint32_t so, uint32_t back) {
+      if (i < AI) dma16(a, oa[i < AI ? i : 0] - back, la + so + i * 1024);
+      else dma16(b, ob[i < AI ? 0 : i - AI] - back, lb + so + (i - AI) * 1024);
+    };
+    const auto base_a = [&](int s) { return s < half ? pa + s * sa : pa2 + (s - half) * sa; };
+    const auto base_b = [&](int s) { return s < half ? pb + s * sb : pb2 + (s - half) * sb; };
+    // (int8: a last stage of 64 has no granules 4..7; they are read as 0..3)
+    const auto back_of = [&](int s) -> uint32_t {
+      return I8 && rest && s == ns - 1 && (((lane & 7) ^ (lane >> 3)) & 4) ? 64 : 0;
+    };
     auto issue = [&](int s) {
-      const uint32_t so = (s & 1) * STAGE;
-      const char* a = s < half ? pa + s * sa : pa2 + (s - half) * sa;
-      const char* b = s < half ? pb + s * sb : pb2 + (s - half) * sb;
+      const uint32_t so = (s & 1) * STAGE, back = back_of(s);
+      const char *a = base_a(s), *b = base_b(s);
       if ((AT && BT) && rest && s == ns - 1) {
         uint32_t ta[AI], tb[BI];
         offsets<AT, BM, AI>(ta, A, wave, lane, rest);
@@ -225,12 +254,8 @@ struct Tile {
         for (int i = 0; i < BI; ++i) dma16(b, tb[i], lb + so + i * 1024);
         return;
       }
-      // (int8: a last stage of 64 has no granules 4..7; they are read as 0..3)
-      const uint32_t back = I8 && rest && s == ns - 1 && (((lane & 7) ^ (lane >> 3)) & 4) ? 64 : 0;
 #pragma unroll
-      for (int i = 0; i < AI; ++i) dma16(a, oa[i] - back, la + so + i * 1024);
-#pragma unroll
-      for (int i = 0; i < BI; ++i) dma16(b, ob[i] - back, lb + so + i * 1024);
+      for (int i = 0; i < INSTR; ++i) issue_one(i, a, b, so, back);
     };
     // clears the depth rows from `rest` on of a stage of transposed operands
     auto clear = [&](char* st) {
@@ -256,34 +281,50 @@ struct Tile {
     compiler_fence();
     if ((AT && BT) && rest && ns == 1) clear(lds);
     load_frags(lds, 0, f, a0, b0);
-    const int whole = I8 && rest ? ns - 1 : ns;
-    for (int s = 0; s < whole; ++s) {
-      const char* st = lds + (s & 1) * STAGE;
-      char* nx = lds + (~s & 1) * STAGE;
-      load_frags(st, 1, f, a1, b1);
-      multiply(acc, a0, b0);
-      load_frags(st, 2, f, a0, b0);
-      multiply(acc, a1, b1);
-      load_frags(st, 3, f, a1, b1);
-      multiply(acc, a0, b0);
-      // this wave's reads of the stage have arrived and so has its part of the
-      // next one: after the barrier everyone's have, and the stage is free
+    const auto none = [](int) {};
+    const auto from = [&](const char* st, int kk, Frag (&a)[MB], Frag (&b)[NB]) {
+      return [&, st, kk](int u) { load_frag(u, st, kk, f, a, b); };
+    };
+    // this wave's reads of a stage have arrived and so has its part of the
+    // next one: after the barrier everyone's have, and the stage is free
+    const auto meet = [] {
       compiler_fence();
       __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0) lgkmcnt(0)
       __builtin_amdgcn_s_barrier();
       compiler_fence();
+    };
+    // steady state: the stage after the next one is whole and loaded
+    const int steady = rest ? ns - 3 : ns - 2;
+    int s = 0;
+    for (; s < steady; ++s) {
+      const char* st = lds + (s & 1) * STAGE;
+      const char* nx = lds + (~s & 1) * STAGE;
+      multiply(acc, a0, b0, from(st, 1, a1, b1), none);
+      multiply(acc, a1, b1, from(st, 2, a0, b0), none);
+      multiply(acc, a0, b0, from(st, 3, a1, b1), none);
+      meet();
+      const char *pan = base_a(s + 2), *pbn = base_b(s + 2);
+      const uint32_t so = (s & 1) * STAGE;
+      multiply(acc, a1, b1, from(nx, 0, a0, b0), [&](int i) { issue_one(i, pan, pbn, so, 0); });
+    }
+    const int whole = I8 && rest ? ns - 1 : ns;
+    for (; s < whole; ++s) {
+      const char* st = lds + (s & 1) * STAGE;
+      char* nx = lds + (~s & 1) * STAGE;
+      multiply(acc, a0, b0, from(st, 1, a1, b1), none);
+      multiply(acc, a1, b1, from(st, 2, a0, b0), none);
+      multiply(acc, a0, b0, from(st, 3, a1, b1), none);
+      meet();
       if (s + 2 < ns) issue(s + 2);
       if (s + 1 < ns) {
         if ((AT && BT) && rest && s + 2 == ns) clear(nx);
         load_frags(nx, 0, f, a0, b0);
       }
-      multiply(acc, a1, b1);
+      multiply(acc, a1, b1, none, none);
     }
-    if (whole < ns) {
-      const char* st = lds + (whole & 1) * STAGE;
-      load_frags(st, 1, f, a1, b1);
-      multiply(acc, a0, b0);
-      multiply(acc, a1, b1);
+    if (I8 && whole < ns) {  // half a stage
+      multiply(acc, a0, b0, from(lds + (whole & 1) * STAGE, 1, a1, b1), none);
+      multiply(acc, a1, b1, none, none);
     }
     lds_barrier();
   }
@@ -343,6 +384,209 @@ struct Tile {
     }
   }
 };
+
+// ---------------------------------------------------------------------------
+// Few rows: up to 32 rows x 64 columns (gated: 64 of each matrix), whose time
+// is that of streaming the weights.  The four or
+// eight waves share the columns and take
+// the steps of the depth (64 bytes: 32 bf16 or 64 int8 values) in turn, each
+// with slots of LDS of its own, so the loop has no barrier: a wave waits for
+// its oldest slot, multiplies it and loads a later step into it.  The waves'
+// sums are added in a fixed order at the end.
+// LDS images of a slot: weights, k-contiguous as rows of 64 bytes, granule c
+// at c ^ (r / 2) % 4, or transposed as 32 depth rows of 64 columns per matrix
+// (a panel of PW = 64, as above); then the 32 rows of A, k-contiguous.
+// ---------------------------------------------------------------------------
+template <int NW_, bool I8_, bool BT_, bool GATED_>
+struct Few {
+  static constexpr bool I8 = I8_, BT = BT_, GATED = GATED_;
+  static constexpr int NW = NW_, THREADS = NW * 64, BM = 32, COLS = 64, STEP = 64, KE = I8 ? 64 : 32;
+  static constexpr int NB = GATED ? 4 : 2, W_BYTES = NB * 2048, SLOT = W_BYTES + 2048, SLOTS = GATED ? 2 : 3;
+  static constexpr int WI = W_BYTES / 1024, INSTR = SLOT / 1024, SUMS = 32 * NB * 32 * 4;  // bytes of a wave's sums
+  static constexpr int LDS = NW * SLOTS * SLOT;
+  static_assert(NW * SUMS <= LDS, "the sums fit");
+  static_assert(!I8 || !BT, "int8 operands are k-contiguous");
+  using Acc1 = std::conditional_t<I8, i32x16_t, f32x16_t>;
+  using Frag = std::conditional_t<I8, i32x4_t, bf16x8_t>;
+  using Big = Tile<Small, I8, false, BT>;  // the transposed reads, which are the same
+
+  // fn(row, col, v) for every 8 consecutive columns of each row, v[8..15] the
+  // second matrix's where gated: the sums over steps [s0, s1) of the depth.
+  // Rows of A past A.valid are read as the last and not handed out.
+  template <typename Fn>
+  static __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int s0, int s1, Fn&& fn) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    uint32_t ow[WI], ox[2];
+#pragma unroll
+    for (int i = 0; i < WI; ++i) {
+      if constexpr (BT) {
+        const int k = i % 4 * 8 + (lane >> 3), c = (lane & 7) ^ Big::template swz<64>(k);
+        ow[i] = (uint32_t)k * B.ld + (uint32_t)min(B.col + c * 8, B.cols - 8) * 2u;
+      } else {
+        const int r = i % 4 * 16 + (lane >> 2);
+        ow[i] = (uint32_t)min(r, B.valid - 1) * B.ld + (uint32_t)(((lane & 3) ^ ((r >> 1) & 3)) * 16);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = i * 16 + (lane >> 2);
+      ox[i] = (uint32_t)min(r, A.valid - 1) * A.ld + (uint32_t)(((lane & 3) ^ ((r >> 1) & 3)) * 16);
+    }
+    const char *pa = uniform_ptr(A.p), *pb = uniform_ptr(B.p), *pb2 = GATED ? uniform_ptr(B.p2) : nullptr;
+    const size_t sb = BT ? (size_t)B.ld * 32 : STEP;
+    char* mine = lds + wave * SLOTS * SLOT;
+    const uint32_t l0 = lds_u32(mine);
+    const int n = (s1 - s0 - wave + NW - 1) / NW;  // this wave's steps
+    auto issue = [&](int j) {
+      const size_t s = s0 + wave + j * NW;
+      const uint32_t l = l0 + j % SLOTS * SLOT;
+#pragma unroll
+      for (int i = 0; i < WI; ++i) dma16((GATED && i >= 4 ? pb2 : pb) + s * sb, ow[i], l + i * 1024);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) dma16(pa + s * STEP, ox[i], l + W_BYTES + i * 1024);
+    };
+    uint32_t fw[2], fx[2];  // fragment offsets (k-contiguous: of slice 0 and 1; transposed: of column block 0 and 1)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = lane & 31;
+      fx[i] = (uint32_t)(r * STEP + ((i * 2 + (lane >> 5)) ^ ((r >> 1) & 3)) * 16);
+      fw[i] = BT ? Big::template tr_offset<64>(0, i * 32, lane) : fx[i];
+    }
+    Acc1 acc[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[nb][r] = 0;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j)
+      if (j < n) issue(j);
+    for (int j = 0; j < n; ++j) {
+      if (j + SLOTS <= n) wait_vm<(SLOTS - 1) * INSTR>();
+      else if (SLOTS > 2 && j + 2 == n) wait_vm<INSTR>();
+      else wait_vm<0>();
+      compiler_fence();
+      const char* st = mine + j % SLOTS * SLOT;
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) {
+        const Frag x = *reinterpret_cast<const Frag*>(st + W_BYTES + fx[kk]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          Frag w;
+          if constexpr (BT) w = Big::template read_tr<64>(st + nb / 2 * 4096, fw[nb % 2], kk);
+          else w = *reinterpret_cast<const Frag*>(st + nb * 2048 + fw[kk]);
+          if constexpr (I8) acc[nb] = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x, acc[nb], 0, 0, 0);
+          else acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, x, acc[nb], 0, 0, 0);
+        }
+      }
+      // the slot's reads are done before it is loaded again
+      compiler_fence();
+      __builtin_amdgcn_s_waitcnt((3 << 14) | (7 << 4) | 15);  // lgkmcnt(0)
+      if (j + SLOTS < n) issue(j + SLOTS);
+    }
+    lds_barrier();
+    // [wave][row][column], granules of 4 columns at position c ^ (row & 15)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int row = lane & 31, g = nb * 8 + q * 2 + (lane >> 5);
+        u32x4_t v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (I8) v[r] = (uint32_t)acc[nb][q * 4 + r];
+          else v[r] = __float_as_uint(acc[nb][q * 4 + r]);
+        }
+        *reinterpret_cast<u32x4_t*>(lds + wave * SUMS + row * (NB * 128) + (g ^ (row & 15)) * 16) = v;
+      }
+    lds_barrier();
+    if (threadIdx.x >= 256) return;
+    const int row = threadIdx.x >> 3, c = (threadIdx.x & 7) * 8;
+    if (row >= A.valid) return;
+    uint32_t v[NB * 4];
+#pragma unroll
+    for (int p = 0; p < NB; ++p) {
+      const int g = (c + p / 2 * 64) / 4 + p % 2;
+      const char* at = lds + row * (NB * 128) + (g ^ (row & 15)) * 16;
+      u32x4_t t = *reinterpret_cast<const u32x4_t*>(at);
+#pragma unroll
+      for (int w = 1; w < NW; ++w) {
+        const u32x4_t o = *reinterpret_cast<const u32x4_t*>(at + w * SUMS);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (I8) t[r] += o[r];
+          else t[r] = __float_as_uint(__uint_as_float(t[r]) + __uint_as_float(o[r]));
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[p * 4 + r] = t[r];
+    }
+    fn(row, c, v);
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Which tiles a product is computed by, and in how many parts its depth is
+// split (a kernel behind it adds the parts' sums, in order).
+// ---------------------------------------------------------------------------
+struct Plan {
+  enum Kind { FEW4, FEW8, SMALL, WIDE } kind;
+  int split;
+};
+constexpr int MAX_SPLIT = 16;
+
+// Small or Wide tiles, from how many there are of each: rounds of workgroups
+// (one Wide or two Small per CU) times the time of one.  Measured, us per
+// stage: Wide 1.9 to 2.2; Small 0.85 with one workgroup per CU and 1.4 with
+// two.  So Wide tiles take 1.4 times less where they fill the chip, and Small
+// ones win where Wide ones leave CUs idle: dh of 2000 rows, H = F = 4096, 128
+// Wide tiles 123, 512 Small 89; of 4000 rows 147 : 179.  A split costs a
+// launch (6 with its gap) and the sums' way out and back, `sum_bytes` per part
+// (6 TB/s): dx of 333 rows in 4 groups, H = 1024, F = 2816 (40 Small tiles, 88
+// stages), 80 : 52 : 33 : 25 in 1, 2, 4 and 8 parts; dh of 2000 rows above, 89
+// against 83 + 27 in two.
+inline Plan tile_plan(double wide, double small, int stages, double sum_bytes) {
+  Plan best{Plan::WIDE, 1};
+  double least = std::ceil(wide / 256) * (stages * 2.0 + 6);
+  for (int s = 1; s <= MAX_SPLIT && s <= std::max(stages, 1); s *= 2) {
+    const double w = small * s;
+    const double t = std::ceil(w / 512) * (ceil_div(stages, s) * (w <= 256 ? 0.85 : 1.4) + 4) +
+                     (s > 1 ? 6 + 2 * s * sum_bytes / 6e6 : 0);
+    if (t < least) least = t, best = {Plan::SMALL, s};
+  }
+  return best;
+}
+
+// Tiles of few rows where a group has up to 32 on average, or where all of
+// them run at once (256 workgroups): beyond, every further row tile streams
+// the weights again.  Few rows against Small, us: H = 4096, F = 14336, up and
+// down projection, 32 rows 52 + 50 : 57 + 56, 64 rows 77 + 46 : 60 + 57; H =
+// 2048, F = 1408, 256 rows 14 + 8 : 17 + 17; 16 groups of 32 rows on average
+// 43 + 27 : 46 + 27, of 64 rows 60 + 37 : 49 + 34.
+// Eight waves share the depth where one workgroup per CU holds all tiles, else
+// four.  A step is 0.5 us, and a part's sum costs some 6 us more, so the depth
+// is split while a wave has more than 24 steps: 1 row, H = 4096, down
+// projection of F = 14336 (64 tiles, 448 steps) 60, 39 in two parts, 31 in four.
+inline bool few_rows(int T, int G, double tiles) { return T <= 32LL * G || tiles <= 256; }
+inline Plan few_plan(double tiles, int steps) {
+  const auto waves = [&](int s) { return tiles * s <= 256 ? 8 : 4; };
+  int s = 1;
+  while (s < MAX_SPLIT && tiles * s * 2 <= 512 && steps / (s * waves(s)) > 24) s *= 2;
+  return {waves(s) == 8 ? Plan::FEW8 : Plan::FEW4, s};
+}
+
+// Row tiles of T rows in G groups: the last of a group is half full on average.
+inline double row_tiles(int T, int G, int bm) {
+  return G == 1 ? (double)ceil_div(T, bm) : std::min((double)T, (double)T / bm + 0.5 * G);
+}
+
+// The plan of a product of T rows in G groups: `cols` columns of the output
+// from `per` (2 where gated) columns of weights each, a depth of `stages`.
+inline Plan plan_of(int T, int G, int cols, int per, int stages, bool can_be_few) {
+  const double few = row_tiles(T, G, 32) * ceil_div(cols, 64);
+  if (can_be_few && few_rows(T, G, few)) return few_plan(few, stages * 2);
+  return tile_plan(row_tiles(T, G, Wide::BM) * ceil_div(cols * per, Wide::BN),
+                   row_tiles(T, G, Small::BM) * ceil_div(cols * per, Small::BN), stages, 4.0 * T * cols * per);
+}
 
 __device__ __forceinline__ u32x4_t pack8(const float (&v)[8]) {
   return u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
