@@ -330,43 +330,51 @@ def moe_tile_geometry(h: int):
 
 
 # The calls over row groups take no handle, so nothing else knows the sizes of
-# their tensors: each is checked here against the config, and the call runs on
-# the tensors' own device.
+# their tensors: each is checked here against the config (dense, of the given
+# type and size, on one GPU), and the call runs on the tensors' own device.
 
-class _Operands:
-    """Pointers of a call's tensors, checked to be dense, of the given type and size, and on one device."""
+def _device_of(name: str, t: Optional[torch.Tensor]) -> int:
+    if t is None or not t.is_cuda:
+        raise ValueError(f"{name} must be in GPU memory")
+    return t.get_device()
 
-    def __init__(self, first: torch.Tensor, name: str):
-        if first is None or not first.is_cuda:
-            raise ValueError(f"{name} must be in GPU memory")
-        self.device = first.device
 
-    def __call__(self, name: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, optional: bool = False):
-        if t is None:
-            if not optional:
-                raise ValueError(f"{name} is missing")
-            return None
-        if t.dtype != dtype or t.numel() != numel or t.device != self.device:
-            raise ValueError(f"{name} must be {dtype} with {numel} elements on {self.device}, "
-                             f"not {t.dtype} with {t.numel()} on {t.device}")
-        return _ptr(t)
+def _arg(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, dev: int) -> int:
+    """The address of a tensor that is as it has to be."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != dev:
+        raise ValueError(f"{name} must be {dtype} with {numel} elements on cuda:{dev}, "
+                         f"not {t.dtype} with {t.numel()} on {t.device}")
+    if not t.is_contiguous():
+        raise ValueError("tensors passed to the MoE library must be contiguous")
+    return t.data_ptr()
 
-    def off(self, t: Optional[torch.Tensor], n_groups: int):
-        return self("group_off", t, torch.int32, n_groups + 1, optional=n_groups == 1)
 
-    def ws(self, t: torch.Tensor):
-        if t is None:
-            raise ValueError("ws is missing")
-        nbytes = t.numel() * t.element_size()
-        return self("ws", t, t.dtype, t.numel()), nbytes
+def _off(t: Optional[torch.Tensor], n_groups: int, dev: int) -> Optional[int]:
+    return None if t is None and n_groups == 1 else _arg("group_off", t, torch.int32, n_groups + 1, dev)
 
-    def stream(self, stream):
-        """The given stream, or the device's current one."""
-        if stream is None:
-            stream = torch.cuda.current_stream(self.device)
-        elif stream.device != self.device:
-            raise ValueError(f"the stream is of {stream.device}, the tensors are on {self.device}")
-        return C.c_void_p(stream.cuda_stream)
+
+def _ws(t: Optional[torch.Tensor], dev: int):
+    """Address and size of a workspace."""
+    if t is None:
+        raise ValueError("ws is missing")
+    n = t.numel()
+    return _arg("ws", t, t.dtype, n, dev), n * t.element_size()
+
+
+def _call(name: str, dev: int, stream, *args) -> None:
+    """Calls on device `dev`, on the given stream of it or on its current one."""
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device_index != dev:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{dev}")
+    if torch.cuda.current_device() == dev:
+        st = getattr(_lib, name)(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(dev):
+            st = getattr(_lib, name)(*args, stream.cuda_stream)
+    _check(name, st)
 
 
 def moe_ffn_workspace_size(cfg: moe_ffn_config, backward: bool = False) -> int:
@@ -376,45 +384,41 @@ def moe_ffn_workspace_size(cfg: moe_ffn_config, backward: bool = False) -> int:
 
 
 def moe_ffn_forward(cfg: moe_ffn_config, x, group_off, w1, w3, w2, gate, up, y, ws, stream=None) -> None:
-    o, bf = _Operands(x, "x"), torch.bfloat16
-    T, H, F, G = cfg.rows, cfg.hidden, cfg.ffn, cfg.n_groups
-    args = [o("x", x, bf, T * H), o.off(group_off, G), o("w1", w1, bf, G * H * F), o("w3", w3, bf, G * H * F),
-            o("w2", w2, bf, G * F * H), o("gate", gate, bf, T * F, True), o("up", up, bf, T * F, True),
-            o("y", y, bf, T * H), *o.ws(ws)]
-    with torch.cuda.device(o.device):
-        _check("moe_ffn_forward", _lib.moe_ffn_forward(C.byref(cfg), *args, o.stream(stream)))
+    dev, bf = _device_of("x", x), torch.bfloat16
+    T, G = cfg.rows, cfg.n_groups
+    TH, TF, W = T * cfg.hidden, T * cfg.ffn, G * cfg.hidden * cfg.ffn
+    _call("moe_ffn_forward", dev, stream, cfg, _arg("x", x, bf, TH, dev), _off(group_off, G, dev),
+          _arg("w1", w1, bf, W, dev), _arg("w3", w3, bf, W, dev), _arg("w2", w2, bf, W, dev),
+          None if gate is None else _arg("gate", gate, bf, TF, dev), None if up is None else _arg("up", up, bf, TF, dev),
+          _arg("y", y, bf, TH, dev), *_ws(ws, dev))
 
 
 def moe_ffn_backward(cfg: moe_ffn_config, dy, x, group_off, w1, w3, w2, gate, up, dx, dw1, dw3, dw2, ws,
                      stream=None) -> None:
-    o, bf = _Operands(dy, "dy"), torch.bfloat16
-    T, H, F, G = cfg.rows, cfg.hidden, cfg.ffn, cfg.n_groups
-    args = [o("dy", dy, bf, T * H), o("x", x, bf, T * H), o.off(group_off, G), o("w1", w1, bf, G * H * F),
-            o("w3", w3, bf, G * H * F), o("w2", w2, bf, G * F * H), o("gate", gate, bf, T * F),
-            o("up", up, bf, T * F), o("dx", dx, bf, T * H, True), o("dw1", dw1, bf, G * H * F, True),
-            o("dw3", dw3, bf, G * H * F, True), o("dw2", dw2, bf, G * F * H, True), *o.ws(ws)]
-    with torch.cuda.device(o.device):
-        _check("moe_ffn_backward", _lib.moe_ffn_backward(C.byref(cfg), *args, o.stream(stream)))
+    dev, bf = _device_of("dy", dy), torch.bfloat16
+    T, G = cfg.rows, cfg.n_groups
+    TH, TF, W = T * cfg.hidden, T * cfg.ffn, G * cfg.hidden * cfg.ffn
+    _call("moe_ffn_backward", dev, stream, cfg, _arg("dy", dy, bf, TH, dev), _arg("x", x, bf, TH, dev),
+          _off(group_off, G, dev), _arg("w1", w1, bf, W, dev), _arg("w3", w3, bf, W, dev), _arg("w2", w2, bf, W, dev),
+          _arg("gate", gate, bf, TF, dev), _arg("up", up, bf, TF, dev),
+          None if dx is None else _arg("dx", dx, bf, TH, dev), None if dw1 is None else _arg("dw1", dw1, bf, W, dev),
+          None if dw3 is None else _arg("dw3", dw3, bf, W, dev), None if dw2 is None else _arg("dw2", dw2, bf, W, dev),
+          *_ws(ws, dev))
 
 
 def moe_quantize_rows_i8(rows: int, cols: int, x, q, scale, stream=None) -> None:
-    o = _Operands(x, "x")
-    args = [o("x", x, torch.bfloat16, rows * cols), o("q", q, torch.int8, rows * cols),
-            o("scale", scale, torch.float32, rows)]
-    with torch.cuda.device(o.device):
-        _check("moe_quantize_rows_i8", _lib.moe_quantize_rows_i8(int(rows), int(cols), *args, o.stream(stream)))
+    dev = _device_of("x", x)
+    _call("moe_quantize_rows_i8", dev, stream, int(rows), int(cols), _arg("x", x, torch.bfloat16, rows * cols, dev),
+          _arg("q", q, torch.int8, rows * cols, dev), _arg("scale", scale, torch.float32, rows, dev))
 
 
 def moe_quantize_weights_i8(n_groups: int, depth: int, channels: int, q_channels: int, first: int, w, wq, scale,
                             stream=None) -> None:
-    o = _Operands(w, "w")
-    args = [o("w", w, torch.bfloat16, n_groups * depth * channels),
-            o("wq", wq, torch.int8, n_groups * q_channels * depth),
-            o("scale", scale, torch.float32, n_groups * q_channels)]
-    with torch.cuda.device(o.device):
-        _check("moe_quantize_weights_i8",
-               _lib.moe_quantize_weights_i8(int(n_groups), int(depth), int(channels), int(q_channels), int(first),
-                                            *args, o.stream(stream)))
+    dev = _device_of("w", w)
+    _call("moe_quantize_weights_i8", dev, stream, int(n_groups), int(depth), int(channels), int(q_channels), int(first),
+          _arg("w", w, torch.bfloat16, n_groups * depth * channels, dev),
+          _arg("wq", wq, torch.int8, n_groups * q_channels * depth, dev),
+          _arg("scale", scale, torch.float32, n_groups * q_channels, dev))
 
 
 def moe_gemm_i8_workspace_size(cfg: moe_gemm_i8_config) -> int:
@@ -424,14 +428,13 @@ def moe_gemm_i8_workspace_size(cfg: moe_gemm_i8_config) -> int:
 
 
 def moe_gemm_i8(cfg: moe_gemm_i8_config, xq, x_scale, group_off, wq, w_scale, y, ws, stream=None) -> None:
-    o = _Operands(xq, "xq")
+    dev = _device_of("xq", xq)
     T, K, N, G = cfg.rows, cfg.depth, cfg.channels, cfg.n_groups
     out = N if cfg.act == MOE_ACT_NONE else N // 2
-    args = [o("xq", xq, torch.int8, T * K), o("x_scale", x_scale, torch.float32, T), o.off(group_off, G),
-            o("wq", wq, torch.int8, G * N * K), o("w_scale", w_scale, torch.float32, G * N),
-            o("y", y, torch.bfloat16, T * out), *o.ws(ws)]
-    with torch.cuda.device(o.device):
-        _check("moe_gemm_i8", _lib.moe_gemm_i8(C.byref(cfg), *args, o.stream(stream)))
+    _call("moe_gemm_i8", dev, stream, cfg, _arg("xq", xq, torch.int8, T * K, dev),
+          _arg("x_scale", x_scale, torch.float32, T, dev), _off(group_off, G, dev),
+          _arg("wq", wq, torch.int8, G * N * K, dev), _arg("w_scale", w_scale, torch.float32, G * N, dev),
+          _arg("y", y, torch.bfloat16, T * out, dev), *_ws(ws, dev))
 
 
 # ---- convenience --------------------------------------------------------------
