@@ -9,9 +9,10 @@
 // A stage of the depth is 128 bytes of it: 64 bf16 or 128 int8 values, BM * 128
 // and BN * 128 bytes, loaded straight into LDS (global_load_lds_dwordx4), two
 // stages in turn.  LDS images, in 16-byte granules:
-//  - k-contiguous: row r at r * 128 bytes, granule c at position c ^ (r & 7).
+//  - k-contiguous: row r at r * 128 bytes, granule c at position c ^ (r / 2) % 8.
 //    A fragment (lane: row l % 32, 16 bytes of the depth) is one ds_read_b128,
-//    and eight consecutive lanes read eight different positions.
+//    and the 16 rows read together lie on different banks (c ^ r % 8: every
+//    read took twice the cycles).
 //  - transposed (bf16): two panels of half the tile's width, each 64 depth rows
 //    of PW columns; granule c of row k at position c ^ swz(k).  A fragment is
 //    two ds_read_b64_tr_b16: 16 lanes address 4 depth rows x 16 columns, lane
@@ -33,7 +34,7 @@
 #include <cmath>
 #include <type_traits>
 
-#include "common.h"
+#include "blocks.h"
 #include "gemm.h"
 
 namespace moe {
@@ -112,10 +113,16 @@ struct Tile {
       for (int i = 0; i < N; ++i) {
         const int r = (wave * N + i) * 8 + (lane >> 3);
         const int rr = m.p2 && r >= ROWS / 2 ? r - ROWS / 2 : r;
-        o[i] = (uint32_t)min(rr, m.valid - 1) * m.ld + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+        o[i] = (uint32_t)min(rr, m.valid - 1) * m.ld + (uint32_t)(granule<N>(i, wave, lane) * 16);
       }
     }
   }
+  // the granule of its row that a lane's k-contiguous load i takes
+  template <int N>
+  static __device__ __forceinline__ int granule(int i, int wave, int lane) {
+    return (lane & 7) ^ swz_row((wave * N + i) * 8 + (lane >> 3));
+  }
+  static __device__ __forceinline__ int swz_row(int r) { return (r >> 1) & 7; }
   template <int PW>
   static __device__ __forceinline__ int swz(int k) {
     return PW == 128 ? 4 * (k & 3) : 4 * ((k >> 1) & 1);
@@ -142,7 +149,7 @@ struct Tile {
     } else {
       const int r = wm * 32 + (lane & 31);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk) f.a[kk] = (uint32_t)(r * DEPTH + ((kk * 2 + (lane >> 5)) ^ (r & 7)) * 16);
+      for (int kk = 0; kk < 4; ++kk) f.a[kk] = (uint32_t)(r * DEPTH + ((kk * 2 + (lane >> 5)) ^ swz_row(r)) * 16);
     }
     if constexpr (BT) {
       constexpr int PW = BN / 2;
@@ -153,7 +160,7 @@ struct Tile {
       const int r = wn * (NB / 2) * 32 + (lane & 31);
 #pragma unroll
       for (int kk = 0; kk < 4; ++kk)
-        f.b[kk] = (uint32_t)(A_BYTES + r * DEPTH + ((kk * 2 + (lane >> 5)) ^ (r & 7)) * 16);
+        f.b[kk] = (uint32_t)(A_BYTES + r * DEPTH + ((kk * 2 + (lane >> 5)) ^ swz_row(r)) * 16);
     }
     return f;
   }
@@ -232,14 +239,19 @@ struct Tile {
     const int rest = n1 % KE;  // depth of the last stage, 0: whole (only without a second pair)
     // instruction i of stage s (its operands' addresses at, its offsets and LDS)
     auto issue_one = [&](int i, const char* a, const char* b, uint32_t so, uint32_t back) {
-      if (i < AI) dma16(a, oa[i < AI ? i : 0] - back, la + so + i * 1024);
-      else dma16(b, ob[i < AI ? 0 : i - AI] - back, lb + so + (i - AI) * 1024);
+      if (i < AI) {
+        const uint32_t o = oa[i < AI ? i : 0];
+        dma16(a, I8 && (granule<AI>(i, wave, lane) & 4) ? o - back : o, la + so + i * 1024);
+      } else {
+        const uint32_t o = ob[i < AI ? 0 : i - AI];
+        dma16(b, I8 && (granule<BI>(i - AI, wave, lane) & 4) ? o - back : o, lb + so + (i - AI) * 1024);
+      }
     };
     const auto base_a = [&](int s) { return s < half ? pa + s * sa : pa2 + (s - half) * sa; };
     const auto base_b = [&](int s) { return s < half ? pb + s * sb : pb2 + (s - half) * sb; };
     // (int8: a last stage of 64 has no granules 4..7; they are read as 0..3)
     const auto back_of = [&](int s) -> uint32_t {
-      return I8 && rest && s == ns - 1 && (((lane & 7) ^ (lane >> 3)) & 4) ? 64 : 0;
+      return I8 && rest && s == ns - 1 ? 64 : 0;
     };
     auto issue = [&](int s) {
       const uint32_t so = (s & 1) * STAGE, back = back_of(s);
@@ -385,6 +397,14 @@ struct Tile {
   }
 };
 
+// dma16 for lines that are read once: they do not displace what the L2 holds
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16_once(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // ---------------------------------------------------------------------------
 // Few rows: up to 32 rows x 64 columns (gated: 64 of each matrix), whose time
 // is that of streaming the weights.  The four or
@@ -394,7 +414,7 @@ struct Tile {
 // its oldest slot, multiplies it and loads a later step into it.  The waves'
 // sums are added in a fixed order at the end.
 // LDS images of a slot: weights, k-contiguous as rows of 64 bytes, granule c
-// at c ^ (r / 2) % 4, or transposed as 32 depth rows of 64 columns per matrix
+// at c ^ (r / 4) % 4, or transposed as 32 depth rows of 64 columns per matrix
 // (a panel of PW = 64, as above); then the 32 rows of A, k-contiguous.
 // ---------------------------------------------------------------------------
 template <int NW_, bool I8_, bool BT_, bool GATED_>
@@ -424,13 +444,13 @@ struct Few {
         ow[i] = (uint32_t)k * B.ld + (uint32_t)min(B.col + c * 8, B.cols - 8) * 2u;
       } else {
         const int r = i % 4 * 16 + (lane >> 2);
-        ow[i] = (uint32_t)min(r, B.valid - 1) * B.ld + (uint32_t)(((lane & 3) ^ ((r >> 1) & 3)) * 16);
+        ow[i] = (uint32_t)min(r, B.valid - 1) * B.ld + (uint32_t)(((lane & 3) ^ ((r >> 2) & 3)) * 16);
       }
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = i * 16 + (lane >> 2);
-      ox[i] = (uint32_t)min(r, A.valid - 1) * A.ld + (uint32_t)(((lane & 3) ^ ((r >> 1) & 3)) * 16);
+      ox[i] = (uint32_t)min(r, A.valid - 1) * A.ld + (uint32_t)(((lane & 3) ^ ((r >> 2) & 3)) * 16);
     }
     const char *pa = uniform_ptr(A.p), *pb = uniform_ptr(B.p), *pb2 = GATED ? uniform_ptr(B.p2) : nullptr;
     const size_t sb = BT ? (size_t)B.ld * 32 : STEP;
@@ -441,7 +461,13 @@ struct Few {
       const size_t s = s0 + wave + j * NW;
       const uint32_t l = l0 + j % SLOTS * SLOT;
 #pragma unroll
-      for (int i = 0; i < WI; ++i) dma16((GATED && i >= 4 ? pb2 : pb) + s * sb, ow[i], l + i * 1024);
+      for (int i = 0; i < WI; ++i) {
+        const char* w = (GATED && i >= 4 ? pb2 : pb) + s * sb;
+        // transposed weights come in whole lines, read once (8 to 10% of the
+        // time); a step of k-contiguous ones is half of each line
+        if constexpr (BT) dma16_once(w, ow[i], l + i * 1024);
+        else dma16(w, ow[i], l + i * 1024);
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i) dma16(pa + s * STEP, ox[i], l + W_BYTES + i * 1024);
     };
@@ -449,7 +475,7 @@ struct Few {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = lane & 31;
-      fx[i] = (uint32_t)(r * STEP + ((i * 2 + (lane >> 5)) ^ ((r >> 1) & 3)) * 16);
+      fx[i] = (uint32_t)(r * STEP + ((i * 2 + (lane >> 5)) ^ ((r >> 2) & 3)) * 16);
       fw[i] = BT ? Big::template tr_offset<64>(0, i * 32, lane) : fx[i];
     }
     Acc1 acc[NB];
@@ -536,20 +562,21 @@ constexpr int MAX_SPLIT = 16;
 
 // Small or Wide tiles, from how many there are of each: rounds of workgroups
 // (one Wide or two Small per CU) times the time of one.  Measured, us per
-// stage: Wide 1.9 to 2.2; Small 0.85 with one workgroup per CU and 1.4 with
-// two.  So Wide tiles take 1.4 times less where they fill the chip, and Small
-// ones win where Wide ones leave CUs idle: dh of 2000 rows, H = F = 4096, 128
-// Wide tiles 123, 512 Small 89; of 4000 rows 147 : 179.  A split costs a
+// stage: Wide 1.85 to 2.2; Small 0.85 with one workgroup per CU and 1.2 to 1.4
+// with two.  So Wide tiles take 1.3 times less where they fill the chip, and
+// Small ones win where Wide ones leave CUs idle: dh of 2000 rows, H = F = 4096,
+// 128 Wide tiles 123, 512 Small 89; of 4000 rows 147 : 179; int8, 6007 rows in
+// 16 groups, 2048 x 2816, 352 Wide tiles 71, 1210 Small 60.  A split costs a
 // launch (6 with its gap) and the sums' way out and back, `sum_bytes` per part
 // (6 TB/s): dx of 333 rows in 4 groups, H = 1024, F = 2816 (40 Small tiles, 88
 // stages), 80 : 52 : 33 : 25 in 1, 2, 4 and 8 parts; dh of 2000 rows above, 89
 // against 83 + 27 in two.
 inline Plan tile_plan(double wide, double small, int stages, double sum_bytes) {
   Plan best{Plan::WIDE, 1};
-  double least = std::ceil(wide / 256) * (stages * 2.0 + 6);
+  double least = std::ceil(wide / 256) * (stages * 2.0 + 4);
   for (int s = 1; s <= MAX_SPLIT && s <= std::max(stages, 1); s *= 2) {
-    const double w = small * s;
-    const double t = std::ceil(w / 512) * (ceil_div(stages, s) * (w <= 256 ? 0.85 : 1.4) + 4) +
+    const double w = small * s, rounds = w <= 512 ? 1 : w / 512 + 0.35;
+    const double t = rounds * (ceil_div(stages, s) * (w <= 256 ? 0.85 : 1.25) + 3) +
                      (s > 1 ? 6 + 2 * s * sum_bytes / 6e6 : 0);
     if (t < least) least = t, best = {Plan::SMALL, s};
   }
@@ -562,28 +589,31 @@ inline Plan tile_plan(double wide, double small, int stages, double sum_bytes) {
 // down projection, 32 rows 52 + 50 : 57 + 56, 64 rows 77 + 46 : 60 + 57; H =
 // 2048, F = 1408, 256 rows 14 + 8 : 17 + 17; 16 groups of 32 rows on average
 // 43 + 27 : 46 + 27, of 64 rows 60 + 37 : 49 + 34.
-// Eight waves share the depth where one workgroup per CU holds all tiles, else
-// four.  A step is 0.5 us, and a part's sum costs some 6 us more, so the depth
-// is split while a wave has more than 24 steps: 1 row, H = 4096, down
-// projection of F = 14336 (64 tiles, 448 steps) 60, 39 in two parts, 31 in four.
+// Eight waves share the depth where one workgroup per CU holds all tiles (the
+// most there can be: 264 of 8 waves take two rounds), else four.  A step is
+// 0.5 us, and a part's sum costs some 6 us more, so the depth is split while a
+// wave has more than 24 steps: 1 row, H = 4096, down projection of F = 14336
+// (64 tiles, 448 steps) 60, 39 in two parts, 31 in four.
 inline bool few_rows(int T, int G, double tiles) { return T <= 32LL * G || tiles <= 256; }
-inline Plan few_plan(double tiles, int steps) {
-  const auto waves = [&](int s) { return tiles * s <= 256 ? 8 : 4; };
+inline Plan few_plan(long long most, int steps) {
+  const auto waves = [&](int s) { return most * s <= 256 ? 8 : 4; };
   int s = 1;
-  while (s < MAX_SPLIT && tiles * s * 2 <= 512 && steps / (s * waves(s)) > 24) s *= 2;
+  while (s < MAX_SPLIT && most * s * 2 <= 512 && steps / (s * waves(s)) > 24) s *= 2;
   return {waves(s) == 8 ? Plan::FEW8 : Plan::FEW4, s};
 }
 
-// Row tiles of T rows in G groups: the last of a group is half full on average.
+// Row tiles of T rows in G groups to expect: the last of a group is half full,
+// and every group that has rows has one (T rows leave exp(-T / G) of them empty).
 inline double row_tiles(int T, int G, int bm) {
-  return G == 1 ? (double)ceil_div(T, bm) : std::min((double)T, (double)T / bm + 0.5 * G);
+  if (G == 1) return ceil_div(T, bm);
+  return std::min((double)T, std::max((double)T / bm + 0.5 * G, G * (1 - std::exp(-(double)T / G))));
 }
 
 // The plan of a product of T rows in G groups: `cols` columns of the output
 // from `per` (2 where gated) columns of weights each, a depth of `stages`.
 inline Plan plan_of(int T, int G, int cols, int per, int stages, bool can_be_few) {
-  const double few = row_tiles(T, G, 32) * ceil_div(cols, 64);
-  if (can_be_few && few_rows(T, G, few)) return few_plan(few, stages * 2);
+  if (can_be_few && few_rows(T, G, row_tiles(T, G, 32) * ceil_div(cols, 64)))
+    return few_plan((long long)max_row_tiles(T, G, 32) * ceil_div(cols, 64), stages * 2);
   return tile_plan(row_tiles(T, G, Wide::BM) * ceil_div(cols * per, Wide::BN),
                    row_tiles(T, G, Small::BM) * ceil_div(cols * per, Small::BN), stages, 4.0 * T * cols * per);
 }
