@@ -19,6 +19,9 @@ struct FfnArgs {
   uint16_t *dx, *dw1, *dw3, *dw2;  // backward's (dx, or the three dw, may be NULL)
   float* part;                     // partial sums [split][T][width] of a split product
   int split;
+  float* dw_part;                  // and [dw_split][3][G][H F] of the weights' gradients
+  int dw_split;
+  int dx_blocks;                   // workgroups of dx, before those of the weights' gradients
 };
 
 __device__ __forceinline__ const char* bytes(const uint16_t* p) { return reinterpret_cast<const char*>(p); }
@@ -123,15 +126,15 @@ __device__ __forceinline__ tile::Operand weights_op(const FfnArgs& a, const RowT
   }
 }
 
+// The product OP's tile of workgroup `block`
 template <Op OP, typename S>
-__global__ __launch_bounds__(S::THREADS) void ffn_kernel(FfnArgs a) {
+__device__ __forceinline__ void rows_tile(const FfnArgs& a, int block, char* lds) {
   using Tl = tile::Tile<S, false, false, OP == UP || OP == DOWN>;
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
   const RowTiles list(a.off, a.G, a.T, Tl::BM);
   constexpr int COLS = GATED<OP> ? Tl::BN / 2 : Tl::BN;
   const int nt = ceil_div(cols_of<OP>(a), COLS), stages = depth_of<OP>(a) / 64;
   int m, n;
-  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
+  if (!tile::pick(block, list.total, nt * a.split, &m, &n)) return;
   const RowTile rt = list.at(m);
   const int part = n / nt, n0 = n % nt * COLS, rows = rt.end - rt.begin;
   const int k0 = stages * part / a.split * 64, k1 = stages * (part + 1) / a.split * 64;
@@ -146,6 +149,15 @@ __global__ __launch_bounds__(S::THREADS) void ffn_kernel(FfnArgs a) {
   });
 }
 
+template <typename S>
+constexpr int LDS_OF = tile::Tile<S, false, false, false>::LDS;
+
+template <Op OP, typename S>
+__global__ __launch_bounds__(S::THREADS) void ffn_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[LDS_OF<S>];
+  rows_tile<OP, S>(a, blockIdx.x, lds);
+}
+
 template <Op OP, int NW>
 using FewOf = tile::Few<NW, false, true, GATED<OP>>;
 
@@ -156,7 +168,7 @@ __global__ __launch_bounds__(NW * 64) void ffn_few_kernel(FfnArgs a) {
   const RowTiles list(a.off, a.G, a.T, Fw::BM);
   const int nt = cols_of<OP>(a) / Fw::COLS, steps = depth_of<OP>(a) / Fw::KE;
   int m, n;
-  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
+  if (!tile::pick(blockIdx.x, list.total, nt * a.split, &m, &n)) return;
   const RowTile rt = list.at(m);
   const int part = n / nt, n0 = n % nt * Fw::COLS;
   Fw::run(lds, rows_op<OP>(a, rt, 0), weights_op<OP>(a, rt, 0, n0), steps * part / a.split, steps * (part + 1) / a.split,
@@ -183,19 +195,24 @@ __global__ __launch_bounds__(256) void ffn_sum_kernel(FfnArgs a) {
 // dW1 = x^T dgate, dW3 = x^T dup, dW2 = h^T dy, each group's: its rows are the
 // depth, in stages of 64; a split takes runs of whole stages.
 template <typename S>
-__global__ __launch_bounds__(S::THREADS) void ffn_dw_kernel(FfnArgs a) {
+__device__ __forceinline__ void dw_tile(const FfnArgs& a, int block, char* lds) {
   using Tl = tile::Tile<S, false, true, true>;
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
-  // tiles of a group: those of dW1, of dW3, then of dW2 (each XCD takes an
-  // eighth of every group's: groups differ in depth)
+  static_assert(Tl::LDS <= LDS_OF<S>, "LDS");
+  // Tiles of a group: those of dW1, of dW3, then of dW2.  Groups differ in
+  // depth, so each XCD takes an eighth of every group's, and up to 64 groups
+  // are taken in the order of their depths, the deepest first: 32 groups of 83
+  // to 5286 rows, H = 2048, F = 768, 438 us with runs of groups on each XCD,
+  // TODO.
   const int hm = ceil_div(a.H, Tl::BM), fn = ceil_div(a.F, Tl::BN), fm = ceil_div(a.F, Tl::BM), hn = ceil_div(a.H, Tl::BN);
-  const int t13 = hm * fn, per = 2 * t13 + fm * hn, run = ceil_div(per * a.split, NXCD);
-  const int slot = blockIdx.x / NXCD, g = slot / run, w = (blockIdx.x % NXCD) * run + slot % run;
-  if (w >= per * a.split) return;
+  const int t13 = hm * fn, per = 2 * t13 + fm * hn, run = ceil_div(per * a.dw_split, NXCD);
+  const int slot = block / NXCD, w = block % NXCD * run + slot % run;
+  if (w >= per * a.dw_split) return;
   const int part = w / per, i = w % per, which = i / t13 < 2 ? i / t13 : 2;
-  int b, e;
-  group_rows(a.off, a.T, g, &b, &e);
-  const int stages = ceil_div(e - b, 64), k0 = stages * part / a.split * 64, k1 = min(stages * (part + 1) / a.split * 64, e - b);
+  int g = slot / run, b, e;
+  if (a.off && a.G <= 64) g = ranked_group(a.off, a.T, a.G, g, &b, &e);
+  else group_rows(a.off, a.T, g, &b, &e);
+  const int stages = ceil_div(e - b, 64);
+  const int k0 = stages * part / a.dw_split * 64, k1 = min(stages * (part + 1) / a.dw_split * 64, e - b);
   const uint16_t *p = which == 2 ? a.h : a.x, *q = which == 0 ? a.dgate : which == 1 ? a.dup : a.dy;
   const int M = which == 2 ? a.F : a.H, N = which == 2 ? a.H : a.F, mt = which == 2 ? fm : hm, nt = which == 2 ? hn : fn;
   const int j = i - which * t13, band = j / (tile::NEAR * nt), first = band * tile::NEAR;
@@ -208,10 +225,10 @@ __global__ __launch_bounds__(S::THREADS) void ffn_dw_kernel(FfnArgs a) {
   Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
   const size_t at = ((size_t)g * M + m0) * N + n0, all = (size_t)a.G * a.H * a.F;
   uint16_t* out = (which == 0 ? a.dw1 : which == 1 ? a.dw3 : a.dw2) + at;
-  float* sums = a.part + (part * 3 + which) * all + at;
+  float* sums = a.dw_part + (part * 3 + which) * all + at;
   Tl::template epilogue<false>(acc, lds, min(Tl::BM, M - m0), [&](int r, int c, const uint32_t (&v)[8]) {
     if (n0 + c >= N) return;
-    if (a.split > 1) {
+    if (a.dw_split > 1) {
       u32x4_t* o = reinterpret_cast<u32x4_t*>(sums + (size_t)r * N + c);
       o[0] = u32x4_t{v[0], v[1], v[2], v[3]};
       o[1] = u32x4_t{v[4], v[5], v[6], v[7]};
@@ -224,13 +241,22 @@ __global__ __launch_bounds__(S::THREADS) void ffn_dw_kernel(FfnArgs a) {
   });
 }
 
+// dx and the weights' gradients in one launch (either may have no workgroups):
+// the last tiles of the one run beside the first of the other.
+template <typename S>
+__global__ __launch_bounds__(S::THREADS) void ffn_grad_kernel(FfnArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[LDS_OF<S>];
+  if ((int)blockIdx.x < a.dx_blocks) rows_tile<DX, S>(a, blockIdx.x, lds);
+  else dw_tile<S>(a, blockIdx.x - a.dx_blocks, lds);
+}
+
 __global__ __launch_bounds__(256) void ffn_dw_sum_kernel(FfnArgs a) {
   const size_t all = (size_t)a.G * a.H * a.F, i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= 3 * all) return;
   float f[8] = {};
-  for (int s = 0; s < a.split; ++s)
+  for (int s = 0; s < a.dw_split; ++s)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] += a.part[s * 3 * all + i + j];
+    for (int j = 0; j < 8; ++j) f[j] += a.dw_part[s * 3 * all + i + j];
   store8((i < all ? a.dw1 : i < 2 * all ? a.dw3 : a.dw2) + i % all, f);
 }
 
@@ -243,9 +269,36 @@ template <typename S>
 int dw_tiles(const FfnArgs& a) {  // of a group
   return 2 * ceil_div(a.H, S::BM) * ceil_div(a.F, S::BN) + ceil_div(a.F, S::BM) * ceil_div(a.H, S::BN);
 }
-tile::Plan dw_plan(const FfnArgs& a) {
-  return tile::tile_plan((double)a.G * dw_tiles<tile::Wide>(a), (double)a.G * dw_tiles<tile::Small>(a),
-                         ceil_div(ceil_div(a.T, a.G), 64), 12.0 * a.G * a.H * a.F);
+// The kind of tiles and the splits of dx and of the weights' gradients, which
+// share a launch: its time is that of all their tiles, or of the deepest one
+// (us per stage and per tile, and for a split, as in tile_plan).  The same
+// whichever of them are asked for, so that results do not depend on it.
+struct GradPlan {
+  tile::Plan::Kind kind;
+  int dx_split, dw_split;
+};
+template <typename S>
+void grad_times(const FfnArgs& a, tile::Plan::Kind kind, GradPlan* best, double* least) {
+  const bool wide = kind == tile::Plan::WIDE;
+  const double cap = wide ? 256 : 512, busy = wide ? 2.0 : 1.25, alone = wide ? 1.85 : 0.85, over = wide ? 4 : 3;
+  const double tx = tile::row_tiles(a.T, a.G, S::BM) * ceil_div(a.H, S::BN), tw = (double)a.G * dw_tiles<S>(a);
+  const int sx = 2 * a.F / 64, sw = std::max(1, ceil_div(ceil_div(a.T, a.G), 64)), most = wide ? 1 : tile::MAX_SPLIT;
+  for (int x = 1; x <= most && x <= sx; x *= 2)
+    for (int w = 1; w <= most && w <= sw; w *= 2) {
+      const int dx_stages = ceil_div(sx, x), dw_stages = ceil_div(sw, w);
+      const double all = tx * x * (dx_stages * busy + over) + tw * w * (dw_stages * busy + over);
+      const double deepest = std::max(dx_stages, dw_stages) * alone + over;
+      const double t = (tx * x + tw * w <= cap ? deepest : std::max(all / cap, deepest) + 0.35 * deepest) +
+                       (x > 1 ? 6 + 8.0 * x * a.T * a.H / 6e6 : 0) + (w > 1 ? 6 + 24.0 * w * a.G * a.H * a.F / 6e6 : 0);
+      if (t < *least) *least = t, *best = {kind, x, w};
+    }
+}
+GradPlan grad_plan(const FfnArgs& a) {
+  GradPlan p{};
+  double least = 1e30;
+  grad_times<tile::Wide>(a, tile::Plan::WIDE, &p, &least);
+  grad_times<tile::Small>(a, tile::Plan::SMALL, &p, &least);
+  return p;
 }
 
 // Launches are for the most tiles that the groups can have.
@@ -267,15 +320,20 @@ void launch(FfnArgs a, hipStream_t s) {
   if (a.split > 1) ffn_sum_kernel<OP><<<(int)(((long long)a.T * cols_of<OP>(a) / 8 + 255) / 256), 256, 0, s>>>(a);
 }
 
-void launch_dw(FfnArgs a, hipStream_t s) {
-  const tile::Plan p = dw_plan(a);
-  a.split = p.split;
-  const auto go = [&](auto kernel, int tiles, int threads) {
-    kernel<<<a.G * ceil_div(tiles * a.split, NXCD) * NXCD, threads, 0, s>>>(a);
+void launch_grad(FfnArgs a, hipStream_t s) {
+  const GradPlan p = grad_plan(a);
+  a.split = p.dx_split, a.dw_split = p.dw_split;
+  a.dw_part = a.part + (a.dx && a.split > 1 ? (size_t)a.split * a.T * a.H : 0);
+  const auto go = [&](auto kernel, int bm, int bn, int threads, int tiles) {
+    a.dx_blocks = a.dx ? tile::grid_of(max_row_tiles(a.T, a.G, bm), ceil_div(a.H, bn) * a.split) : 0;
+    const int dw_blocks = a.dw1 ? a.G * ceil_div(tiles * a.dw_split, NXCD) * NXCD : 0;
+    kernel<<<a.dx_blocks + dw_blocks, threads, 0, s>>>(a);
   };
-  if (p.kind == tile::Plan::SMALL) go(ffn_dw_kernel<tile::Small>, dw_tiles<tile::Small>(a), tile::Small::THREADS);
-  else go(ffn_dw_kernel<tile::Wide>, dw_tiles<tile::Wide>(a), tile::Wide::THREADS);
-  if (a.split > 1) ffn_dw_sum_kernel<<<(int)((3LL * a.G * a.H * a.F / 8 + 255) / 256), 256, 0, s>>>(a);
+  using tile::Small, tile::Wide;
+  if (p.kind == tile::Plan::SMALL) go(ffn_grad_kernel<Small>, Small::BM, Small::BN, Small::THREADS, dw_tiles<Small>(a));
+  else go(ffn_grad_kernel<Wide>, Wide::BM, Wide::BN, Wide::THREADS, dw_tiles<Wide>(a));
+  if (a.dx && a.split > 1) ffn_sum_kernel<DX><<<(int)(((long long)a.T * a.H / 8 + 255) / 256), 256, 0, s>>>(a);
+  if (a.dw1 && a.dw_split > 1) ffn_dw_sum_kernel<<<(int)((3LL * a.G * a.H * a.F / 8 + 255) / 256), 256, 0, s>>>(a);
 }
 
 moe_status check_cfg(const moe_ffn_config* c) {
@@ -310,9 +368,10 @@ size_t part_bytes(const FfnArgs& a) {
 size_t ws_size(const moe_ffn_config* c, bool backward) {
   const FfnArgs a = args_of(c, nullptr);
   if (!backward) return 256 + plane(c) + std::max(part_bytes<UP>(a), part_bytes<DOWN>(a));
-  const int s = dw_plan(a).split;
-  const size_t dw = s > 1 ? 3 * sizeof(float) * (size_t)s * a.G * a.H * a.F : 0;
-  return 256 + 3 * plane(c) + std::max(dw, std::max(part_bytes<DH>(a), part_bytes<DX>(a)));
+  const GradPlan p = grad_plan(a);
+  const size_t grad = sizeof(float) * ((p.dx_split > 1 ? (size_t)p.dx_split * a.T * a.H : 0) +
+                                       (p.dw_split > 1 ? 3 * (size_t)p.dw_split * a.G * a.H * a.F : 0));
+  return 256 + 3 * plane(c) + std::max(part_bytes<DH>(a), grad);
 }
 
 moe_status check_ws(const moe_ffn_config* c, bool backward, const void* ws, size_t bytes) {
@@ -382,11 +441,9 @@ moe_status moe_ffn_backward(const moe_ffn_config* cfg, const uint16_t* dy, const
   a.dup = reinterpret_cast<uint16_t*>(at + 2 * plane(cfg));
   a.part = reinterpret_cast<float*>(at + 3 * plane(cfg));
   a.dx = dx, a.dw1 = dw1, a.dw3 = dw3, a.dw2 = dw2;
-  if (a.T > 0 && (dx || dw1)) {
-    launch<DH>(a, s);
-    if (dx) launch<DX>(a, s);
-  }
-  if (dw1) launch_dw(a, s);
+  if (a.T == 0) a.dx = nullptr;
+  if (a.T > 0 && (dx || dw1)) launch<DH>(a, s);
+  if (a.dx || dw1) launch_grad(a, s);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }

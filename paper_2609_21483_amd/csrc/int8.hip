@@ -170,7 +170,7 @@ __global__ __launch_bounds__(S::THREADS) void gemm_i8_kernel(I8Args a) {
   constexpr int COLS = GATED ? Tl::BN / 2 : Tl::BN;
   const int out = GATED ? a.N / 2 : a.N, nt = ceil_div(out, COLS), stages = ceil_div(a.K, 128);
   int m, n;
-  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
+  if (!tile::pick(blockIdx.x, list.total, nt * a.split, &m, &n)) return;
   const RowTile rt = list.at(m);
   const int part = n / nt, n0 = n % nt * COLS, rows = rt.end - rt.begin;
   const int k0 = stages * part / a.split * 128, k1 = min(stages * (part + 1) / a.split * 128, a.K);
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(NW * 64) void gemm_i8_few_kernel(I8Args a) {
   const RowTiles list(a.off, a.G, a.T, Fw::BM);
   const int out = GATED ? a.N / 2 : a.N, nt = ceil_div(out, Fw::COLS), steps = a.K / Fw::KE;
   int m, n;
-  if (!tile::pick(list.total, nt * a.split, &m, &n)) return;
+  if (!tile::pick(blockIdx.x, list.total, nt * a.split, &m, &n)) return;
   const RowTile rt = list.at(m);
   const int part = n / nt, n0 = n % nt * Fw::COLS;
   Fw::run(lds, rows_op<GATED>(a, rt, 0), weights_op<GATED>(a, rt, 0, n0), steps * part / a.split,

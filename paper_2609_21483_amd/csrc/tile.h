@@ -629,14 +629,14 @@ __device__ __forceinline__ void unpack8(u32x4_t w, float (&v)[8]) {
   }
 }
 
-// The tile of this workgroup among mt row tiles x nt column tiles: workgroup i
+// The tile of workgroup `block` among mt row tiles x nt column tiles: workgroup i
 // runs on XCD i % 8, and each XCD takes a run of consecutive tiles, ordered so
 // that 8 row tiles share each column tile's operand while it is in the XCD's
 // L2.  False: no tile (the grid is sized for the most row tiles there can be).
 constexpr int NEAR = 8;
-__device__ __forceinline__ bool pick(int mt, int nt, int* m, int* n) {
-  const int total = mt * nt, chunk = ceil_div(total, NXCD), t = (blockIdx.x % NXCD) * chunk + blockIdx.x / NXCD;
-  if ((int)(blockIdx.x / NXCD) >= chunk || t >= total) return false;
+__device__ __forceinline__ bool pick(int block, int mt, int nt, int* m, int* n) {
+  const int total = mt * nt, chunk = ceil_div(total, NXCD), t = block % NXCD * chunk + block / NXCD;
+  if (block / NXCD >= chunk || t >= total) return false;
   const int band = t / (NEAR * nt), first = band * NEAR, wide = min(NEAR, mt - first), in = t - band * NEAR * nt;
   *m = first + in % wide;
   *n = in / wide;
