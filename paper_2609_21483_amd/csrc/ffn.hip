@@ -280,14 +280,14 @@ struct GradPlan {
 template <typename S>
 void grad_times(const FfnArgs& a, tile::Plan::Kind kind, GradPlan* best, double* least) {
   const bool wide = kind == tile::Plan::WIDE;
-  const double cap = wide ? 256 : 512, busy = wide ? 2.0 : 1.25, alone = wide ? 1.85 : 0.85, over = wide ? 4 : 3;
+  const double cap = wide ? 256 : 512, busy = wide ? 2.0 : 1.25, alone = wide ? 1.85 : 1.0, over = wide ? 4 : 3;
   const double tx = tile::row_tiles(a.T, a.G, S::BM) * ceil_div(a.H, S::BN), tw = (double)a.G * dw_tiles<S>(a);
   const int sx = 2 * a.F / 64, sw = std::max(1, ceil_div(ceil_div(a.T, a.G), 64)), most = wide ? 1 : tile::MAX_SPLIT;
   for (int x = 1; x <= most && x <= sx; x *= 2)
     for (int w = 1; w <= most && w <= sw; w *= 2) {
       const int dx_stages = ceil_div(sx, x), dw_stages = ceil_div(sw, w);
       const double all = tx * x * (dx_stages * busy + over) + tw * w * (dw_stages * busy + over);
-      const double deepest = std::max(dx_stages, dw_stages) * alone + over;
+      const double deepest = std::max(dx_stages, dw_stages) * alone + 8;
       const double t = (tx * x + tw * w <= cap ? deepest : std::max(all / cap, deepest) + 0.35 * deepest) +
                        (x > 1 ? 6 + 8.0 * x * a.T * a.H / 6e6 : 0) + (w > 1 ? 6 + 24.0 * w * a.G * a.H * a.F / 6e6 : 0);
       if (t < *least) *least = t, *best = {kind, x, w};

@@ -562,21 +562,21 @@ constexpr int MAX_SPLIT = 16;
 
 // Small or Wide tiles, from how many there are of each: rounds of workgroups
 // (one Wide or two Small per CU) times the time of one.  Measured, us per
-// stage: Wide 1.85 to 2.2; Small 0.85 with one workgroup per CU and 1.2 to 1.4
-// with two.  So Wide tiles take 1.3 times less where they fill the chip, and
+// stage: Wide 1.85 to 2.2; Small 0.85 to 1.1 (and 8 at the ends) with one
+// workgroup per CU and 1.2 to 1.4 with two.  So Wide tiles take 1.3 times less where they fill the chip, and
 // Small ones win where Wide ones leave CUs idle: dh of 2000 rows, H = F = 4096,
 // 128 Wide tiles 123, 512 Small 89; of 4000 rows 147 : 179; int8, 6007 rows in
 // 16 groups, 2048 x 2816, 352 Wide tiles 71, 1210 Small 60.  A split costs a
 // launch (6 with its gap) and the sums' way out and back, `sum_bytes` per part
 // (6 TB/s): dx of 333 rows in 4 groups, H = 1024, F = 2816 (40 Small tiles, 88
-// stages), 80 : 52 : 33 : 25 in 1, 2, 4 and 8 parts; dh of 2000 rows above, 89
-// against 83 + 27 in two.
+// stages), 80 : 52 : 33 : 25 in 1, 2, 4 and 8 parts; dh of the same rows (88
+// tiles, 16 stages) 27 : 21; dh of 2000 rows above, 89 against 83 + 27 in two.
 inline Plan tile_plan(double wide, double small, int stages, double sum_bytes) {
   Plan best{Plan::WIDE, 1};
   double least = std::ceil(wide / 256) * (stages * 2.0 + 4);
   for (int s = 1; s <= MAX_SPLIT && s <= std::max(stages, 1); s *= 2) {
     const double w = small * s, rounds = w <= 512 ? 1 : w / 512 + 0.35;
-    const double t = rounds * (ceil_div(stages, s) * (w <= 256 ? 0.85 : 1.25) + 3) +
+    const double t = rounds * (w <= 256 ? ceil_div(stages, s) * 1.0 + 8 : ceil_div(stages, s) * 1.25 + 3) +
                      (s > 1 ? 6 + 2 * s * sum_bytes / 6e6 : 0);
     if (t < least) least = t, best = {Plan::SMALL, s};
   }
