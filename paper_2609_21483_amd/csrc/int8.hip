@@ -19,23 +19,18 @@ constexpr uint32_t BF16_INF = 0x7f80;
 __device__ __forceinline__ float scale_of(uint32_t amax) {
   return amax >= BF16_INF ? __builtin_nanf("") : bf16_to_f32((uint16_t)amax) / 127.0f;
 }
-// (a scale rounded down in the subnormal range can give a quotient above 127)
-__device__ __forceinline__ int quantize(uint16_t v, float scale) {
-  if (!(scale > 0.0f)) return 0;
-  return (int)fminf(fmaxf(rintf(bf16_to_f32(v) / scale), -127.0f), 127.0f);
-}
-
 // The quotient of a value by its row's scale, rounded to a whole number as the
 // IEEE quotient would be.  The value times the hardware reciprocal is within
 // 127 * 3 * 2^-24 < 3e-5 of it, so only where that lies within 1e-4 of a half
 // does the division itself decide (about 1 value in 5000).
 struct Quantizer {
   float scale, inv;
-  bool slow;
+  bool slow;  // (a subnormal reciprocal, or a scale whose quotients the bound does not hold for)
   __device__ __forceinline__ explicit Quantizer(float s) : scale(s), inv(__builtin_amdgcn_rcpf(s)), slow(s < 0x1p-100f) {}
   __device__ __forceinline__ int operator()(float v) const {
     float q = v * inv, r = rintf(q);
     if (slow || fabsf(q - r) > 0.4999f) r = rintf(v / scale);
+    // (a scale rounded down in the subnormal range can give a quotient above 127)
     return (int)fminf(fmaxf(r, -127.0f), 127.0f);
   }
 };
@@ -88,26 +83,89 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(int rows, int cols, 
   }
 }
 
-// a workgroup takes 64 channels of a group: the largest magnitudes, then the
-// values, transposed through LDS 64 rows of the depth at a time
-__global__ __launch_bounds__(256) void quantize_weights_kernel(int K, int N, int Nq, int first, const uint16_t* w,
-                                                               int8_t* wq, float* scale) {
-  __shared__ uint32_t red[4][64];
-  __shared__ int8_t tile[64][65];
-  const int g = blockIdx.y, n0 = blockIdx.x * 64, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const uint16_t* wg = w + (size_t)g * K * N + n0;
-  uint32_t m = 0;
-  for (int k = wave; k < K; k += 4) m = max(m, wg[(size_t)k * N + lane] & 0x7fffu);
-  red[wave][lane] = m;
+// Weights: 64 channels x 256 rows of the depth a workgroup, in three passes, the
+// largest magnitudes of the channels (their bits gathered where the scales go;
+// a maximum does not depend on the order), the values, transposed through LDS,
+// and the scales.  Reads the weights twice: TODO.
+constexpr int QW_N = 64, QW_K = 256;
+
+// what = 0: clears, 1: turns magnitudes into scales
+__global__ __launch_bounds__(256) void quantize_scales_kernel(int N, int Nq, int first, float* scale, int what) {
+  const int n = blockIdx.x * 256 + threadIdx.x;
+  if (n >= N) return;
+  float* p = scale + (size_t)blockIdx.y * Nq + first + n;
+  *p = what ? scale_of(__float_as_uint(*p)) : 0.0f;
+}
+
+__global__ __launch_bounds__(256) void quantize_max_kernel(int K, int N, int Nq, int first, const uint16_t* w, float* scale) {
+  __shared__ uint32_t red[4][QW_N];
+  const int k0 = blockIdx.x * QW_K, n0 = blockIdx.y * QW_N, g = blockIdx.z;
+  const int c = threadIdx.x % 8 * 8, r = threadIdx.x / 8;
+  const uint16_t* p = w + ((size_t)g * K + k0) * N + n0 + c;
+  u32x4_t v[QW_K / 32];
+#pragma unroll
+  for (int i = 0; i < QW_K / 32; ++i)
+    v[i] = k0 + r + i * 32 < K ? *reinterpret_cast<const u32x4_t*>(p + (size_t)(r + i * 32) * N) : u32x4_t{0, 0, 0, 0};
+  uint32_t m[8] = {};
+#pragma unroll
+  for (int i = 0; i < QW_K / 32; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[2 * j] = max(m[2 * j], v[i][j] & 0x7fffu);
+      m[2 * j + 1] = max(m[2 * j + 1], (v[i][j] >> 16) & 0x7fffu);
+    }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+#pragma unroll
+    for (int d = 8; d < 64; d <<= 1) m[j] = max(m[j], (uint32_t)__shfl_xor((int)m[j], d));
+    if (threadIdx.x % 64 < 8) red[threadIdx.x / 64][c + j] = m[j];
+  }
   __syncthreads();
-  m = max(max(red[0][lane], red[1][lane]), max(red[2][lane], red[3][lane]));
-  const float s = scale_of(m);
-  if (wave == 0) scale[(size_t)g * Nq + first + n0 + lane] = s;
-  for (int k0 = 0; k0 < K; k0 += 64) {
-    __syncthreads();
-    for (int k = wave; k < 64; k += 4) tile[lane][k] = (int8_t)quantize(wg[(size_t)(k0 + k) * N + lane], s);
-    __syncthreads();
-    for (int n = wave; n < 64; n += 4) wq[((size_t)g * Nq + first + n0 + n) * K + k0 + lane] = tile[n][lane];
+  if (threadIdx.x < QW_N) {
+    const int t = threadIdx.x;
+    atomicMax(reinterpret_cast<uint32_t*>(scale + (size_t)g * Nq + first + n0 + t),
+              max(max(red[0][t], red[1][t]), max(red[2][t], red[3][t])));
+  }
+}
+
+__global__ __launch_bounds__(256) void quantize_weights_kernel(int K, int N, int Nq, int first, const uint16_t* w,
+                                                               int8_t* wq, const float* scale) {
+  // rows of 65 words: a wavefront's 8 channel groups x 8 words fall on 64 banks
+  __shared__ uint32_t tile[QW_N][QW_K / 4 + 1];
+  const int k0 = blockIdx.x * QW_K, n0 = blockIdx.y * QW_N, g = blockIdx.z;
+  const int c = threadIdx.x % 8 * 8, r = threadIdx.x / 8;
+  const uint16_t* p = w + ((size_t)g * K + k0) * N + n0 + c;
+  const float* sc = scale + (size_t)g * Nq + first + n0 + c;
+  u32x4_t v[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int k = i * 128 + r * 4 + j;
+      v[i][j] = k0 + k < K ? *reinterpret_cast<const u32x4_t*>(p + (size_t)k * N) : u32x4_t{0, 0, 0, 0};
+    }
+#pragma unroll
+  for (int n = 0; n < 8; ++n) {
+    const float s = scale_of(__float_as_uint(sc[n]));
+    const bool zero = !(s > 0.0f);
+    const Quantizer quant(s);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t q = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        q |= (uint32_t)(quant(n % 2 ? bf16_hi(v[i][j][n / 2]) : bf16_lo(v[i][j][n / 2])) & 255) << (8 * j);
+      tile[c + n][i * 32 + r] = zero ? 0u : q;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < QW_N * QW_K / 16 / 256; ++i) {
+    const int piece = threadIdx.x + i * 256, n = piece / (QW_K / 16), k = piece % (QW_K / 16);
+    if (k0 + k * 16 < K) {
+      const uint32_t* t = &tile[n][k * 4];
+      *reinterpret_cast<u32x4_t*>(wq + ((size_t)g * Nq + first + n0 + n) * K + k0 + k * 16) = u32x4_t{t[0], t[1], t[2], t[3]};
+    }
   }
 }
 
@@ -309,8 +367,12 @@ moe_status moe_quantize_weights_i8(int32_t n_groups, int32_t depth, int32_t chan
   if (!w || !wq || !scale) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
   if (!aligned16(w) || !aligned16(wq) || !aligned16(scale))
     return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
-  quantize_weights_kernel<<<dim3(channels / 64, n_groups), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(
-      depth, channels, q_channels, first, w, wq, scale);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const dim3 all(ceil_div(depth, QW_K), channels / QW_N, n_groups), each(ceil_div(channels, 256), n_groups);
+  quantize_scales_kernel<<<each, 256, 0, s>>>(channels, q_channels, first, scale, 0);
+  quantize_max_kernel<<<all, 256, 0, s>>>(depth, channels, q_channels, first, w, scale);
+  quantize_weights_kernel<<<all, 256, 0, s>>>(depth, channels, q_channels, first, w, wq, scale);
+  quantize_scales_kernel<<<each, 256, 0, s>>>(channels, q_channels, first, scale, 1);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }
