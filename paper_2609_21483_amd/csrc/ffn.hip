@@ -401,6 +401,7 @@ moe_status moe_ffn_forward(const moe_ffn_config* cfg, const uint16_t* x, const i
   if (cfg->rows == 0) return MOE_OK;
   if (!x || !w1 || !w3 || !w2 || !y) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
   if (!group_off && cfg->n_groups > 1) return fail(MOE_ERR_INVALID_ARG, "group_off is NULL with more than one group");
+  if (reinterpret_cast<uintptr_t>(group_off) % 4) return fail(MOE_ERR_INVALID_ARG, "group_off is not aligned to its values");
   if (!gate != !up) return fail(MOE_ERR_INVALID_ARG, "gate and up are kept both or neither");
   for (const void* p : {(const void*)x, (const void*)w1, (const void*)w3, (const void*)w2, (const void*)gate,
                         (const void*)up, (const void*)y})
@@ -426,6 +427,7 @@ moe_status moe_ffn_backward(const moe_ffn_config* cfg, const uint16_t* dy, const
   // (without rows there is no dx, but the weights' gradients are written: zeros)
   if (cfg->rows > 0 && (!dy || !x || !w1 || !w3 || !w2 || !gate || !up)) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
   if (!group_off && cfg->n_groups > 1) return fail(MOE_ERR_INVALID_ARG, "group_off is NULL with more than one group");
+  if (reinterpret_cast<uintptr_t>(group_off) % 4) return fail(MOE_ERR_INVALID_ARG, "group_off is not aligned to its values");
   if (!dw1 != !dw3 || !dw1 != !dw2) return fail(MOE_ERR_INVALID_ARG, "dw1, dw3 and dw2 are all wanted or none");
   for (const void* p : {(const void*)dy, (const void*)x, (const void*)w1, (const void*)w3, (const void*)w2,
                         (const void*)gate, (const void*)up, (const void*)dx, (const void*)dw1, (const void*)dw3,

@@ -392,6 +392,7 @@ moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const fl
   if (cfg->rows == 0) return MOE_OK;
   if (!xq || !x_scale || !wq || !w_scale || !y) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
   if (!group_off && cfg->n_groups > 1) return fail(MOE_ERR_INVALID_ARG, "group_off is NULL with more than one group");
+  if (reinterpret_cast<uintptr_t>(group_off) % 4) return fail(MOE_ERR_INVALID_ARG, "group_off is not aligned to its values");
   for (const void* p : {(const void*)xq, (const void*)x_scale, (const void*)wq, (const void*)w_scale, (const void*)y})
     if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
   if (!ws || ws_bytes < ws_size(cfg))

@@ -154,3 +154,10 @@ def test_oracle_derivative_of_the_activation(name):
     t = torch.from_numpy(v)
     ref = torch.nn.functional.silu(t) if name == "silu" else torch.nn.functional.gelu(t, approximate="tanh")
     assert np.max(np.abs(ref.numpy() - a)) <= 1e-12
+
+
+@pytest.mark.parametrize("call", [lambda: ffn("moe_ffn_forward", (8, 64, 64, 2, 1), off=AT + 2),
+                                  lambda: ffn("moe_ffn_backward", (8, 64, 64, 2, 1), off=AT + 1),
+                                  lambda: gemm((8, 64, 64, 2, 0), off=AT + 2)])
+def test_offsets_off_their_alignment_are_refused(call):
+    assert call() == B.MOE_ERR_INVALID_ARG
