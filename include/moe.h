@@ -408,11 +408,13 @@ moe_status moe_tile_geometry(const moe_handle* h, int32_t* bm, int32_t* nt0, int
  *
  * These calls need no handle.  They run on the current device, whose memory
  * every argument is; pointers start on 16-byte boundaries (group_off on its
- * values', the workspace on 256 bytes), else MOE_ERR_INVALID_ARG.  A workspace holds scratch only: it
- * needs no initialisation, keeps nothing from one call for the next, and may
- * serve any calls that run one after the other, but not two that overlap.  No
- * call allocates, waits, or adds in an order that changes from run to run, and
- * all can be captured into a graph.  Outputs must not overlap inputs.
+ * values', the workspace on 256 bytes), else MOE_ERR_INVALID_ARG.  A workspace
+ * holds scratch only: it needs no initialisation, keeps nothing from one call
+ * for the next, and may serve any calls that run one after the other, but not
+ * two that overlap.  No call allocates, waits, or adds in an order that changes
+ * from run to run, and all can be captured into a graph.  Outputs must not
+ * overlap inputs or each other.  A result depends on its own row (and its
+ * group's weights) alone, a weight's gradient on its own group's rows.
  */
 typedef enum {
   MOE_ACT_NONE = 0,

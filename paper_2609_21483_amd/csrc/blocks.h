@@ -14,6 +14,7 @@ namespace moe {
 
 struct RowTile {
   int group, begin, end;  // the tile's rows: [begin, end) of its group
+  int tiles;              // row tiles of the group
 };
 
 __device__ __forceinline__ int clamp_off(int v, int T) { return v < 0 ? 0 : (v > T ? T : v); }
@@ -75,14 +76,15 @@ struct RowTiles {
 
   // tile t < total
   __device__ __forceinline__ RowTile at(int t) const {
-    if (!off) return {0, t * bm, min((t + 1) * bm, T)};
-    int group = 0, begin = 0, end = 0, left = t - (incl - n);
+    if (!off) return {0, t * bm, min((t + 1) * bm, T), total};
+    int group = 0, begin = 0, end = 0, tiles = 0, left = t - (incl - n);
     const bool mine = left >= 0 && left < n;
     if (mine)
       for (int g = g0, a = first; g < g1; ++g) {
         const int e = max(a, clamp_off(off[g + 1], T)), k = ceil_div(e - a, bm);
         if (left >= 0 && left < k) {
           group = g;
+          tiles = k;
           begin = a + left * bm;
           end = min(begin + bm, e);
         }
@@ -91,7 +93,7 @@ struct RowTiles {
       }
     const int src = __ffsll((unsigned long long)__ballot(mine)) - 1;
     return {__builtin_amdgcn_readlane(group, src), __builtin_amdgcn_readlane(begin, src),
-            __builtin_amdgcn_readlane(end, src)};
+            __builtin_amdgcn_readlane(end, src), __builtin_amdgcn_readlane(tiles, src)};
   }
 };
 

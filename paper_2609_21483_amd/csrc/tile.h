@@ -28,6 +28,14 @@
 // b % WM.  B is the first operand of the instruction, so that a lane's
 // accumulators are 4 consecutive columns of one row: column 8 (r / 4) + 4 (l /
 // 32) + r % 4 of row l % 32 in register r.
+//
+// What bounds Wide tiles (x W of 8192 x 4096 x 28672, 1640 us): the loads alone
+// take 1340 (13 TB/s over all CUs, 80% of it L2 hits), the LDS reads and
+// products alone 1475, at a clock that falls to 1.65 GHz (int8: 2.0).  A ring of
+// five 64-byte steps, three to four ahead, took 5 to 12% longer (half lines of
+// the k-contiguous operand, twice the barriers); four waves of 128 x 128 1 to 8%
+// longer; uniform branches around a partly filled tile's empty row blocks 8%
+// longer on full ones and no shorter on ragged groups.
 #pragma once
 
 #include <algorithm>
@@ -200,7 +208,8 @@ struct Tile {
   // The products of one slice, with next(u) for u in [0, FRAGS), the loads of
   // the next slice's fragments, and dma(i) for i in [0, INSTR) between them,
   // in this order: left to itself the compiler loads each fragment right
-  // before the product that takes it, and every product waits for LDS.
+  // before the product that takes it, and every product waits for LDS (4 to 9%
+  // of the time of large products).
   template <typename Next, typename Dma>
   static __device__ __forceinline__ void multiply(Acc& acc, const Frag (&a)[MB], const Frag (&b)[NB], Next&& next, Dma&& dma) {
     constexpr int P = MB * NB;
@@ -432,9 +441,11 @@ struct Few {
 
   // fn(row, col, v) for every 8 consecutive columns of each row, v[8..15] the
   // second matrix's where gated: the sums over steps [s0, s1) of the depth.
-  // Rows of A past A.valid are read as the last and not handed out.
+  // Rows of A past A.valid are read as the last and not handed out.  once: no
+  // other row tile reads these weights.
   template <typename Fn>
-  static __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int s0, int s1, Fn&& fn) {
+  static __device__ __forceinline__ void run(char* lds, const Operand& A, const Operand& B, int s0, int s1, bool once,
+                                             Fn&& fn) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     uint32_t ow[WI], ox[2];
 #pragma unroll
@@ -463,9 +474,10 @@ struct Few {
 #pragma unroll
       for (int i = 0; i < WI; ++i) {
         const char* w = (GATED && i >= 4 ? pb2 : pb) + s * sb;
-        // transposed weights come in whole lines, read once (8 to 10% of the
-        // time); a step of k-contiguous ones is half of each line
-        if constexpr (BT) dma16_once(w, ow[i], l + i * 1024);
+        // transposed weights come in whole lines: past the L2 where no other
+        // tile reads them (8 to 10% of the time; 50% more where two do).  A step
+        // of k-contiguous ones is half of each line, which the next one reads
+        if (BT && once) dma16_once(w, ow[i], l + i * 1024);
         else dma16(w, ow[i], l + i * 1024);
       }
 #pragma unroll
@@ -571,35 +583,49 @@ constexpr int MAX_SPLIT = 16;
 // (6 TB/s): dx of 333 rows in 4 groups, H = 1024, F = 2816 (40 Small tiles, 88
 // stages), 80 : 52 : 33 : 25 in 1, 2, 4 and 8 parts; dh of the same rows (88
 // tiles, 16 stages) 27 : 21; dh of 2000 rows above, 89 against 83 + 27 in two.
-inline Plan tile_plan(double wide, double small, int stages, double sum_bytes) {
-  Plan best{Plan::WIDE, 1};
-  double least = std::ceil(wide / 256) * (stages * 2.0 + 4);
+struct Timed {
+  Plan plan;
+  double us;
+};
+inline Timed tile_plan(double wide, double small, int stages, double sum_bytes, double weight_bytes) {
+  // the weights once (1 row, the down projection of F = 14336 in 16 parts: 10 us
+  // longer than tiles of few rows where nothing is left in the caches)
+  const double stream = weight_bytes / 3.8e6;
+  Timed best{{Plan::WIDE, 1}, std::max(std::ceil(wide / 256) * (stages * 2.0 + 4), stream)};
   for (int s = 1; s <= MAX_SPLIT && s <= std::max(stages, 1); s *= 2) {
     const double w = small * s, rounds = w <= 512 ? 1 : w / 512 + 0.35;
-    const double t = rounds * (w <= 256 ? ceil_div(stages, s) * 1.0 + 8 : ceil_div(stages, s) * 1.25 + 3) +
+    const double t = std::max(rounds * (w <= 256 ? ceil_div(stages, s) * 1.0 + 8 : ceil_div(stages, s) * 1.25 + 3), stream) +
                      (s > 1 ? 6 + 2 * s * sum_bytes / 6e6 : 0);
-    if (t < least) least = t, best = {Plan::SMALL, s};
+    if (t < best.us) best = {{Plan::SMALL, s}, t};
   }
   return best;
 }
 
-// Tiles of few rows where a group has up to 32 on average, or where all of
-// them run at once (256 workgroups): beyond, every further row tile streams
-// the weights again.  Few rows against Small, us: H = 4096, F = 14336, up and
-// down projection, 32 rows 52 + 50 : 57 + 56, 64 rows 77 + 46 : 60 + 57; H =
-// 2048, F = 1408, 256 rows 14 + 8 : 17 + 17; 16 groups of 32 rows on average
-// 43 + 27 : 46 + 27, of 64 rows 60 + 37 : 49 + 34.
+// Tiles of few rows: a wave's steps (0.7 to 1.2 us: a load's latency over the
+// slots) behind 5 of ends, or the weights' stream where that is longer, once
+// from memory (5 TB/s) and for further row tiles mostly out of the caches (9).
+// Few rows against Small, us: H = 4096, F = 14336, up and down projection, 32
+// rows 52 + 50 : 57 + 56, 64 rows 77 + 46 : 60 + 57; H = 2048, F = 1408, 256 rows
+// 14 + 8 : 17 + 17; 16 groups of 32 rows on average 43 + 27 : 46 + 27, of 64 rows
+// 60 + 37 : 49 + 34.
 // Eight waves share the depth where one workgroup per CU holds all tiles (the
-// most there can be: 264 of 8 waves take two rounds), else four.  A step is
-// 0.5 us, and a part's sum costs some 6 us more, so the depth is split while a
-// wave has more than 24 steps: 1 row, H = 4096, down projection of F = 14336
-// (64 tiles, 448 steps) 60, 39 in two parts, 31 in four.
-inline bool few_rows(int T, int G, double tiles) { return T <= 32LL * G || tiles <= 256; }
-inline Plan few_plan(long long most, int steps) {
-  const auto waves = [&](int s) { return most * s <= 256 ? 8 : 4; };
-  int s = 1;
-  while (s < MAX_SPLIT && most * s * 2 <= 512 && steps / (s * waves(s)) > 24) s *= 2;
-  return {waves(s) == 8 ? Plan::FEW8 : Plan::FEW4, s};
+// most there can be: 264 of 8 waves take two rounds), else four.  Parts cost 6
+// (a launch with its gap) and their sums' way out and back, `sum_bytes` each: 1
+// row, H = 4096, down projection of F = 14336 (64 tiles, 448 steps) 60, 39 in two
+// parts, 31 in four; 2 rows, H = 3008, F = 192 (3 gated tiles, 94 steps) 20, 13 in
+// four.
+inline Timed few_plan(long long most, double tiles, int steps, double sum_bytes, double weight_bytes,
+                      double streamed_bytes) {
+  Timed best{{Plan::FEW4, 1}, 1e30};
+  for (int s = 1; s <= MAX_SPLIT && (s == 1 || (most * s <= 512 && s * 4 <= steps)); s *= 2) {
+    const int waves = most * s <= 256 ? 8 : 4;
+    const double rounds = std::ceil(tiles * s / (waves == 8 ? 256 : 512));
+    const double stream = weight_bytes / 5e6 + std::max(0.0, streamed_bytes - weight_bytes) / 9e6;
+    const double t = 5 + std::max(rounds * ceil_div(steps, s * waves), stream) +
+                     (s > 1 ? 6 + 2 * s * sum_bytes / 5e6 : 0);
+    if (t < best.us) best = {{waves == 8 ? Plan::FEW8 : Plan::FEW4, s}, t};
+  }
+  return best;
 }
 
 // Row tiles of T rows in G groups to expect: the last of a group is half full,
@@ -612,10 +638,16 @@ inline double row_tiles(int T, int G, int bm) {
 // The plan of a product of T rows in G groups: `cols` columns of the output
 // from `per` (2 where gated) columns of weights each, a depth of `stages`.
 inline Plan plan_of(int T, int G, int cols, int per, int stages, bool can_be_few) {
-  if (can_be_few && few_rows(T, G, row_tiles(T, G, 32) * ceil_div(cols, 64)))
-    return few_plan((long long)max_row_tiles(T, G, 32) * ceil_div(cols, 64), stages * 2);
-  return tile_plan(row_tiles(T, G, Wide::BM) * ceil_div(cols * per, Wide::BN),
-                   row_tiles(T, G, Small::BM) * ceil_div(cols * per, Small::BN), stages, 4.0 * T * cols * per);
+  const double column = (double)DEPTH * stages * per, groups = G == 1 ? 1 : G * (1 - std::exp(-(double)T / G));
+  const double weights = groups * cols * column, sums = 4.0 * T * cols * per;
+  const Timed t = tile_plan(row_tiles(T, G, Wide::BM) * ceil_div(cols * per, Wide::BN),
+                            row_tiles(T, G, Small::BM) * ceil_div(cols * per, Small::BN), stages, sums, weights);
+  if (!can_be_few) return t.plan;
+  const int nt = ceil_div(cols, 64);
+  const double few = row_tiles(T, G, 32);
+  const Timed f = few_plan((long long)max_row_tiles(T, G, 32) * nt, few * nt, stages * 2, sums, weights,
+                           few * cols * column);
+  return f.us <= t.us ? f.plan : t.plan;
 }
 
 __device__ __forceinline__ u32x4_t pack8(const float (&v)[8]) {

@@ -1,0 +1,100 @@
+"""GPU tests of the products over row groups at sizes that take every kind of tile (few rows by 4 and 8 waves, 128
+and 256 wide) and every split of the depth, in each direction; and of calls that run at the same time."""
+import numpy as np
+import pytest
+import torch
+
+from tests import blocks as K
+from tests.test_gpu_ffn import B, Block, verify  # noqa: F401  (B is the fixture)
+from tests.test_gpu_int8 import Gemm, rows_bf16
+
+pytestmark = pytest.mark.gpu
+
+
+def sums(B, b, backward):
+    """Bytes of partial sums in a block's workspace: none where no product is split."""
+    planes = (3 if backward else 1) * ((b.T * b.F * 2 + 255) // 256 * 256)
+    return B.moe_ffn_workspace_size(b.cfg, backward) - planes - 256
+
+
+# whole 256-row tiles fill the chip: one and more stages, both widths, rows that end inside a tile
+@pytest.mark.parametrize("T,H,F,G,off", [(8192, 64, 1024, 1, None), (8192, 1024, 64, 1, None), (8190, 192, 1024, 1, None),
+                                         (8190, 1024, 320, 1, None), (9000, 256, 960, 3, [5, 4100, 4101, 8999])])
+def test_large_tiles(B, T, H, F, G, off):
+    verify(Block(T, H, F, G, off, "silu", seed=21).cuda(B))
+
+
+# 128-row tiles, the depth of each product in several parts
+@pytest.mark.parametrize("T,H,F", [(300, 2048, 4096), (290, 4096, 2112)])
+def test_small_tiles_in_parts(B, T, H, F):
+    b = Block(T, H, F, 1, None, "gelu", seed=22).cuda(B)
+    assert sums(B, b, False) > 0 and sums(B, b, True) > 0
+    verify(b)
+
+
+# few rows, the depth of the second or of the first product in several parts
+@pytest.mark.parametrize("T,H,F,G,off", [(5, 64, 8192, 1, None), (5, 8256, 64, 1, None), (33, 128, 7168, 2, [0, 1, 32])])
+def test_few_rows_in_parts(B, T, H, F, G, off):
+    b = Block(T, H, F, G, off, "silu", seed=23).cuda(B)
+    assert sums(B, b, False) > 0
+    verify(b)
+
+
+# weights' gradients of few tiles over many rows: the rows in several parts, of groups that differ in depth
+@pytest.mark.parametrize("T,off", [(3000, [0, 3000]), (3001, [0, 1, 2987]), (2500, [0, 0, 2490, 2491])])
+def test_weight_gradients_in_parts(B, T, off):
+    b = Block(T, 64, 64, len(off) - 1, off, "silu", seed=24).cuda(B)
+    assert sums(B, b, True) > 0
+    verify(b)
+
+
+@pytest.mark.parametrize("T,D,N,G,off,act", [(8192, 128, 2048, 1, None, "silu"), (8190, 192, 1032, 1, None, "none"),
+                                             (9000, 448, 1920, 3, [5, 4100, 4101, 8999], "gelu"),
+                                             (300, 4160, 272, 1, None, "silu"), (5, 28736, 144, 1, None, "silu"),
+                                             (40, 16384, 200, 2, [1, 3, 39], "none")])
+def test_products_of_every_plan(B, T, D, N, G, off, act):
+    Gemm(B, T, D, N, G, off, act, seed=25).verify()
+
+
+def test_calls_at_the_same_time(B):
+    """Blocks on four streams, each with its own workspace, against the same ones run alone."""
+    shapes = [(700, 256, 320, 3, [0, 300, 301, 700]), (5, 64, 8192, 1, None), (2048, 128, 512, 2, [0, 2000, 2048]),
+              (3000, 64, 64, 1, None)]
+    blocks = [Block(*s, "silu", seed=26 + i).cuda(B) for i, s in enumerate(shapes)]
+    alone = []
+    for b in blocks:
+        (y, gate, up), _ = b.forward()
+        alone.append((y, gate, up, b.backward(gate, up)[0]))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for _ in range(3):
+        runs = []
+        for b, s in zip(blocks, streams):
+            with torch.cuda.stream(s):
+                fwd, _ = b.forward(stream=s)
+                runs.append((*fwd, b.backward(fwd[1], fwd[2], stream=s)[0]))
+        torch.cuda.synchronize()
+        for a, r in zip(alone, runs):
+            for x, y in zip(a[:3], r[:3]):
+                assert torch.equal(x.view(torch.int16), y.view(torch.int16))
+            for n in a[3]:
+                assert torch.equal(a[3][n].view(torch.int16), r[3][n].view(torch.int16)), n
+
+
+def test_weight_quantiser_replays(B):
+    G, D, N = 3, 320, 192
+    w = torch.empty(G, D, N, dtype=torch.bfloat16, device="cuda")
+    q, s = torch.empty(G, N, D, dtype=torch.int8, device="cuda"), torch.empty(G, N, device="cuda")
+    w.copy_(rows_bf16(G * D, N, 1).view(G, D, N))
+    B.moe_quantize_weights_i8(G, D, N, N, 0, w, q, s)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.moe_quantize_weights_i8(G, D, N, N, 0, w, q, s)
+    for turn in range(4):
+        x = rows_bf16(G * D, N, turn).view(G, D, N) * 2.0 ** -turn
+        w.copy_(x)
+        g.replay()
+        torch.cuda.synchronize()
+        eq, es = K.quantize_rows(x.float().transpose(1, 2).numpy())
+        assert np.array_equal(q.cpu().numpy(), eq) and np.array_equal(s.cpu().numpy(), es), turn
