@@ -58,7 +58,6 @@ using gemm::wait_vm;
 typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef int i32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((__vector_size__(4 * sizeof(short))));
-typedef short s16x8_t __attribute__((__vector_size__(8 * sizeof(short))));
 
 constexpr int DEPTH = 128;  // bytes of the depth per stage
 
@@ -97,11 +96,6 @@ struct Tile {
   using Acc1 = std::conditional_t<I8, i32x16_t, f32x16_t>;
   typedef Acc1 Acc[MB][NB];
   using Frag = std::conditional_t<I8, i32x4_t, bf16x8_t>;
-
-  template <bool TR, int ROWS, int N>
-  struct Offs {
-    uint32_t o[N];
-  };
 
   // Byte offsets of a wave's DMA lanes from the operand's base; `last` the
   // valid depth rows of the stage (transposed operands; 64 except in the end)
@@ -416,12 +410,11 @@ __device__ __forceinline__ void dma16_once(const char* base, uint32_t off, uint3
 
 // ---------------------------------------------------------------------------
 // Few rows: up to 32 rows x 64 columns (gated: 64 of each matrix), whose time
-// is that of streaming the weights.  The four or
-// eight waves share the columns and take
-// the steps of the depth (64 bytes: 32 bf16 or 64 int8 values) in turn, each
-// with slots of LDS of its own, so the loop has no barrier: a wave waits for
-// its oldest slot, multiplies it and loads a later step into it.  The waves'
-// sums are added in a fixed order at the end.
+// is that of streaming the weights.  The four or eight waves share the columns
+// and take the steps of the depth (64 bytes: 32 bf16 or 64 int8 values) in turn,
+// each with slots of LDS of its own, so the loop has no barrier: a wave waits
+// for its oldest slot, multiplies it and loads a later step into it.  The
+// waves' sums are added in a fixed order at the end.
 // LDS images of a slot: weights, k-contiguous as rows of 64 bytes, granule c
 // at c ^ (r / 4) % 4, or transposed as 32 depth rows of 64 columns per matrix
 // (a panel of PW = 64, as above); then the 32 rows of A, k-contiguous.
@@ -575,10 +568,10 @@ constexpr int MAX_SPLIT = 16;
 // Small or Wide tiles, from how many there are of each: rounds of workgroups
 // (one Wide or two Small per CU) times the time of one.  Measured, us per
 // stage: Wide 1.85 to 2.2; Small 0.85 to 1.1 (and 8 at the ends) with one
-// workgroup per CU and 1.2 to 1.4 with two.  So Wide tiles take 1.3 times less where they fill the chip, and
-// Small ones win where Wide ones leave CUs idle: dh of 2000 rows, H = F = 4096,
-// 128 Wide tiles 123, 512 Small 89; of 4000 rows 147 : 179; int8, 6007 rows in
-// 16 groups, 2048 x 2816, 352 Wide tiles 71, 1210 Small 60.  A split costs a
+// workgroup per CU and 1.2 to 1.4 with two.  So Wide tiles take 1.3 times less
+// where they fill the chip, and Small ones win where Wide ones leave CUs idle:
+// dh of 2000 rows, H = F = 4096, 128 Wide tiles 123, 512 Small 89; of 4000 rows
+// 147 : 179; int8, 6007 rows in 16 groups, 2048 x 2816, 352 Wide tiles 71, 1210 Small 60.  A split costs a
 // launch (6 with its gap) and the sums' way out and back, `sum_bytes` per part
 // (6 TB/s): dx of 333 rows in 4 groups, H = 1024, F = 2816 (40 Small tiles, 88
 // stages), 80 : 52 : 33 : 25 in 1, 2, 4 and 8 parts; dh of the same rows (88
