@@ -181,17 +181,33 @@ struct I8Args {
   int split;
 };
 
+// A row's scale, times which a sum and its channel's scale are multiplied:
+// mantissas (0.5 to 1) first and the powers of two in one step at the end, since
+// the product of the scales, or of a sum and one of them, may leave fp32 where
+// the result does not (1e25 * 1e14 * 0 is 0).  The same bits as v * (x * w)
+// where nothing of that is subnormal or infinite.
+struct RowScale {
+  float mant;
+  int exp;
+  __device__ __forceinline__ explicit RowScale(float x)
+      : mant(__builtin_amdgcn_frexp_mantf(x)), exp(__builtin_amdgcn_frexp_expf(x)) {}
+  __device__ __forceinline__ float times(uint32_t v, float w) const {
+    return __builtin_amdgcn_ldexpf((float)(int)v * (mant * __builtin_amdgcn_frexp_mantf(w)),
+                                   exp + __builtin_amdgcn_frexp_expf(w));
+  }
+};
+
 // 8 columns of y from their sums (gated: v[8..15] the ups'): n the column of y
 template <bool GATED>
 __device__ __forceinline__ void finish(const I8Args& a, size_t row, int group, int n, const uint32_t* v) {
   const int out = GATED ? a.N / 2 : a.N;
-  const float sx = a.sx[row];
+  const RowScale sx(a.sx[row]);
   const float* sw = a.sw + (size_t)group * a.N + n;
   float y[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    y[i] = (float)(int)v[i] * (sx * sw[i]);
-    if constexpr (GATED) y[i] = act_of(y[i], a.act) * ((float)(int)v[8 + i] * (sx * sw[out + i]));
+    y[i] = sx.times(v[i], sw[i]);
+    if constexpr (GATED) y[i] = act_of(y[i], a.act) * sx.times(v[8 + i], sw[out + i]);
   }
   *reinterpret_cast<u32x4_t*>(a.y + row * out + n) = tile::pack8(y);
 }

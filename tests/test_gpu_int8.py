@@ -209,3 +209,46 @@ def test_binding_refuses_what_does_not_fit(B):
         B.moe_quantize_rows_i8(70, 128, torch.empty(70, 128, dtype=torch.bfloat16, device="cuda"), ok[0], ok[1][:69])
     with pytest.raises(ValueError):
         B.moe_quantize_weights_i8(2, 128, 64, 64, 0, torch.empty(2, 128, 64, device="cuda"), ok[2], ok[3])
+
+
+@pytest.mark.parametrize("act", ["none", "silu"])
+@pytest.mark.parametrize("T,D,N", [(5, 192, 528), (130, 192, 528), (5, 28736, 144), (300, 4160, 272)])
+def test_scales_whose_product_leaves_fp32(B, T, D, N, act):
+    """sum * x_scale * w_scale where the scales' product, or the sum's with either, is below or beyond fp32 but the
+    result is not; and sums of 0, which stay 0 whatever finite scales they meet."""
+    g = Gemm(B, T, D, N, 1, None, act, seed=10)
+    rng = np.random.default_rng(11)
+    g.xq[1] = 0
+    if act == "none":
+        # exponents of the whole range on either side
+        g.sx = np.ldexp(rng.uniform(0.5, 1, T), rng.integers(-140, 122, T)).astype(np.float32)
+        g.sw = np.ldexp(rng.uniform(0.5, 1, (1, N)), rng.integers(-140, 122, (1, N))).astype(np.float32)
+        g.sx[1] = 1e30
+        g.sw[0, 7] = 1e30
+    else:
+        # gates of some hundreds either way, ups whose scales' product has 6 bits left in fp32
+        g.sx = (2.0 ** -90 * rng.uniform(0.5, 1, T)).astype(np.float32)
+        g.sw = (2.0 ** 87 / D ** 0.5 * rng.uniform(0.5, 1, (1, N))).astype(np.float32)
+        g.sw[:, N // 2:] = 2.0 ** -52 * rng.uniform(0.5, 1, (1, N // 2))
+    g.d = [torch.from_numpy(v).cuda() for v in (g.xq, g.sx, g.wq, g.sw)]
+    y, _ = g.run()
+    got = y.float().cpu().numpy().astype(np.float64)
+    v = (g.xq.astype(np.float64) @ g.wq[0].astype(np.float64).T) * g.sx[:, None].astype(np.float64) * g.sw[0].astype(np.float64)
+    if act == "none":
+        ref, rel = v, 3 * K.F32
+    else:
+        a, _, ea, _ = K.act(v[:, :N // 2], act)
+        ref = a * v[:, N // 2:]
+        # the two scaled sums are off by 3 2^-24 each (the activation's slope times its argument over its value is at
+        # most 1 + |v|), the activation and the last product by their own roundings
+        rel = ea / np.maximum(np.abs(a), 1e-300) + (3 * (1 + np.abs(v[:, :N // 2])) + 4) * K.F32
+        assert (np.abs(ref) > 2.0 ** -122).mean() > 0.2
+    assert (got[1] == 0).all()
+    # half a step of a subnormal bf16 result is 2^-134, of the fp32 value before it 2^-150
+    bound = K.BF * np.abs(ref) + (1 + K.BF) * rel * np.abs(ref) + 2.0 ** -134 + 2.0 ** -149
+    inside = np.abs(ref) + bound < 3.38e38
+    assert inside.mean() > 0.5 and np.isfinite(got[inside]).all()
+    far = np.abs(got - ref)[inside] - bound[inside]
+    assert far.max() <= 0, (int((far > 0).sum()), far.size)
+    over = np.abs(ref) > 3.41e38
+    assert (got[over] == np.sign(ref[over]) * np.inf).all()
