@@ -161,3 +161,26 @@ def test_oracle_derivative_of_the_activation(name):
                                   lambda: gemm((8, 64, 64, 2, 0), off=AT + 2)])
 def test_offsets_off_their_alignment_are_refused(call):
     assert call() == B.MOE_ERR_INVALID_ARG
+
+
+BF = torch.bfloat16
+G, H, F, T = 2, 64, 192, 6
+# (weights [G][H][F], rows [T][H]; a CPU tensor's device is -1)
+WHOLE_ROWS = [((G, H, F), F, G * H * F), ((G * H, F), F, G * H * F), ((1, G, H, F), F, G * H * F), ((H, F), F, H * F),
+              ((G * H * F,), F, G * H * F), ((2, 3, H), H, T * H), ((T, 4, 16), H, T * H), ((1, H), H, H), ((H,), H, H),
+              ((0, H), H, 0), ((0,), H, 0), ((G, H, F, 1), F, G * H * F)]
+OTHER_ROWS = [((G, F, H), F, G * H * F), ((F, H), F, H * F), ((H, T), H, T * H), ((T * 16, 4), H, T * H),
+              ((T // 2, 2 * H), H, T * H)]
+
+
+@pytest.mark.parametrize("shape,width,n", WHOLE_ROWS)
+def test_binding_takes_tensors_whose_rows_are_whole(shape, width, n):
+    t = torch.zeros(shape, dtype=BF)
+    assert B._arg("w", t, BF, n, -1, width) == t.data_ptr()
+
+
+@pytest.mark.parametrize("shape,width,n", OTHER_ROWS)
+def test_binding_refuses_tensors_of_other_rows(shape, width, n):
+    """As many elements, but in rows of another length: the weights of torch's Linear, transposed rows."""
+    with pytest.raises(ValueError, match=f"rows of {width}"):
+        B._arg("w", torch.zeros(shape, dtype=BF), BF, n, -1, width)

@@ -396,3 +396,19 @@ def test_layer_experts_in_training_then_served_in_8_bits(B):
         bound = eh @ np.abs(W2) + (habs + eh).sum(1, keepdims=True) * 0.5 * s2[i].cpu().numpy()[None] + 2 * K.BF * np.abs(ref[rows])
         K.check("block in 8 bits", f64(y)[rows], ref[rows], 1.01 * bound)
     B.moe_destroy(h)
+
+
+def test_weights_of_the_other_layout_are_refused(B):
+    """[G][F][H], torch's Linear, holds as many values as [G][H][F]; x and y in any split of their rows are taken."""
+    b = Block(70, 64, 128, 2, [0, 30, 70], "silu", seed=14).cuda(B)
+    (y, gate, up), _ = b.forward()
+    ok = dict(b.d)
+    for n in ("w1", "w3", "w2"):
+        b.d = dict(ok, **{n: ok[n].transpose(1, 2).contiguous()})
+        with pytest.raises(ValueError, match="rows of"):
+            b.forward()
+        with pytest.raises(ValueError, match="rows of"):
+            b.backward(gate, up)
+    b.d = dict(ok, x=ok["x"].view(2, 35, 4, 16), w1=ok["w1"].flatten(), w3=ok["w3"].view(128, 128))
+    (y2, _, _), _ = b.forward()
+    assert torch.equal(y.view(torch.int16), y2.view(torch.int16))

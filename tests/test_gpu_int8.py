@@ -252,3 +252,17 @@ def test_scales_whose_product_leaves_fp32(B, T, D, N, act):
     assert far.max() <= 0, (int((far > 0).sum()), far.size)
     over = np.abs(ref) > 3.41e38
     assert (got[over] == np.sign(ref[over]) * np.inf).all()
+
+
+def test_operands_of_the_other_layout_are_refused(B):
+    g = Gemm(B, 70, 128, 64, 2, [0, 30, 70], "none")
+    ok = list(g.d)
+    for i, t in [(0, ok[0].t().contiguous()), (2, ok[2].transpose(1, 2).contiguous()), (3, ok[3].t().contiguous())]:
+        g.d = [*ok[:i], t, *ok[i + 1:]]
+        with pytest.raises(ValueError, match="rows of"):
+            g.run()
+    w = torch.empty(2, 64, 128, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="rows of"):
+        B.moe_quantize_weights_i8(2, 128, 64, 64, 0, w, ok[2], ok[3])
+    with pytest.raises(ValueError, match="rows of"):
+        B.moe_quantize_rows_i8(70, 128, torch.empty(128, 70, dtype=torch.bfloat16, device="cuda"), ok[0], ok[1])
