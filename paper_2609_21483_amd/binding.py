@@ -9,6 +9,7 @@ no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import re
 from typing import Optional
@@ -340,41 +341,43 @@ def _device_of(name: str, t: Optional[torch.Tensor]) -> int:
     return t.get_device()
 
 
-def _whole_rows(shape, width: int) -> bool:
-    """Whether the last dimensions of a shape make up a row of `width` values."""
+def _same_rows(shape, want) -> bool:
+    """Whether a tensor of `shape` holds that of shape `want` in rows of the same length."""
+    if math.prod(shape) != math.prod(want):
+        return False
+    if len(shape) < 2 or len(want) < 2 or 0 in shape:
+        return True
     n = 1
     for d in reversed(shape):
         n *= d
-        if n == width:
-            return True
-    return n == 0
+        if n >= want[-1]:
+            return n == want[-1]
+    return False
 
 
-def _arg(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, dev: int, width: int = 0) -> int:
-    """The address of a tensor that is as it has to be.  width: the length of its rows; dimensions before them may
-    be joined or split, and a tensor of one dimension is taken as it is.  So [F][H] in place of [H][F] is refused."""
+def _arg(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, want, dev: int) -> int:
+    """The address of a tensor that is as it has to be.  want: its shape, of which dimensions may be joined or split
+    as long as the last ones make up the same rows, and which may be given as one dimension.  So weights [F][H] in
+    place of [H][F] are refused."""
     if t is None:
         raise ValueError(f"{name} is missing")
-    if t.dtype is not dtype or t.numel() != numel or t.get_device() != dev:
-        raise ValueError(f"{name} must be {dtype} with {numel} elements on cuda:{dev}, "
-                         f"not {t.dtype} with {t.numel()} on {t.device}")
+    if t.dtype is not dtype or t.get_device() != dev or (t.shape != want and not _same_rows(t.shape, want)):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(want)} on cuda:{dev}, "
+                         f"not {t.dtype} of {tuple(t.shape)} on {t.device}")
     if not t.is_contiguous():
         raise ValueError("tensors passed to the MoE library must be contiguous")
-    if width and t.size(-1) != width and t.dim() > 1 and not _whole_rows(t.shape, width):
-        raise ValueError(f"{name} must have rows of {width}, not the shape {tuple(t.shape)}")
     return t.data_ptr()
 
 
 def _off(t: Optional[torch.Tensor], n_groups: int, dev: int) -> Optional[int]:
-    return None if t is None and n_groups == 1 else _arg("group_off", t, torch.int32, n_groups + 1, dev)
+    return None if t is None and n_groups == 1 else _arg("group_off", t, torch.int32, (n_groups + 1,), dev)
 
 
 def _ws(t: Optional[torch.Tensor], dev: int):
     """Address and size of a workspace."""
     if t is None:
         raise ValueError("ws is missing")
-    n = t.numel()
-    return _arg("ws", t, t.dtype, n, dev), n * t.element_size()
+    return _arg("ws", t, t.dtype, t.shape, dev), t.nbytes
 
 
 def _call(name: str, dev: int, stream, *args) -> None:
@@ -400,40 +403,40 @@ def moe_ffn_workspace_size(cfg: moe_ffn_config, backward: bool = False) -> int:
 def moe_ffn_forward(cfg: moe_ffn_config, x, group_off, w1, w3, w2, gate, up, y, ws, stream=None) -> None:
     dev, bf = _device_of("x", x), torch.bfloat16
     T, H, F, G = cfg.rows, cfg.hidden, cfg.ffn, cfg.n_groups
-    TH, TF, W = T * H, T * F, G * H * F
-    _call("moe_ffn_forward", dev, stream, cfg, _arg("x", x, bf, TH, dev, H), _off(group_off, G, dev),
-          _arg("w1", w1, bf, W, dev, F), _arg("w3", w3, bf, W, dev, F), _arg("w2", w2, bf, W, dev, H),
-          None if gate is None else _arg("gate", gate, bf, TF, dev, F),
-          None if up is None else _arg("up", up, bf, TF, dev, F), _arg("y", y, bf, TH, dev, H), *_ws(ws, dev))
+    TH, TF, HF, FH = (T, H), (T, F), (G, H, F), (G, F, H)
+    _call("moe_ffn_forward", dev, stream, cfg, _arg("x", x, bf, TH, dev), _off(group_off, G, dev),
+          _arg("w1", w1, bf, HF, dev), _arg("w3", w3, bf, HF, dev), _arg("w2", w2, bf, FH, dev),
+          None if gate is None else _arg("gate", gate, bf, TF, dev),
+          None if up is None else _arg("up", up, bf, TF, dev), _arg("y", y, bf, TH, dev), *_ws(ws, dev))
 
 
 def moe_ffn_backward(cfg: moe_ffn_config, dy, x, group_off, w1, w3, w2, gate, up, dx, dw1, dw3, dw2, ws,
                      stream=None) -> None:
     dev, bf = _device_of("dy", dy), torch.bfloat16
     T, H, F, G = cfg.rows, cfg.hidden, cfg.ffn, cfg.n_groups
-    TH, TF, W = T * H, T * F, G * H * F
-    _call("moe_ffn_backward", dev, stream, cfg, _arg("dy", dy, bf, TH, dev, H), _arg("x", x, bf, TH, dev, H),
-          _off(group_off, G, dev), _arg("w1", w1, bf, W, dev, F), _arg("w3", w3, bf, W, dev, F),
-          _arg("w2", w2, bf, W, dev, H), _arg("gate", gate, bf, TF, dev, F), _arg("up", up, bf, TF, dev, F),
-          None if dx is None else _arg("dx", dx, bf, TH, dev, H),
-          None if dw1 is None else _arg("dw1", dw1, bf, W, dev, F),
-          None if dw3 is None else _arg("dw3", dw3, bf, W, dev, F),
-          None if dw2 is None else _arg("dw2", dw2, bf, W, dev, H), *_ws(ws, dev))
+    TH, TF, HF, FH = (T, H), (T, F), (G, H, F), (G, F, H)
+    _call("moe_ffn_backward", dev, stream, cfg, _arg("dy", dy, bf, TH, dev), _arg("x", x, bf, TH, dev),
+          _off(group_off, G, dev), _arg("w1", w1, bf, HF, dev), _arg("w3", w3, bf, HF, dev),
+          _arg("w2", w2, bf, FH, dev), _arg("gate", gate, bf, TF, dev), _arg("up", up, bf, TF, dev),
+          None if dx is None else _arg("dx", dx, bf, TH, dev),
+          None if dw1 is None else _arg("dw1", dw1, bf, HF, dev),
+          None if dw3 is None else _arg("dw3", dw3, bf, HF, dev),
+          None if dw2 is None else _arg("dw2", dw2, bf, FH, dev), *_ws(ws, dev))
 
 
 def moe_quantize_rows_i8(rows: int, cols: int, x, q, scale, stream=None) -> None:
     dev = _device_of("x", x)
-    _call("moe_quantize_rows_i8", dev, stream, int(rows), int(cols), _arg("x", x, torch.bfloat16, rows * cols, dev, cols),
-          _arg("q", q, torch.int8, rows * cols, dev, cols), _arg("scale", scale, torch.float32, rows, dev))
+    _call("moe_quantize_rows_i8", dev, stream, int(rows), int(cols), _arg("x", x, torch.bfloat16, (rows, cols), dev),
+          _arg("q", q, torch.int8, (rows, cols), dev), _arg("scale", scale, torch.float32, (rows,), dev))
 
 
 def moe_quantize_weights_i8(n_groups: int, depth: int, channels: int, q_channels: int, first: int, w, wq, scale,
                             stream=None) -> None:
     dev = _device_of("w", w)
     _call("moe_quantize_weights_i8", dev, stream, int(n_groups), int(depth), int(channels), int(q_channels), int(first),
-          _arg("w", w, torch.bfloat16, n_groups * depth * channels, dev, channels),
-          _arg("wq", wq, torch.int8, n_groups * q_channels * depth, dev, depth),
-          _arg("scale", scale, torch.float32, n_groups * q_channels, dev, q_channels))
+          _arg("w", w, torch.bfloat16, (n_groups, depth, channels), dev),
+          _arg("wq", wq, torch.int8, (n_groups, q_channels, depth), dev),
+          _arg("scale", scale, torch.float32, (n_groups, q_channels), dev))
 
 
 def moe_gemm_i8_workspace_size(cfg: moe_gemm_i8_config) -> int:
@@ -446,10 +449,10 @@ def moe_gemm_i8(cfg: moe_gemm_i8_config, xq, x_scale, group_off, wq, w_scale, y,
     dev = _device_of("xq", xq)
     T, K, N, G = cfg.rows, cfg.depth, cfg.channels, cfg.n_groups
     out = N if cfg.act == MOE_ACT_NONE else N // 2
-    _call("moe_gemm_i8", dev, stream, cfg, _arg("xq", xq, torch.int8, T * K, dev, K),
-          _arg("x_scale", x_scale, torch.float32, T, dev), _off(group_off, G, dev),
-          _arg("wq", wq, torch.int8, G * N * K, dev, K), _arg("w_scale", w_scale, torch.float32, G * N, dev, N),
-          _arg("y", y, torch.bfloat16, T * out, dev, out), *_ws(ws, dev))
+    _call("moe_gemm_i8", dev, stream, cfg, _arg("xq", xq, torch.int8, (T, K), dev),
+          _arg("x_scale", x_scale, torch.float32, (T,), dev), _off(group_off, G, dev),
+          _arg("wq", wq, torch.int8, (G, N, K), dev), _arg("w_scale", w_scale, torch.float32, (G, N), dev),
+          _arg("y", y, torch.bfloat16, (T, out), dev), *_ws(ws, dev))
 
 
 # ---- convenience --------------------------------------------------------------

@@ -165,22 +165,24 @@ def test_offsets_off_their_alignment_are_refused(call):
 
 BF = torch.bfloat16
 G, H, F, T = 2, 64, 192, 6
-# (weights [G][H][F], rows [T][H]; a CPU tensor's device is -1)
-WHOLE_ROWS = [((G, H, F), F, G * H * F), ((G * H, F), F, G * H * F), ((1, G, H, F), F, G * H * F), ((H, F), F, H * F),
-              ((G * H * F,), F, G * H * F), ((2, 3, H), H, T * H), ((T, 4, 16), H, T * H), ((1, H), H, H), ((H,), H, H),
-              ((0, H), H, 0), ((0,), H, 0), ((G, H, F, 1), F, G * H * F)]
-OTHER_ROWS = [((G, F, H), F, G * H * F), ((F, H), F, H * F), ((H, T), H, T * H), ((T * 16, 4), H, T * H),
-              ((T // 2, 2 * H), H, T * H)]
+# (a tensor's shape, the shape that a call wants; a CPU tensor's device is -1)
+WHOLE_ROWS = [((G, H, F), (G, H, F)), ((G * H, F), (G, H, F)), ((1, G, H, F), (G, H, F)), ((H, F), (1, H, F)),
+              ((G * H * F,), (G, H, F)), ((2, 3, H), (T, H)), ((T, 4, 16), (T, H)), ((1, H), (1, H)), ((H,), (1, H)),
+              ((0, H), (0, H)), ((0,), (0, H)), ((0, 7), (0, H)), ((G, H, F, 1), (G, H, F)), ((T, 1), (T,)),
+              ((2, 3), (T,)), ((), (1,))]
+OTHER_ROWS = [((G, F, H), (G, H, F)), ((F, H), (1, H, F)), ((H, T), (T, H)), ((T * 16, 4), (T, H)),
+              ((T // 2, 2 * H), (T, H)), ((T - 1, H), (T, H)), ((T - 1,), (T,)), ((T, H), (-1, H))]
 
 
-@pytest.mark.parametrize("shape,width,n", WHOLE_ROWS)
-def test_binding_takes_tensors_whose_rows_are_whole(shape, width, n):
+@pytest.mark.parametrize("shape,want", WHOLE_ROWS, ids=str)
+def test_binding_takes_tensors_whose_rows_are_whole(shape, want):
     t = torch.zeros(shape, dtype=BF)
-    assert B._arg("w", t, BF, n, -1, width) == t.data_ptr()
+    assert B._arg("w", t, BF, want, -1) == t.data_ptr()
 
 
-@pytest.mark.parametrize("shape,width,n", OTHER_ROWS)
-def test_binding_refuses_tensors_of_other_rows(shape, width, n):
-    """As many elements, but in rows of another length: the weights of torch's Linear, transposed rows."""
-    with pytest.raises(ValueError, match=f"rows of {width}"):
-        B._arg("w", torch.zeros(shape, dtype=BF), BF, n, -1, width)
+@pytest.mark.parametrize("shape,want", OTHER_ROWS, ids=str)
+def test_binding_refuses_tensors_of_other_rows(shape, want):
+    """Another number of elements, or as many in rows of another length: the weights of torch's Linear, transposed
+    rows."""
+    with pytest.raises(ValueError, match="of shape"):
+        B._arg("w", torch.zeros(shape, dtype=BF), BF, want, -1)
