@@ -453,6 +453,28 @@ moe_status moe_ffn_backward(const moe_ffn_config* cfg, const uint16_t* dy, const
                             const uint16_t* gate, const uint16_t* up, uint16_t* dx, uint16_t* dw1, uint16_t* dw3,
                             uint16_t* dw2, void* ws, size_t ws_bytes, void* stream);
 
+/* Which tiles a product over row groups is computed by, and in how many parts
+ * its depth is split (on the host; no device is touched). */
+typedef enum {
+  MOE_TILES_FEW4 = 0,  /* 32 rows x 64 columns, 4 waves that share the depth */
+  MOE_TILES_FEW8 = 1,  /* the same, 8 waves */
+  MOE_TILES_SMALL = 2, /* 128 x 128 */
+  MOE_TILES_WIDE = 3   /* 256 x 256 */
+} moe_tiles;
+
+typedef struct {
+  int32_t tiles; /* moe_tiles */
+  int32_t split; /* parts of the depth, 1: whole */
+} moe_product_plan;
+
+typedef struct {
+  moe_product_plan up, down; /* forward: both projections of x, and of the hidden rows */
+  moe_product_plan dh;       /* backward: the hidden rows' gradients */
+  moe_product_plan dx, dw;   /* and those of x and of the weights, in one launch of the same tiles */
+} moe_ffn_plan;
+
+moe_status moe_ffn_plan_host(const moe_ffn_config* cfg, moe_ffn_plan* out);
+
 /* Rows in 8 bits: scale[t] = max |x[t][.]| / 127 in fp32, q[t][c] = x[t][c] /
  * scale[t] in fp32, rounded to the nearest whole number (halves to even), in
  * [-127, 127].  A row of zeros has scale 0 and q = 0.  A row that holds an
@@ -480,6 +502,7 @@ typedef struct {
 } moe_gemm_i8_config;
 
 moe_status moe_gemm_i8_workspace_size(const moe_gemm_i8_config* cfg, size_t* bytes);
+moe_status moe_gemm_i8_plan_host(const moe_gemm_i8_config* cfg, moe_product_plan* out);
 
 /* v[t][n] = (sum_k xq[t][k] wq[g][n][k]) * x_scale[t] * w_scale[g][n] for the
  * rows t of group g: the sum exact in 32-bit integers (any int8 values), the

@@ -85,6 +85,20 @@ class moe_gemm_i8_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("rows", "depth", "channels", "n_groups", "act")]
 
 
+MOE_TILES = ("few4", "few8", "small", "wide")
+
+
+class moe_product_plan(C.Structure):
+    _fields_ = [("tiles", C.c_int32), ("split", C.c_int32)]
+
+    def as_tuple(self):
+        return MOE_TILES[self.tiles], self.split
+
+
+class moe_ffn_plan(C.Structure):
+    _fields_ = [(n, moe_product_plan) for n in ("up", "down", "dh", "dx", "dw")]
+
+
 class MoeError(RuntimeError):
     def __init__(self, fn: str, status: int, msg: str):
         super().__init__(f"{fn} failed ({status}): {msg}")
@@ -124,11 +138,13 @@ _SIGS = {
     "moe_plan_host": ([_H, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_int64), C.POINTER(moe_plan)], C.c_int),
     "moe_tile_geometry": ([_H, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32)], C.c_int),
     "moe_ffn_workspace_size": ([C.POINTER(moe_ffn_config), C.c_int32, C.POINTER(C.c_size_t)], C.c_int),
+    "moe_ffn_plan_host": ([C.POINTER(moe_ffn_config), C.POINTER(moe_ffn_plan)], C.c_int),
     "moe_ffn_forward": ([C.POINTER(moe_ffn_config)] + [_P] * 9 + [C.c_size_t, _P], C.c_int),
     "moe_ffn_backward": ([C.POINTER(moe_ffn_config)] + [_P] * 13 + [C.c_size_t, _P], C.c_int),
     "moe_quantize_rows_i8": ([C.c_int32, C.c_int32, _P, _P, _P, _P], C.c_int),
     "moe_quantize_weights_i8": ([C.c_int32] * 5 + [_P, _P, _P, _P], C.c_int),
     "moe_gemm_i8_workspace_size": ([C.POINTER(moe_gemm_i8_config), C.POINTER(C.c_size_t)], C.c_int),
+    "moe_gemm_i8_plan_host": ([C.POINTER(moe_gemm_i8_config), C.POINTER(moe_product_plan)], C.c_int),
     "moe_gemm_i8": ([C.POINTER(moe_gemm_i8_config)] + [_P] * 7 + [C.c_size_t, _P], C.c_int),
 }
 for _name, (_args, _res) in _SIGS.items():
@@ -400,6 +416,12 @@ def moe_ffn_workspace_size(cfg: moe_ffn_config, backward: bool = False) -> int:
     return n.value
 
 
+def moe_ffn_plan_host(cfg: moe_ffn_config) -> moe_ffn_plan:
+    p = moe_ffn_plan()
+    _check("moe_ffn_plan_host", _lib.moe_ffn_plan_host(C.byref(cfg), C.byref(p)))
+    return p
+
+
 def moe_ffn_forward(cfg: moe_ffn_config, x, group_off, w1, w3, w2, gate, up, y, ws, stream=None) -> None:
     dev, bf = _device_of("x", x), torch.bfloat16
     T, H, F, G = cfg.rows, cfg.hidden, cfg.ffn, cfg.n_groups
@@ -443,6 +465,12 @@ def moe_gemm_i8_workspace_size(cfg: moe_gemm_i8_config) -> int:
     n = C.c_size_t()
     _check("moe_gemm_i8_workspace_size", _lib.moe_gemm_i8_workspace_size(C.byref(cfg), C.byref(n)))
     return n.value
+
+
+def moe_gemm_i8_plan_host(cfg: moe_gemm_i8_config) -> moe_product_plan:
+    p = moe_product_plan()
+    _check("moe_gemm_i8_plan_host", _lib.moe_gemm_i8_plan_host(C.byref(cfg), C.byref(p)))
+    return p
 
 
 def moe_gemm_i8(cfg: moe_gemm_i8_config, xq, x_scale, group_off, wq, w_scale, y, ws, stream=None) -> None:

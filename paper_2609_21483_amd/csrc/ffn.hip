@@ -401,6 +401,17 @@ moe_status moe_ffn_workspace_size(const moe_ffn_config* cfg, int32_t backward, s
   return MOE_OK;
 }
 
+moe_status moe_ffn_plan_host(const moe_ffn_config* cfg, moe_ffn_plan* out) {
+  moe_status st = check_cfg(cfg);
+  if (st != MOE_OK) return st;
+  if (!out) return fail(MOE_ERR_INVALID_ARG, "out is NULL");
+  const FfnArgs a = args_of(cfg, nullptr);
+  const auto of = [](const tile::Plan& p) { return moe_product_plan{p.kind, p.split}; };
+  const GradPlan g = grad_plan(a);
+  *out = {of(plan<UP>(a)), of(plan<DOWN>(a)), of(plan<DH>(a)), {g.kind, g.dx_split}, {g.kind, g.dw_split}};
+  return MOE_OK;
+}
+
 moe_status moe_ffn_forward(const moe_ffn_config* cfg, const uint16_t* x, const int32_t* group_off, const uint16_t* w1,
                            const uint16_t* w3, const uint16_t* w2, uint16_t* gate, uint16_t* up, uint16_t* y, void* ws,
                            size_t ws_bytes, void* stream) {

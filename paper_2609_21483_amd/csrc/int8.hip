@@ -406,6 +406,15 @@ moe_status moe_gemm_i8_workspace_size(const moe_gemm_i8_config* cfg, size_t* byt
   return MOE_OK;
 }
 
+moe_status moe_gemm_i8_plan_host(const moe_gemm_i8_config* cfg, moe_product_plan* out) {
+  moe_status st = check_cfg(cfg);
+  if (st != MOE_OK) return st;
+  if (!out) return fail(MOE_ERR_INVALID_ARG, "out is NULL");
+  const tile::Plan p = plan(args_of(cfg));
+  *out = {p.kind, p.split};
+  return MOE_OK;
+}
+
 moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const float* x_scale, const int32_t* group_off,
                        const int8_t* wq, const float* w_scale, uint16_t* y, void* ws, size_t ws_bytes, void* stream) {
   moe_status st = check_cfg(cfg);

@@ -560,7 +560,7 @@ struct Few {
 // split (a kernel behind it adds the parts' sums, in order).
 // ---------------------------------------------------------------------------
 struct Plan {
-  enum Kind { FEW4, FEW8, SMALL, WIDE } kind;
+  enum Kind { FEW4 = MOE_TILES_FEW4, FEW8 = MOE_TILES_FEW8, SMALL = MOE_TILES_SMALL, WIDE = MOE_TILES_WIDE } kind;
   int split;
 };
 constexpr int MAX_SPLIT = 16;

@@ -186,3 +186,34 @@ def test_binding_refuses_tensors_of_other_rows(shape, want):
     rows."""
     with pytest.raises(ValueError, match="of shape"):
         B._arg("w", torch.zeros(shape, dtype=BF), BF, want, -1)
+
+
+def ffn_plan(*cfg):
+    return {n: getattr(B.moe_ffn_plan_host(B.moe_ffn_config(*cfg)), n).as_tuple() for n in ("up", "down", "dh", "dx", "dw")}
+
+
+def test_plan_queries_refuse_bad_arguments():
+    lib = B.library()
+    for cfg in BAD_FFN:
+        assert lib.moe_ffn_plan_host(C.byref(B.moe_ffn_config(*cfg)), C.byref(B.moe_ffn_plan())) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_ffn_plan_host(C.byref(B.moe_ffn_config(8, 64, 64, 1, 1)), None) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_ffn_plan_host(None, C.byref(B.moe_ffn_plan())) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_gemm_i8_plan_host(C.byref(B.moe_gemm_i8_config(8, 64, 64, 1, 0)), None) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_gemm_i8_plan_host(C.byref(B.moe_gemm_i8_config(8, 64, 12, 1, 0)), C.byref(B.moe_product_plan())) \
+        == B.MOE_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("T,H,F,G", [(1, 64, 64, 1), (5, 64, 8192, 1), (5, 8256, 64, 1), (300, 2048, 4096, 1), (3001, 64, 64, 2),
+                                     (333, 1024, 2816, 4), (8192, 4096, 14336, 1), (0, 64, 64, 3)])
+def test_workspaces_hold_the_parts_of_the_plan(T, H, F, G):
+    p = ffn_plan(T, H, F, G, 1)
+    parts = lambda n, values: 4 * p[n][1] * values if p[n][1] > 1 else 0
+    plane = (2 * T * F + 255) // 256 * 256
+    cfg = B.moe_ffn_config(T, H, F, G, 1)
+    assert B.moe_ffn_workspace_size(cfg) == 256 + plane + max(parts("up", 2 * T * F), parts("down", T * H))
+    assert B.moe_ffn_workspace_size(cfg, True) == 256 + 3 * plane + max(
+        parts("dh", T * F), parts("dx", T * H) + parts("dw", 3 * G * H * F))
+    for act in (0, 1):
+        c = B.moe_gemm_i8_config(T, H, F, G, act)
+        s = B.moe_gemm_i8_plan_host(c).split
+        assert B.moe_gemm_i8_workspace_size(c) == 256 + (4 * s * T * F if s > 1 else 0)
