@@ -127,10 +127,11 @@ __device__ __forceinline__ void covered_rows(const int32_t* off, int G, int T, i
   else *end = e;
 }
 
-// most row tiles a list can have
+// Most row tiles a list can have: one for each group that has rows, whose
+// first row it holds, and one for every bm of the other rows.
 __host__ __device__ inline int max_row_tiles(int T, int G, int bm) {
-  const int full = T / bm + G;  // every group ends in a partial tile
-  return full < T ? full : T;
+  const int some = G < T ? G : T;
+  return some + (T - some) / bm;
 }
 
 // ---- the gated block's activation ---------------------------------------------

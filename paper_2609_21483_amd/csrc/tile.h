@@ -598,7 +598,7 @@ inline Timed tile_plan(double wide, double small, int stages, double sum_bytes, 
 // slots) behind 5 of ends, or the weights' stream where that is longer, once
 // from memory (5 TB/s) and for further row tiles mostly out of the caches (9).
 // Few rows against Small, us: H = 4096, F = 14336, up and down projection, 32
-// rows 52 + 50 : 57 + 56, 64 rows 77 + 46 : 60 + 57; H = 2048, F = 1408, 256 rows
+// rows 49 + 33 : 57 + 56, 64 rows 77 + 46 : 60 + 57; H = 2048, F = 1408, 256 rows
 // 14 + 8 : 17 + 17; 16 groups of 32 rows on average 43 + 27 : 46 + 27, of 64 rows
 // 60 + 37 : 49 + 34.
 // Eight waves share the depth where one workgroup per CU holds all tiles (the

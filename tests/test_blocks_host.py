@@ -217,3 +217,13 @@ def test_workspaces_hold_the_parts_of_the_plan(T, H, F, G):
         c = B.moe_gemm_i8_config(T, H, F, G, act)
         s = B.moe_gemm_i8_plan_host(c).split
         assert B.moe_gemm_i8_workspace_size(c) == 256 + (4 * s * T * F if s > 1 else 0)
+
+
+@pytest.mark.parametrize("H,F", [(4096, 14336), (2048, 8192), (8192, 4096), (1024, 1024)])
+def test_a_whole_tile_of_few_rows_is_planned_as_one(H, F):
+    """32 rows of one group are one row tile, as 31 are, and 64 are two."""
+    a, b = ffn_plan(31, H, F, 1, 1), ffn_plan(32, H, F, 1, 1)
+    assert a["up"] == b["up"] and a["down"] == b["down"]
+    for act in (0, 1):
+        a, b = (B.moe_gemm_i8_plan_host(B.moe_gemm_i8_config(T, H, F, 1, act)).as_tuple() for T in (31, 32))
+        assert a == b

@@ -98,3 +98,19 @@ def test_weight_quantiser_replays(B):
         torch.cuda.synchronize()
         eq, es = K.quantize_rows(x.float().transpose(1, 2).numpy())
         assert np.array_equal(q.cpu().numpy(), eq) and np.array_equal(s.cpu().numpy(), es), turn
+
+
+@pytest.mark.parametrize("T,off", [(32, None), (64, None), (128, None), (256, None), (512, None), (132, [0, 33, 66, 99, 132]),
+                                   (516, [0, 129, 258, 387, 516]), (259, [0, 1, 258, 259]), (98, [0, 33, 33, 98]),
+                                   (5, [0, 1, 2, 3, 4, 5, 5, 5])])
+def test_the_most_row_tiles_there_can_be(B, T, off):
+    """Groups of whole tiles, and of one row more than whole tiles: each launch has a workgroup for every tile."""
+    verify(Block(T, 128, 192, len(off) - 1 if off else 1, off, "silu", seed=27).cuda(B))
+    Gemm(B, T, 192, 144, len(off) - 1 if off else 1, off, "silu", seed=28).verify()
+
+
+@pytest.mark.parametrize("T,H,F", [(8192, 64, 1024), (8193, 64, 1024)])
+def test_the_most_wide_row_tiles_there_can_be(B, T, H, F):
+    verify(Block(T, H, F, 1, None, "silu", seed=29).cuda(B))
+    b = Block(T, H, F, 3, [0, 2561, 5378, T], "silu", seed=30).cuda(B)
+    verify(b)
