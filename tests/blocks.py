@@ -134,3 +134,38 @@ def check(name, got, ref, bound):
     assert not np.isnan(got[some]).any(), f"{name}: NaN"
     far = np.abs(got[some] - ref[some]) - bound[some]
     assert far.size == 0 or far.max() <= 0, f"{name}: {int((far > 0).sum())} of {far.size} beyond the bound, by up to {far.max():.3g}"
+
+
+def norms(name, got, ref, whole=4e-3, line=6.5e-3):
+    """2-norms of got - ref against those of ref: of the whole matrix, and of every row, column and 32 x 64 block of it.
+
+    A stored value is rounded by up to 2^-8 of itself, evenly: 2^-8 / sqrt(3) = 2.3e-3 of a norm at most.  Results are
+    rounded once and the rounded factors of their sums once, independently: sqrt(2) times that, 3.2e-3.  A line can
+    be the multiple of one rounded factor: 2^-8 of it and 2.3e-3.  fp32 sums add less than 1e-4 of the mean line.  A
+    part p of a sum's depth that is lost is sqrt(p) of the norm: 3e-2 for 32 of 32768.
+    The factors' roundings are 2^-8 / sqrt(3) of the root of the terms' squares, which a line's own norm is on average
+    but may fall below: of n values with a spread of chi^2 over n, n = 32 by a factor of 0.55 once in 20000, and 2.3e-3 /
+    0.55 and 2.3e-3 together are still 4.8e-3; one value alone may cancel to nothing.  So lines of fewer than 32 values
+    are left to the bounds of single values."""
+    got, ref = np.asarray(got, np.float64), np.asarray(ref, np.float64)
+    if got.ndim == 3:
+        for g, r in zip(got, ref):
+            norms(name, g, r, whole, line)
+        return
+    some = ~np.isnan(ref).any(1)
+    got, ref = got[some], ref[some]
+    if not ref.size:
+        return
+    e, r = (got - ref) ** 2, ref ** 2
+    assert e.sum() <= whole ** 2 * r.sum(), f"{name}: off by {math.sqrt(e.sum() / r.sum()):.2e} of its norm"
+    i, j = np.arange(0, ref.shape[0], 32), np.arange(0, ref.shape[1], 64)
+    blocks = [np.add.reduceat(np.add.reduceat(v, i, 0), j, 1) for v in (e, r)]
+    size = np.minimum(32, ref.shape[0] - i)[:, None] * np.minimum(64, ref.shape[1] - j)
+    for what, a, b, n in (("row", e.sum(1), r.sum(1), ref.shape[1]), ("column", e.sum(0), r.sum(0), ref.shape[0]),
+                          ("block", *blocks, size)):
+        if np.max(n) < 32:
+            continue
+        a = np.where(np.asarray(n) < 32, 0.0, a)
+        far = np.sqrt(a) - line * np.sqrt(b) - 1e-4 * math.sqrt(b.mean())
+        assert far.max() <= 0, f"{name}: {what} {np.unravel_index(far.argmax(), far.shape)} is off by " \
+            f"{math.sqrt(a.flat[far.argmax()] / max(b.flat[far.argmax()], 1e-300)):.2e} of its norm"

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests import block_plans as PL
 from tests import blocks as K
 
 B = pytest.importorskip("paper_2609_21483_amd.binding", reason="libmoe.so not built")
@@ -227,3 +228,53 @@ def test_a_whole_tile_of_few_rows_is_planned_as_one(H, F):
     for act in (0, 1):
         a, b = (B.moe_gemm_i8_plan_host(B.moe_gemm_i8_config(T, H, F, 1, act)).as_tuple() for T in (31, 32))
         assert a == b
+
+
+@pytest.mark.parametrize("T,H,F,off,act,plan", PL.FFN, ids=lambda v: str(v)[:24])
+def test_block_sizes_take_their_plan(T, H, F, off, act, plan):
+    assert ffn_plan(T, H, F, PL.groups(off), B.ACTS[act]) == plan
+
+
+@pytest.mark.parametrize("T,D,N,off,act,plan", PL.I8, ids=lambda v: str(v)[:24])
+def test_8_bit_sizes_take_their_plan(T, D, N, off, act, plan):
+    assert B.moe_gemm_i8_plan_host(B.moe_gemm_i8_config(T, D, N, PL.groups(off), B.ACTS[act])).as_tuple() == plan
+
+
+def test_sizes_cover_every_kind_of_tile_in_every_product():
+    # (few rows by 4 waves and wide tiles never split the depth, and the products with dy are never of few rows)
+    few, big = {("few4", False), ("few8", False), ("few8", True)}, {("small", False), ("small", True), ("wide", False)}
+    for n in ("up", "down", "dh", "dx", "dw"):
+        kinds = {(p[n][0], p[n][1] > 1) for *_, p in PL.FFN}
+        assert kinds == (few | big if n in ("up", "down") else big), n
+    for gated in (False, True):
+        assert {(p[0], p[1] > 1) for *_, act, p in PL.I8 if (act != "none") == gated} == few | big, gated
+
+
+def rounded(v):
+    return torch.from_numpy(np.asarray(v, np.float32)).to(BF).double().numpy()
+
+
+@pytest.mark.parametrize("T,H,F,lost", [(290, 512, 2112, 64), (5, 64, 8192, 32)])
+def test_norms_show_a_lost_part_of_a_sum(T, H, F, lost):
+    """With the library's roundings a result passes K.norms; without a step of one product's depth, or without one
+    row of a group, it does not, though every element may be within K.check's bound."""
+    rng = np.random.default_rng(T)
+    x, dy = rounded(rng.normal(size=(T, H))), rounded(rng.normal(size=(T, H)))
+    w1, w3 = (rounded(rng.normal(size=(1, H, F)) * H ** -0.5) for _ in range(2))
+    w2 = rounded(rng.normal(size=(1, F, H)) * F ** -0.5)
+    (y, gate, up), _ = K.forward(x, None, w1, w3, w2, "gelu", T)
+    h = rounded(K.act(gate, "gelu")[0] * up)
+    K.norms("y", rounded(h @ w2[0]), y)
+    K.norms("gate", rounded(gate), gate)
+    for cut in (slice(0, F - lost), slice(lost, F)):
+        with pytest.raises(AssertionError):
+            K.norms("y", rounded(h[:, cut] @ w2[0][cut]), y)
+    # one tile's part alone
+    some = rounded(h @ w2[0])
+    some[:32, :64] = rounded(h[:32, lost:] @ w2[0][lost:, :64])
+    with pytest.raises(AssertionError):
+        K.norms("y", some, y)
+    dw1 = x.T @ (dy @ w2[0].T)
+    K.norms("dw1", rounded(x.T @ rounded(dy @ w2[0].T)), dw1)
+    with pytest.raises(AssertionError):
+        K.norms("dw1", rounded(x[:-1].T @ rounded(dy @ w2[0].T)[:-1]), dw1)

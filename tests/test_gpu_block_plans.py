@@ -1,5 +1,6 @@
-"""GPU tests of the products over row groups at sizes that take every kind of tile (few rows by 4 and 8 waves, 128
-and 256 wide) and every split of the depth, in each direction; and of calls that run at the same time."""
+"""GPU tests of the products over row groups at sizes that take few-row, 128 and 256 wide tiles, whole and with split
+depths, against the 64-bit oracle (every kind of tile in every product, by exact sums: test_gpu_block_sums.py); and of
+calls that run at the same time."""
 import numpy as np
 import pytest
 import torch
