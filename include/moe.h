@@ -413,8 +413,16 @@ moe_status moe_tile_geometry(const moe_handle* h, int32_t* bm, int32_t* nt0, int
  * for the next, and may serve any calls that run one after the other, but not
  * two that overlap.  No call allocates, waits, or adds in an order that changes
  * from run to run, and all can be captured into a graph.  Outputs must not
- * overlap inputs or each other.  A result depends on its own row (and its
- * group's weights) alone, a weight's gradient on its own group's rows.
+ * overlap inputs or each other.
+ *
+ * No value of another row enters a row's results, and none of another group a
+ * weight's gradient.  The tiles, and the parts of a sum and their order, follow
+ * from the config alone (moe_ffn_plan_host): under one config a row's results
+ * are the same bits wherever it lies in its group, whatever the offsets and the
+ * other rows are, and a weight's gradient depends on its group's rows in their
+ * order alone.  Other rows, n_groups or widths in the config may change the last
+ * bits of fp32 sums (a token alone and in a batch).  8-bit sums are exact, so
+ * moe_gemm_i8 and the quantisers give a row the same bits under any config.
  */
 typedef enum {
   MOE_ACT_NONE = 0,

@@ -8,6 +8,7 @@ import torch
 from tests import block_plans as PL
 from tests import blocks as K
 from tests.test_gpu_ffn import B, Block, f64, untouched  # noqa: F401  (B is the fixture)
+from tests.test_gpu_int8 import Gemm
 
 pytestmark = pytest.mark.gpu
 BF = torch.bfloat16
@@ -206,3 +207,69 @@ def test_planes_of_more_than_31_bits_are_exact(B):
     same("dw1", dw1[0], X.t() @ dg, X.abs().t() @ dg.abs())
     same("dw3", dw3[0], X.t() @ du, X.abs().t() @ du.abs())
     same("dw2", dw2[0], h.t() @ D, h.abs().t() @ D.abs())
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16)
+
+
+# few rows whole and in parts, small tiles in parts, wide tiles
+@pytest.mark.parametrize("T,H,F,G,off,off2", [
+    (60, 128, 192, 3, [0, 20, 21, 60], [7, 30, 55, 58]), (5, 64, 8192, 2, [0, 2, 5], [0, 3, 5]),
+    (300, 2048, 4096, 1, [0, 300], [0, 300]), (3001, 64, 64, 2, [0, 1, 2987], [14, 2000, 3001]),
+    (12000, 1024, 1024, 3, [3, 40, 7041, 11990], [0, 6000, 6100, 12000])], ids=lambda v: str(v)[:24])
+def test_bits_follow_from_the_config_and_the_row(B, T, H, F, G, off, off2):
+    """The same rows elsewhere in their groups, among other rows and other offsets."""
+    a, b = Block(T, H, F, G, off, "silu", seed=35), Block(T, H, F, G, off2, "silu", seed=36)
+    for n in ("w1", "w3", "w2"):
+        setattr(b, n, getattr(a, n))
+    rng = np.random.default_rng(T)
+    src, dst = [], []
+    for g in range(G):
+        r, s = np.arange(off[g], off[g + 1]), np.arange(off2[g], off2[g + 1])
+        n = (min(len(r), len(s)) + 1) // 2
+        src += rng.choice(r, n, replace=False).tolist()
+        dst += rng.choice(s, n, replace=False).tolist()
+    b.x[dst], b.dy[dst] = a.x[src], a.dy[src]
+    a.cuda(B), b.cuda(B)
+    src, dst = torch.tensor(src, device="cuda"), torch.tensor(dst, device="cuda")
+    fa, fb = a.forward()[0], b.forward()[0]
+    for p, q in zip(fa, fb):
+        assert torch.equal(bits(p[src]), bits(q[dst]))
+    ra, rb = a.backward(fa[1], fa[2])[0], b.backward(fb[1], fb[2])[0]
+    assert torch.equal(bits(ra["dx"][src]), bits(rb["dx"][dst]))
+
+
+@pytest.mark.parametrize("T,H,F,off,off2", [(300, 64, 64, [0, 90, 290], [10, 100, 300]), (3001, 64, 64, [0, 1200, 2987], [14, 1214, 3001]),
+                                            (2100, 4096, 192, [0, 129, 300, 1000, 1000, 1000, 2100], [0, 1900, 2071, 2072, 2073, 2074, 2075])])
+def test_bits_of_gradients_follow_from_the_config_and_the_group(B, T, H, F, off, off2):
+    """The second group's rows elsewhere, behind another first group of other rows."""
+    G, n = len(off) - 1, off[2] - off[1]
+    a, b = Block(T, H, F, G, off, "gelu", seed=37), Block(T, H, F, G, off2, "gelu", seed=38)
+    for w in ("w1", "w3", "w2"):
+        getattr(b, w)[1] = getattr(a, w)[1]
+    assert n == off2[2] - off2[1]
+    for v in ("x", "dy"):
+        getattr(b, v)[off2[1]:off2[2]] = getattr(a, v)[off[1]:off[2]]
+    a.cuda(B), b.cuda(B)
+    fa, fb = a.forward()[0], b.forward()[0]
+    ra, rb = a.backward(fa[1], fa[2])[0], b.backward(fb[1], fb[2])[0]
+    for w in ("dw1", "dw3", "dw2"):
+        assert torch.equal(bits(ra[w][1]), bits(rb[w][1])), w
+
+
+# against few rows by 8 waves, of one row: every other kind of tile, whole and in parts
+@pytest.mark.parametrize("T,D,N,G,off,act", [
+    (600, 4160, 272, 1, None, "silu"), (600, 192, 320, 2, [0, 300, 600], "gelu"), (9000, 448, 528, 1, None, "none"),
+    (8190, 448, 48, 2, [0, 4000, 8190], "gelu"), (2100, 8256, 48, 1, None, "gelu"), (2100, 8256, 48, 1, None, "none"),
+    (8190, 448, 1040, 2, [0, 4001, 8190], "gelu"), (12000, 448, 272, 1, None, "silu"), (5, 28736, 144, 1, None, "gelu")])
+def test_8_bit_rows_have_the_same_bits_in_any_batch(B, T, D, N, G, off, act):
+    g = Gemm(B, T, D, N, G, off, act, seed=39)
+    y, _ = g.run()
+    for r in (0, 7, T // 2 - 1, T - 1):
+        group = 0 if off is None else int(r >= off[1])
+        cfg = B.moe_gemm_i8_config(1, D, N, 1, B.ACTS[act])
+        one = torch.empty(1, g.out, dtype=BF, device="cuda")
+        ws = torch.empty(B.moe_gemm_i8_workspace_size(cfg), dtype=torch.uint8, device="cuda")
+        B.moe_gemm_i8(cfg, g.d[0][r:r + 1], g.d[1][r:r + 1].clone(), None, g.d[2][group], g.d[3][group], one, ws)
+        assert torch.equal(bits(one[0]), bits(y[r])), r
