@@ -266,7 +266,7 @@ def test_bits_of_gradients_follow_from_the_config_and_the_group(B, T, H, F, off,
 def test_8_bit_rows_have_the_same_bits_in_any_batch(B, T, D, N, G, off, act):
     g = Gemm(B, T, D, N, G, off, act, seed=39)
     y, _ = g.run()
-    for r in (0, 7, T // 2 - 1, T - 1):
+    for r in sorted({0, min(7, T - 1), T // 2 - 1, T - 1}):
         group = 0 if off is None else int(r >= off[1])
         cfg = B.moe_gemm_i8_config(1, D, N, 1, B.ACTS[act])
         one = torch.empty(1, g.out, dtype=BF, device="cuda")
