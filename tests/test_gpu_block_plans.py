@@ -115,3 +115,54 @@ def test_the_most_wide_row_tiles_there_can_be(B, T, H, F):
     verify(Block(T, H, F, 1, None, "silu", seed=29).cuda(B))
     b = Block(T, H, F, 3, [0, 2561, 5378, T], "silu", seed=30).cuda(B)
     verify(b)
+
+
+def test_8_bit_calls_at_the_same_time(B):
+    """Quantisers and products on streams of their own, each behind its own inputs and sentinels, against the same
+    ones run alone: by the stream given, and by the current one."""
+    shapes = [(700, 448, 320, 3, [0, 300, 301, 700], "silu"), (5, 28736, 144, 1, None, "silu"),
+              (8190, 448, 528, 1, None, "none"), (40, 16384, 200, 2, [1, 3, 39], "none")]
+    gemms = [Gemm(B, *s, seed=40 + i) for i, s in enumerate(shapes)]
+    xs = [rows_bf16(s[0], s[1], 44 + i).cuda() for i, s in enumerate(shapes)]
+    w = [rows_bf16(192 * (i + 1), 128, 48 + i).view(i + 1, 192, 128).cuda() for i in range(4)]
+
+    def run(g, x, w, stream):
+        B.moe_quantize_rows_i8(*x.shape, x, g.d[0], g.d[1], stream)
+        wq, ws = torch.full((len(w), 128, 192), 99, dtype=torch.int8, device="cuda"), torch.full((len(w), 128), 9.0, device="cuda")
+        B.moe_quantize_weights_i8(len(w), 192, 128, 128, 0, w, wq, ws, stream)
+        return g.run(stream)[0], g.d[0].clone(), g.d[1].clone(), wq, ws
+
+    alone = [run(*a, None) for a in zip(gemms, xs, w)]
+    streams = [torch.cuda.Stream() for _ in gemms]
+    torch.cuda.synchronize()
+    for turn in range(4):
+        runs = []
+        for a, s in zip(zip(gemms, xs, w), streams):
+            # fills and launches on one stream, so in order
+            with torch.cuda.stream(s):
+                runs.append(run(*a, s if turn % 2 else None))
+        torch.cuda.synchronize()
+        for a, r in zip(alone, runs):
+            for p, q in zip(a, r):
+                assert torch.equal(p.contiguous().view(torch.int8), q.contiguous().view(torch.int8))
+
+
+def test_a_stream_that_waits_for_another(B):
+    """Inputs and sentinels of the current stream, the calls on a given one that waits for it, and back."""
+    b = Block(700, 256, 320, 3, [0, 300, 301, 700], "silu", seed=52).cuda(B)
+    g = Gemm(B, 333, 448, 320, 3, [0, 100, 101, 333], "silu", seed=53)
+    (y, gate, up), _ = b.forward()
+    r, _ = b.backward(gate, up)
+    y8, _ = g.run()
+    torch.cuda.synchronize()
+    s, here = torch.cuda.Stream(), torch.cuda.current_stream()
+    out = {n: torch.full_like(t, 3.0) for n, t in dict(y=y, gate=gate, up=up, y8=y8, **r).items()}
+    s.wait_stream(here)
+    d = b.d
+    B.moe_ffn_forward(b.cfg, d["x"], d["off"], d["w1"], d["w3"], d["w2"], out["gate"], out["up"], out["y"], b.ws, s)
+    B.moe_ffn_backward(b.cfg, d["dy"], d["x"], d["off"], d["w1"], d["w3"], d["w2"], out["gate"], out["up"], out["dx"],
+                       out["dw1"], out["dw3"], out["dw2"], b.ws, s)
+    B.moe_gemm_i8(g.cfg, g.d[0], g.d[1], g.doff, g.d[2], g.d[3], out["y8"], g.ws, s)
+    here.wait_stream(s)
+    for n, t in dict(y=y, gate=gate, up=up, y8=y8, **r).items():
+        assert torch.equal(out[n].view(torch.int16), t.view(torch.int16)), n
