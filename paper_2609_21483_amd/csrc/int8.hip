@@ -25,7 +25,7 @@ __device__ __forceinline__ float scale_of(uint32_t amax) {
 // does the division itself decide (about 1 value in 5000).
 struct Quantizer {
   float scale, inv;
-  bool slow;  // (a subnormal reciprocal, or a scale whose quotients the bound does not hold for)
+  bool slow;  // a tiny scale, whose reciprocal may be infinite and whose values subnormal: always divided
   __device__ __forceinline__ explicit Quantizer(float s) : scale(s), inv(__builtin_amdgcn_rcpf(s)), slow(s < 0x1p-100f) {}
   __device__ __forceinline__ int operator()(float v) const {
     float q = v * inv, r = rintf(q);
@@ -177,7 +177,7 @@ struct I8Args {
   const int8_t *x, *w;
   const float *sx, *sw;
   uint16_t* y;
-  int32_t* part;  // few rows: partial sums [split][T][N] of a split product
+  int32_t* part;  // partial sums [split][T][N] of a split product
   int split;
 };
 
