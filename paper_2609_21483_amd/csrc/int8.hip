@@ -87,7 +87,11 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(int rows, int cols, 
 // Weights: 64 channels x 256 rows of the depth a workgroup, in three passes, the
 // largest magnitudes of the channels (their bits gathered where the scales go;
 // a maximum does not depend on the order), the values, transposed through LDS,
-// and the scales.  14336 x 4096 in 66 us: the weights are read twice, 4.4 TB/s.
+// and the scales.  14336 x 4096 in 62 us, 71 where other weights pass between
+// (1.8 and 2.1 times what one read of them takes at 5.1 TB/s): a channel's
+// values lie a row apart, so its largest is known only after the whole depth,
+// and a strip of 64 channels by the depth that a workgroup would keep for its
+// second pass (1.8 MB here) does not fit its LDS.
 constexpr int QW_N = 64, QW_K = 256;
 
 // what = 0: clears, 1: turns magnitudes into scales
@@ -237,8 +241,9 @@ __device__ __forceinline__ tile::Operand weights_op(const I8Args& a, const RowTi
   return {w, GATED ? w + (size_t)out * a.K : nullptr, (uint32_t)a.K, out - n0, 0, 0};
 }
 
-// 16384 x 14336 x 4096 in 820 us, 2.3 POP/s (Wide); 6007 rows in 16 groups, 2048
-// x 2816 gated, in 65 us, 1.07 (Small).
+// 16384 x 14336 x 4096 in 805 us, 2.4 POP/s (Wide; calls in a row, 850 to 880 one
+// by one under the profiler); 6007 rows in 16 groups, 2048 x 2816 gated, in 57 to
+// 67 us by what the caches hold, 1.03 to 1.2 (Small).
 template <typename S, bool GATED>
 __global__ __launch_bounds__(S::THREADS) void gemm_i8_kernel(I8Args a) {
   using Tl = tile::Tile<S, true, false, false>;
