@@ -514,8 +514,9 @@ moe_status moe_gemm_i8_plan_host(const moe_gemm_i8_config* cfg, moe_product_plan
 
 /* v[t][n] = (sum_k xq[t][k] wq[g][n][k]) * x_scale[t] * w_scale[g][n] for the
  * rows t of group g: the sum exact in 32-bit integers (any int8 values), the
- * scales fp32 (no two of the three need to have a product within fp32's range).  act = MOE_ACT_NONE: y bf16 [T][N] is v.  Else channels [0, N/2)
- * are gates and the rest their ups: y bf16 [T][N/2] = act(v[t][f]) *
+ * scales fp32 (neither their product nor the sum's with one of them has to be
+ * within fp32's range).  act = MOE_ACT_NONE: y bf16 [T][N] is v.  Else channels
+ * [0, N/2) are gates and the rest their ups: y bf16 [T][N/2] = act(v[t][f]) *
  * v[t][N/2 + f], v unrounded.  xq: int8 [T][K], x_scale: fp32 [T], wq: int8
  * [G][N][K], w_scale: fp32 [G][N]. */
 moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const float* x_scale,
