@@ -273,3 +273,40 @@ def test_8_bit_rows_have_the_same_bits_in_any_batch(B, T, D, N, G, off, act):
         ws = torch.empty(B.moe_gemm_i8_workspace_size(cfg), dtype=torch.uint8, device="cuda")
         B.moe_gemm_i8(cfg, g.d[0][r:r + 1], g.d[1][r:r + 1].clone(), None, g.d[2][group], g.d[3][group], one, ws)
         assert torch.equal(bits(one[0]), bits(y[r])), r
+
+
+def test_gradients_of_groups_beyond_4_gib_of_weights_are_exact(B):
+    """The last group's weights and gradients start more than 4 GiB in; groups without rows have gradients of 0."""
+    T, H, F, G = 5, 16384, 32768, 6
+    off = torch.tensor([0, 1, 1, 1, 1, 1, 5], dtype=torch.int32, device="cuda")
+    assert 5 * H * F * 2 > 1 << 32
+    g = torch.Generator(device="cuda").manual_seed(41)
+    thin = lambda t, n: t * (torch.rand(t.shape, generator=g, device="cuda") < 1.0 / n).to(BF)
+    x, dy = thin(sparse(g, T, H), 4), thin(sparse(g, T, H), 16)
+    w1, w3, w2 = (torch.zeros(G, *s, dtype=BF, device="cuda") for s in ((H, F), (H, F), (F, H)))
+    for w in (w1, w3, w2):
+        w[-1] = sparse(g, *w.shape[1:])
+    x[:, -1], w1[-1, -1], w3[-1, -1] = 1, 128, 0
+    cfg = B.moe_ffn_config(T, H, F, G, B.MOE_ACT_SILU)
+    assert B.moe_ffn_plan_host(cfg).dw.as_tuple() == ("wide", 1)
+    ws = torch.empty(B.moe_ffn_workspace_size(cfg, True), dtype=torch.uint8, device="cuda")
+    gate, up, y = (torch.empty(T, n, dtype=BF, device="cuda") for n in (F, F, H))
+    B.moe_ffn_forward(cfg, x, off, w1, w3, w2, gate, up, y, ws)
+    dx, dw1, dw3, dw2 = (torch.full_like(t, 3.0) for t in (x, w1, w3, w2))
+    B.moe_ffn_backward(cfg, dy, x, off, w1, w3, w2, gate, up, dx, dw1, dw3, dw2, ws)
+    # the first group's weights are zeros, so its gates are too and nothing comes of it
+    assert not y[0].any() and not dx[0].any()
+    for d in (dw1, dw3, dw2):
+        assert not d[:-1].any()
+    X, D, W1, W3, W2 = (v.double() for v in (x[1:], dy[1:], w1[-1], w3[-1], w2[-1]))
+    A, U, dh = X @ W1, X @ W3, D @ W2.t()
+    assert A.min() >= 32 and A.max() <= 256
+    h, dg, du = rne(A * U).double(), rne(dh * U).double(), rne(dh * A).double()
+    same("gate", gate[1:], A, X.abs() @ W1.abs())
+    same("y", y[1:], h @ W2, h.abs() @ W2.abs())
+    ref, terms = dg @ W1.t() + du @ W3.t(), dg.abs() @ W1.abs().t() + du.abs() @ W3.abs().t()
+    same("dx", dx[1:, :-1], ref[:, :-1], terms[:, :-1])
+    same("dx of the last channel", dx[1:, -1], ref[:, -1], terms[:, -1], 128.0)
+    same("dw1", dw1[-1], X.t() @ dg, X.abs().t() @ dg.abs())
+    same("dw3", dw3[-1], X.t() @ du, X.abs().t() @ du.abs())
+    same("dw2", dw2[-1], h.t() @ D, h.abs().t() @ D.abs())
