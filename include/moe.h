@@ -523,6 +523,177 @@ moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const fl
                        const int32_t* group_off, const int8_t* wq, const float* w_scale, uint16_t* y, void* ws,
                        size_t ws_bytes, void* stream);
 
+/* ---- a training step around the products -------------------------------------
+ *
+ * What the layer and the blocks above leave to their user in a training step (and
+ * in serving, the norm): the norm before the layer, the gate's logits and
+ * gradients, the routing's losses, and the optimizer's step.
+ *
+ * Conventions are those of the calls over row groups: no handle, the current
+ * device, pointers on 16-byte boundaries (seq_off on its values', the workspace
+ * on 256 bytes), scratch workspaces without state, no allocation, wait or
+ * addition whose order changes from run to run, and capture into graphs.  Outputs
+ * must not overlap inputs or each other but where a call says so.
+ */
+
+/* ---- root-mean-square norm with the residual's addition ---- */
+typedef struct {
+  int32_t rows;   /* T, 0..2^22 */
+  int32_t hidden; /* H, multiple of 8, 8..16384 */
+  float eps;      /* > 0, added to the mean square */
+} moe_rms_norm_config;
+
+/* s = x + residual, rounded to bf16 (x where residual is NULL), r = 1 /
+ * sqrt(mean_h(s^2) + eps) and y = s weight r, the norm of the rounded s.
+ * x, residual: bf16 [T][H]; weight: bf16 [H].  Outputs, each NULL if not wanted,
+ * but y or q has to be:
+ *   sum    bf16 [T][H]  s
+ *   rstd   fp32 [T]     r, for the backward pass
+ *   y      bf16 [T][H]
+ *   q      int8 [T][H] and scale fp32 [T] (both or neither): y in 8 bits as
+ *          moe_quantize_rows_i8 would have it, from y in fp32
+ * sum may be x or residual, and y may be x (the same address): a row is read
+ * before it is written.  Sums are fp32: a row with magnitudes above 2^56 has an
+ * infinite mean square, r = 0 and y = 0; one with an infinity or a NaN has y = NaN
+ * wherever r or s is not finite, q = 0 and scale = NaN.  A row's results have the
+ * same bits in any batch. */
+moe_status moe_rms_norm_forward(const moe_rms_norm_config* cfg, const uint16_t* x, const uint16_t* residual,
+                                const uint16_t* weight, uint16_t* sum, float* rstd, uint16_t* y, int8_t* q,
+                                float* scale, void* stream);
+
+/* Workspace of moe_rms_norm_backward. */
+moe_status moe_rms_norm_workspace_size(const moe_rms_norm_config* cfg, size_t* bytes);
+
+/* The gradients of moe_rms_norm_forward from dy (bf16 [T][H]), the s it kept (sum,
+ * or x where there was no residual), weight and rstd:
+ *   dx[t] = r (g - n mean_h(g n)) + dsum[t],  n = s r,  g = weight dy
+ * the gradient of x and of residual alike; dsum: bf16 [T][H], the gradient that
+ * reaches sum from elsewhere, or NULL.  dweight: fp32 [H], sum_t dy n (zeros where
+ * T = 0).  dx (bf16 [T][H]) or dweight may be NULL.  dx may be dy, dsum or sum.
+ * A row of dx has the same bits in any batch. */
+moe_status moe_rms_norm_backward(const moe_rms_norm_config* cfg, const uint16_t* dy, const uint16_t* dsum,
+                                 const uint16_t* sum, const uint16_t* weight, const float* rstd, uint16_t* dx,
+                                 float* dweight, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- the gate and the routing's losses in training ----
+ *
+ * moe_route chooses experts and gives their weights; these calls give what its
+ * training needs: the logits, losses on them, and gradients back to the tokens
+ * and to the gate.
+ *
+ * seq_off: int32 [n_seqs + 1]; sequence s has rows [seq_off[s], seq_off[s + 1]),
+ * under the rules of group_off: NULL where n_seqs = 1 (every row), ascending
+ * offsets in [0, rows], any of them empty, and rows before the first or behind the
+ * last sequence are neither read nor written. */
+typedef struct {
+  int32_t rows;      /* T, 0..2^22 */
+  int32_t hidden;    /* H, multiple of 64, 64..16384 */
+  int32_t n_experts; /* E, 1..512 */
+  int32_t top_k;     /* k, 1..min(E, 8) */
+  int32_t n_seqs;    /* S, 1..MOE_MAX_GROUPS */
+} moe_router_config;
+
+/* Workspace of moe_gate_logits (backward = 0) or moe_gate_backward (1). */
+moe_status moe_gate_workspace_size(const moe_router_config* cfg, int32_t backward, size_t* bytes);
+
+/* logits[t][e] = sum_h x[t][h] wg[h][e] + logit_bias[e]: x bf16 [T][H], wg bf16
+ * [H][E], logit_bias fp32 [E] or NULL, logits fp32 [T][E].  The sum is fp32, in
+ * another order than moe_route's, so the last bits may differ from the logits that
+ * it compares.  top_k is not read. */
+moe_status moe_gate_logits(const moe_router_config* cfg, const uint16_t* x, const uint16_t* wg,
+                           const float* logit_bias, const int32_t* seq_off, float* logits, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* The gradients of moe_gate_logits from dlogits (fp32 [T][E]): dx bf16 [T][H] =
+ * dlogits wg^T, dwg bf16 [H][E] = x^T dlogits, dbias fp32 [E] = sum_t dlogits; each
+ * may be NULL.  dlogits are rounded to bf16 once for the two products (dbias adds
+ * them unrounded); sums are fp32.  Without rows dwg and dbias are 0. */
+moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits, const uint16_t* x,
+                             const uint16_t* wg, const int32_t* seq_off, uint16_t* dx, uint16_t* dwg, float* dbias,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace of moe_route_loss. */
+moe_status moe_route_loss_workspace_size(const moe_router_config* cfg, size_t* bytes);
+
+/* The losses of a routing: logits fp32 [T][E], topk_idx int32 [T][k].
+ *   counts int32 [S][E]: how often each expert is chosen in each sequence (ids
+ *          outside [0, E) count nowhere, repeated ones each time)
+ *   lse    fp32 [T]: log sum_e exp(logits)
+ *   loss   fp32 [2]: loss[0], balance: the mean over sequences that have rows of
+ *          E / (k n^2) sum_e counts[s][e] P[s][e], n the sequence's rows and P the
+ *          sums of their softmax over all experts (1 where both are even);
+ *          loss[1], z: the mean of lse^2 over the rows of all sequences.
+ * Without any rows both are 0.  A logit of -inf is an expert that cannot be chosen;
+ * a row of nothing else has lse = -inf and adds 0 to both sums.  A row with a NaN
+ * or +inf has lse = NaN, and so have the losses it enters.  hidden is not read. */
+moe_status moe_route_loss(const moe_router_config* cfg, const float* logits, const int32_t* topk_idx,
+                          const int32_t* seq_off, int32_t* counts, float* lse, float* loss, void* ws, size_t ws_bytes,
+                          void* stream);
+
+/* dlogits fp32 [T][E] from the losses' gradients dloss (fp32 [2], device: the
+ * coefficients times whatever the losses are scaled by; NULL: zeros) and from the
+ * gradient dtopk_w (fp32 [T][k]) of moe_route's topk_w (fp32 [T][k]; both or
+ * neither).  With p = exp(logits - lse), c = counts of the row's sequence, of n rows,
+ * S' sequences and N rows in all:
+ *   dloss[0] E / (k n^2 S') p_e (c_e - sum_i c_i p_i) + dloss[1] 2 / N lse p_e
+ *   + sum over j with topk_idx[j] = e of w_j (dw_j - sum_i w_i dw_i)
+ * (the counts are constants; the weights are the softmax over the chosen logits).
+ * counts and lse as moe_route_loss gave them.  A row of -inf alone has gradient 0.
+ * dlogits may be logits (the same address). */
+moe_status moe_route_loss_backward(const moe_router_config* cfg, const float* logits, const int32_t* topk_idx,
+                                   const float* topk_w, const int32_t* seq_off, const int32_t* counts,
+                                   const float* lse, const float* dloss, const float* dtopk_w, float* dlogits,
+                                   void* stream);
+
+/* ---- AdamW over many tensors ---- */
+typedef struct {
+  float lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps > 0 */
+  float grad_scale;            /* gradients are multiplied by it */
+  int32_t step;                /* t, counted from 1 */
+  uint32_t seed;               /* of what is rounded at random */
+  int32_t state_bits;          /* 32 or 8 */
+} moe_adamw_config;
+
+#define MOE_ADAMW_BLOCK 256
+
+/* One tensor of n values.  param: bf16, or NULL; master: the same weights in fp32,
+ * or NULL (param alone is stepped then); at least one of them.  grad: bf16, or fp32
+ * where grad_fp32 = 1.  m, v: fp32, or 8 bits each: m in e4m3, v in e5m2 (OCP), times
+ * a scale for every MOE_ADAMW_BLOCK consecutive values, m_scale and v_scale: fp32
+ * [ceil(n / 256)] (NULL with 32 bits).  All zeros is the state before the first step. */
+typedef struct {
+  int64_t n; /* 0..2^40 */
+  uint16_t* param;
+  float* master;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  float weight_decay; /* >= 0 */
+  int32_t grad_fp32;  /* 0 or 1 */
+} moe_adamw_tensor;
+
+/* One step for every tensor (host array of n_tensors, copied before the call
+ * returns), in place:
+ *   g = grad_scale grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   w -= lr (weight_decay w + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+ * in fp32, from m and v before they are rounded.  now: NULL, or device memory with
+ * three fp32 values, lr, grad_scale and step, in place of the config's (a captured
+ * step reads them at each replay; a step below 1 counts as 1).  A grad_scale there
+ * that is NaN leaves every tensor as it was: a step to be skipped.
+ *
+ * master's rounded value goes to param; param alone, and states in 8 bits, are
+ * rounded up or down at random, with the probabilities that keep their means (to
+ * the nearest, an average that moves by less than half a step would stand still).
+ * The random bits are a function of (seed, step, the tensor's place in the list, the
+ * value's place in it), so a step gives the same bits wherever it runs.  An 8-bit
+ * block's scale is its largest magnitude / 448 (m) or / 57344 (v); a block below
+ * 2^-110 is 0; a v above 0 stays above 0; a block that holds an infinity or a NaN
+ * gets scale NaN, so that it stays NaN.  A tensor must not be in the list twice. */
+moe_status moe_adamw(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors, int32_t n_tensors, const float* now,
+                     void* stream);
+
 #ifdef __cplusplus
 }
 #endif

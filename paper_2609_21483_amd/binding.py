@@ -85,6 +85,27 @@ class moe_gemm_i8_config(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("rows", "depth", "channels", "n_groups", "act")]
 
 
+class moe_rms_norm_config(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("hidden", C.c_int32), ("eps", C.c_float)]
+
+
+class moe_router_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "hidden", "n_experts", "top_k", "n_seqs")]
+
+
+MOE_ADAMW_BLOCK = 256
+
+
+class moe_adamw_config(C.Structure):
+    _fields_ = [(n, C.c_float) for n in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [
+        ("step", C.c_int32), ("seed", C.c_uint32), ("state_bits", C.c_int32)]
+
+
+class moe_adamw_tensor(C.Structure):
+    _fields_ = [("n", C.c_int64)] + [(n, C.c_void_p) for n in ("param", "master", "grad", "m", "v", "m_scale", "v_scale")] + [
+        ("weight_decay", C.c_float), ("grad_fp32", C.c_int32)]
+
+
 MOE_TILES = ("few4", "few8", "small", "wide")
 
 
@@ -145,6 +166,16 @@ _SIGS = {
     "moe_quantize_weights_i8": ([C.c_int32] * 5 + [_P, _P, _P, _P], C.c_int),
     "moe_gemm_i8_workspace_size": ([C.POINTER(moe_gemm_i8_config), C.POINTER(C.c_size_t)], C.c_int),
     "moe_gemm_i8_plan_host": ([C.POINTER(moe_gemm_i8_config), C.POINTER(moe_product_plan)], C.c_int),
+    "moe_rms_norm_forward": ([C.POINTER(moe_rms_norm_config)] + [_P] * 9, C.c_int),
+    "moe_rms_norm_workspace_size": ([C.POINTER(moe_rms_norm_config), C.POINTER(C.c_size_t)], C.c_int),
+    "moe_rms_norm_backward": ([C.POINTER(moe_rms_norm_config)] + [_P] * 8 + [C.c_size_t, _P], C.c_int),
+    "moe_gate_workspace_size": ([C.POINTER(moe_router_config), C.c_int32, C.POINTER(C.c_size_t)], C.c_int),
+    "moe_gate_logits": ([C.POINTER(moe_router_config)] + [_P] * 6 + [C.c_size_t, _P], C.c_int),
+    "moe_gate_backward": ([C.POINTER(moe_router_config)] + [_P] * 8 + [C.c_size_t, _P], C.c_int),
+    "moe_route_loss_workspace_size": ([C.POINTER(moe_router_config), C.POINTER(C.c_size_t)], C.c_int),
+    "moe_route_loss": ([C.POINTER(moe_router_config)] + [_P] * 7 + [C.c_size_t, _P], C.c_int),
+    "moe_route_loss_backward": ([C.POINTER(moe_router_config)] + [_P] * 10, C.c_int),
+    "moe_adamw": ([C.POINTER(moe_adamw_config), C.POINTER(moe_adamw_tensor), C.c_int32, _P, _P], C.c_int),
     "moe_gemm_i8": ([C.POINTER(moe_gemm_i8_config)] + [_P] * 7 + [C.c_size_t, _P], C.c_int),
 }
 for _name, (_args, _res) in _SIGS.items():
@@ -481,6 +512,160 @@ def moe_gemm_i8(cfg: moe_gemm_i8_config, xq, x_scale, group_off, wq, w_scale, y,
           _arg("x_scale", x_scale, torch.float32, (T,), dev), _off(group_off, G, dev),
           _arg("wq", wq, torch.int8, (G, N, K), dev), _arg("w_scale", w_scale, torch.float32, (G, N), dev),
           _arg("y", y, torch.bfloat16, (T, out), dev), *_ws(ws, dev))
+
+
+# A training step around the products: the norm, the gate and the routing's losses, the optimizer.
+
+def _opt(name: str, t: Optional[torch.Tensor], dtype: torch.dtype, want, dev: int) -> Optional[int]:
+    return None if t is None else _arg(name, t, dtype, want, dev)
+
+
+def _size(call: str, cfg, *args) -> int:
+    n = C.c_size_t()
+    _check(call, getattr(_lib, call)(C.byref(cfg), *args, C.byref(n)))
+    return n.value
+
+
+def moe_rms_norm_forward(cfg: moe_rms_norm_config, x, residual, weight, sum, rstd, y, q, scale, stream=None) -> None:
+    dev, bf, f32 = _device_of("x", x), torch.bfloat16, torch.float32
+    T, TH = (cfg.rows,), (cfg.rows, cfg.hidden)
+    _call("moe_rms_norm_forward", dev, stream, cfg, _arg("x", x, bf, TH, dev), _opt("residual", residual, bf, TH, dev),
+          _arg("weight", weight, bf, (cfg.hidden,), dev), _opt("sum", sum, bf, TH, dev), _opt("rstd", rstd, f32, T, dev),
+          _opt("y", y, bf, TH, dev), _opt("q", q, torch.int8, TH, dev), _opt("scale", scale, f32, T, dev))
+
+
+def moe_rms_norm_workspace_size(cfg: moe_rms_norm_config) -> int:
+    return _size("moe_rms_norm_workspace_size", cfg)
+
+
+def moe_rms_norm_backward(cfg: moe_rms_norm_config, dy, dsum, sum, weight, rstd, dx, dweight, ws, stream=None) -> None:
+    dev, bf, f32 = _device_of("dy", dy), torch.bfloat16, torch.float32
+    TH, H = (cfg.rows, cfg.hidden), (cfg.hidden,)
+    _call("moe_rms_norm_backward", dev, stream, cfg, _arg("dy", dy, bf, TH, dev), _opt("dsum", dsum, bf, TH, dev),
+          _arg("sum", sum, bf, TH, dev), _arg("weight", weight, bf, H, dev), _arg("rstd", rstd, f32, (cfg.rows,), dev),
+          _opt("dx", dx, bf, TH, dev), _opt("dweight", dweight, f32, H, dev), *_ws(ws, dev))
+
+
+def moe_gate_workspace_size(cfg: moe_router_config, backward: bool = False) -> int:
+    return _size("moe_gate_workspace_size", cfg, int(backward))
+
+
+def moe_gate_logits(cfg: moe_router_config, x, wg, logit_bias, seq_off, logits, ws, stream=None) -> None:
+    dev, bf, f32 = _device_of("x", x), torch.bfloat16, torch.float32
+    T, H, E = cfg.rows, cfg.hidden, cfg.n_experts
+    _call("moe_gate_logits", dev, stream, cfg, _arg("x", x, bf, (T, H), dev), _arg("wg", wg, bf, (H, E), dev),
+          _opt("logit_bias", logit_bias, f32, (E,), dev), _seq(seq_off, cfg.n_seqs, dev),
+          _arg("logits", logits, f32, (T, E), dev), *_ws(ws, dev))
+
+
+def moe_gate_backward(cfg: moe_router_config, dlogits, x, wg, seq_off, dx, dwg, dbias, ws, stream=None) -> None:
+    """x may be None where dwg is, and wg where dx is."""
+    dev, bf, f32 = _device_of("dlogits", dlogits), torch.bfloat16, torch.float32
+    T, H, E = cfg.rows, cfg.hidden, cfg.n_experts
+    _call("moe_gate_backward", dev, stream, cfg, _arg("dlogits", dlogits, f32, (T, E), dev),
+          _opt("x", x, bf, (T, H), dev), _opt("wg", wg, bf, (H, E), dev), _seq(seq_off, cfg.n_seqs, dev),
+          _opt("dx", dx, bf, (T, H), dev), _opt("dwg", dwg, bf, (H, E), dev), _opt("dbias", dbias, f32, (E,), dev),
+          *_ws(ws, dev))
+
+
+def _seq(t: Optional[torch.Tensor], n_seqs: int, dev: int) -> Optional[int]:
+    return None if t is None and n_seqs == 1 else _arg("seq_off", t, torch.int32, (n_seqs + 1,), dev)
+
+
+def moe_route_loss_workspace_size(cfg: moe_router_config) -> int:
+    return _size("moe_route_loss_workspace_size", cfg)
+
+
+def moe_route_loss(cfg: moe_router_config, logits, topk_idx, seq_off, counts, lse, loss, ws, stream=None) -> None:
+    dev, i32, f32 = _device_of("logits", logits), torch.int32, torch.float32
+    T, E = cfg.rows, cfg.n_experts
+    _call("moe_route_loss", dev, stream, cfg, _arg("logits", logits, f32, (T, E), dev),
+          _arg("topk_idx", topk_idx, i32, (T, cfg.top_k), dev), _seq(seq_off, cfg.n_seqs, dev),
+          _arg("counts", counts, i32, (cfg.n_seqs, E), dev), _arg("lse", lse, f32, (T,), dev),
+          _arg("loss", loss, f32, (2,), dev), *_ws(ws, dev))
+
+
+def moe_route_loss_backward(cfg: moe_router_config, logits, topk_idx, topk_w, seq_off, counts, lse, dloss, dtopk_w, dlogits,
+                            stream=None) -> None:
+    dev, i32, f32 = _device_of("logits", logits), torch.int32, torch.float32
+    T, E, k = cfg.rows, cfg.n_experts, cfg.top_k
+    _call("moe_route_loss_backward", dev, stream, cfg, _arg("logits", logits, f32, (T, E), dev),
+          _arg("topk_idx", topk_idx, i32, (T, k), dev), _opt("topk_w", topk_w, f32, (T, k), dev),
+          _seq(seq_off, cfg.n_seqs, dev), _arg("counts", counts, i32, (cfg.n_seqs, E), dev),
+          _arg("lse", lse, f32, (T,), dev), _opt("dloss", dloss, f32, (2,), dev),
+          _opt("dtopk_w", dtopk_w, f32, (T, k), dev), _arg("dlogits", dlogits, f32, (T, E), dev))
+
+
+class AdamwTensors:
+    """The list that moe_adamw takes, checked and laid out once; it keeps the tensors alive."""
+
+    def __init__(self, array, state_bits: int, device: Optional[int], tensors):
+        self.array, self.state_bits, self.device, self.tensors = array, state_bits, device, tensors
+
+    def __len__(self):
+        return len(self.array)
+
+
+def moe_adamw_tensors(tensors, state_bits: int) -> AdamwTensors:
+    """tensors: a dict each, of param (bf16) and/or master (fp32), grad (bf16 or fp32), m and v (fp32, or torch.float8_e4m3fn
+    and torch.float8_e5m2 with the fp32 scales m_scale and v_scale of every 256 values) and weight_decay (default 0).  All
+    have as many values as grad and lie on one device."""
+    names = ("param", "master", "grad", "m", "v", "m_scale", "v_scale")
+    f32 = torch.float32
+    if state_bits not in (8, 32):
+        raise ValueError(f"state_bits must be 8 or 32, not {state_bits}")
+    kinds = dict(param=torch.bfloat16, master=f32, m=f32, v=f32, m_scale=f32, v_scale=f32)
+    if state_bits == 8:
+        kinds.update(m=torch.float8_e4m3fn, v=torch.float8_e5m2)
+    tensors = [dict(t) for t in tensors]
+    array = (moe_adamw_tensor * len(tensors))()
+    dev, spans = None, []  # spans: first and last byte, whether written, what
+    for i, t in enumerate(tensors):
+        unknown = set(t) - {*names, "weight_decay"}
+        if unknown:
+            raise ValueError(f"tensor {i}: unknown {sorted(unknown)}")
+        grad = t.get("grad")
+        dev = _device_of(f"grad of tensor {i}", grad) if dev is None else dev
+        if grad is None or grad.dtype not in (torch.bfloat16, f32):
+            raise ValueError(f"tensor {i}: grad must be bf16 or fp32")
+        if t.get("param") is None and t.get("master") is None:
+            raise ValueError(f"tensor {i}: param or master is needed")
+        n, c = grad.numel(), array[i]
+        c.n, c.weight_decay, c.grad_fp32 = n, float(t.get("weight_decay", 0.0)), int(grad.dtype is f32)
+        c.grad = _arg(f"grad of tensor {i}", grad, grad.dtype, grad.shape, dev)
+        spans.append((c.grad or 0, (c.grad or 0) + grad.nbytes - 1, False, f"grad of tensor {i}"))
+        for name, kind in kinds.items():
+            v = t.get(name)
+            if name.endswith("_scale") and state_bits == 32:
+                if v is not None:
+                    raise ValueError(f"tensor {i}: states in 32 bits have no {name}")
+                continue
+            if v is None and name in ("param", "master"):
+                continue
+            want = (-(-n // MOE_ADAMW_BLOCK),) if name.endswith("_scale") else grad.shape
+            at = _arg(f"{name} of tensor {i}", v, kind, want, dev)
+            setattr(c, name, at)
+            spans.append((at or 0, (at or 0) + v.nbytes - 1, True, f"{name} of tensor {i}"))
+    # what is written is in the list once, and nobody's gradient
+    written, read = (-1, ""), (-1, "")
+    for first, last, writes, what in sorted(s for s in spans if s[1] >= s[0]):
+        for end, other in (written, read) if writes else (written,):
+            if first <= end:
+                raise ValueError(f"{what} overlaps the {other}")
+        if writes:
+            written = max(written, (last, what))
+        else:
+            read = max(read, (last, what))
+    return AdamwTensors(array, state_bits, dev, tensors)
+
+
+def moe_adamw(cfg: moe_adamw_config, tensors: AdamwTensors, now=None, stream=None) -> None:
+    if cfg.state_bits != tensors.state_bits:
+        raise ValueError(f"the config has states in {cfg.state_bits} bits, the tensors in {tensors.state_bits}")
+    if tensors.device is None:
+        return
+    _call("moe_adamw", tensors.device, stream, cfg, tensors.array, len(tensors),
+          _opt("now", now, torch.float32, (3,), tensors.device))
 
 
 # ---- convenience --------------------------------------------------------------

@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe.so")
-SOURCES = ["gate.hip", "gate_filter.hip", "route.hip", "forward.hip", "ffn.hip", "int8.hip", "api.hip"]
+SOURCES = ["gate.hip", "gate_filter.hip", "route.hip", "forward.hip", "ffn.hip", "int8.hip", "norm.hip", "router.hip", "adamw.hip", "api.hip"]
 ARCH = os.environ.get("MOE_OFFLOAD_ARCH", "gfx950")
 
 HIPCC_FLAGS = [

@@ -95,6 +95,20 @@ struct RowTiles {
     return {__builtin_amdgcn_readlane(group, src), __builtin_amdgcn_readlane(begin, src),
             __builtin_amdgcn_readlane(end, src), __builtin_amdgcn_readlane(tiles, src)};
   }
+
+  // the tiles of the groups before group g
+  __device__ __forceinline__ int before(int g) const {
+    if (!off) return 0;
+    int t = incl - n;
+    const bool mine = g >= g0 && g < g1;
+    if (mine)
+      for (int i = g0, a = first; i < g; ++i) {
+        const int e = max(a, clamp_off(off[i + 1], T));
+        t += ceil_div(e - a, bm);
+        a = e;
+      }
+    return __builtin_amdgcn_readlane(t, __ffsll((unsigned long long)__ballot(mine)) - 1);
+  }
 };
 
 // The group of rank r by its number of rows, the largest first (equal ones in
@@ -161,6 +175,23 @@ __device__ __forceinline__ void act_grad(float v, int act, float* a, float* da) 
   // (t is 0 where s is 0 or 1, and dz may be infinite there)
   *da = t == 0.0f ? s : s + v * t * dz;
 }
+
+// ---- 8-bit values ------------------------------------------------------------
+// The quotient of a value by its row's scale, rounded to a whole number as the
+// IEEE quotient would be.  The value times the hardware reciprocal is within
+// 127 * 3 * 2^-24 < 3e-5 of it, so only where that lies within 1e-4 of a half
+// does the division itself decide (about 1 value in 5000).
+struct Quantizer {
+  float scale, inv;
+  bool slow;  // a tiny scale, whose reciprocal may be infinite and whose values subnormal: always divided
+  __device__ __forceinline__ explicit Quantizer(float s) : scale(s), inv(__builtin_amdgcn_rcpf(s)), slow(s < 0x1p-100f) {}
+  __device__ __forceinline__ int operator()(float v) const {
+    float q = v * inv, r = rintf(q);
+    if (slow || fabsf(q - r) > 0.4999f) r = rintf(v / scale);
+    // (a scale rounded down in the subnormal range can give a quotient above 127)
+    return (int)fminf(fmaxf(r, -127.0f), 127.0f);
+  }
+};
 
 // ---- host checks ----------------------------------------------------------------
 inline bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }

@@ -19,21 +19,6 @@ constexpr uint32_t BF16_INF = 0x7f80;
 __device__ __forceinline__ float scale_of(uint32_t amax) {
   return amax >= BF16_INF ? __builtin_nanf("") : bf16_to_f32((uint16_t)amax) / 127.0f;
 }
-// The quotient of a value by its row's scale, rounded to a whole number as the
-// IEEE quotient would be.  The value times the hardware reciprocal is within
-// 127 * 3 * 2^-24 < 3e-5 of it, so only where that lies within 1e-4 of a half
-// does the division itself decide (about 1 value in 5000).
-struct Quantizer {
-  float scale, inv;
-  bool slow;  // a tiny scale, whose reciprocal may be infinite and whose values subnormal: always divided
-  __device__ __forceinline__ explicit Quantizer(float s) : scale(s), inv(__builtin_amdgcn_rcpf(s)), slow(s < 0x1p-100f) {}
-  __device__ __forceinline__ int operator()(float v) const {
-    float q = v * inv, r = rintf(q);
-    if (slow || fabsf(q - r) > 0.4999f) r = rintf(v / scale);
-    // (a scale rounded down in the subnormal range can give a quotient above 127)
-    return (int)fminf(fmaxf(r, -127.0f), 127.0f);
-  }
-};
 
 // One row by THREADS threads, held in registers: each takes LOADS pieces of 8
 // values.  Bound by memory: 16384 x 14336 in 124 us, 5.7 TB/s (2 bytes read and

@@ -1,0 +1,307 @@
+// Root-mean-square norm with the residual's addition, in bf16 or in 8 bits, and
+// its backward pass (moe.h).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "blocks.h"
+#include "tile.h"
+
+using namespace moe;
+
+namespace {
+
+struct NormArgs {
+  int T, H;
+  float eps;
+  const uint16_t *x, *residual, *weight;
+  uint16_t *sum, *y;
+  float* rstd;
+  int8_t* q;
+  float* scale;
+};
+
+struct NormGradArgs {
+  int T, H;
+  const uint16_t *dy, *dsum, *sum, *weight;
+  const float* rstd;
+  uint16_t* dx;
+  float *dweight, *part;  // part: [parts][H]
+  int parts;
+};
+
+// Sum and largest of (a, m) over the THREADS threads of a row.  red: a slot for
+// each wavefront; a caller in a loop takes two sets in turn.
+template <int THREADS>
+__device__ __forceinline__ void reduce(float& a, uint32_t& m, float* red_a, uint32_t* red_m) {
+#pragma unroll
+  for (int d = (THREADS < 64 ? THREADS : 64) / 2; d; d >>= 1) {
+    a += __shfl_xor(a, d);
+    m = max(m, (uint32_t)__shfl_xor((int)m, d));
+  }
+  if constexpr (THREADS > 64) {
+    if (threadIdx.x % 64 == 0) {
+      red_a[threadIdx.x / 64] = a;
+      red_m[threadIdx.x / 64] = m;
+    }
+    __syncthreads();
+    a = red_a[0], m = red_m[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 64; ++i) {
+      a += red_a[i];
+      m = max(m, red_m[i]);
+    }
+  }
+}
+
+// One row by THREADS threads, held in registers: LOADS pieces of 8 values each.
+// s w is exact in fp32 (two bf16 values), so y = (s w) r is rounded once, and the
+// largest |y| is the largest |s w| times r.
+template <int THREADS, int LOADS>
+__global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
+  constexpr int PER = 256 / THREADS;  // rows of a workgroup
+  __shared__ float red_a[4];
+  __shared__ uint32_t red_m[4];
+  const int t = threadIdx.x % THREADS, row = blockIdx.x * PER + threadIdx.x / THREADS;
+  const bool some = row < a.T;
+  const size_t at = (size_t)row * a.H;
+  u32x4_t s[LOADS], r[LOADS], w[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int c = (t + i * THREADS) * 8;
+    const bool in = some && c < a.H;
+    s[i] = in ? *reinterpret_cast<const u32x4_t*>(a.x + at + c) : u32x4_t{0, 0, 0, 0};
+    r[i] = in && a.residual ? *reinterpret_cast<const u32x4_t*>(a.residual + at + c) : u32x4_t{0, 0, 0, 0};
+    w[i] = in ? *reinterpret_cast<const u32x4_t*>(a.weight + c) : u32x4_t{0, 0, 0, 0};
+  }
+  float squares = 0;
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    float v[8], g[8];
+    tile::unpack8(s[i], v);
+    if (a.residual) {
+      tile::unpack8(r[i], g);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += g[j];
+      s[i] = tile::pack8(v);
+      tile::unpack8(s[i], v);
+    }
+    tile::unpack8(w[i], g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      squares += v[j] * v[j];
+      most = max(most, __float_as_uint(v[j] * g[j]) & 0x7fffffffu);
+    }
+  }
+  reduce<THREADS>(squares, most, red_a, red_m);
+  if (!some) return;
+  const float rstd = 1.0f / sqrtf(squares / a.H + a.eps);
+  float scale = 0;
+  if (a.q) {
+    scale = __uint_as_float(most) * rstd;
+    scale = scale < __builtin_inff() ? scale / 127.0f : __builtin_nanf("");
+  }
+  if (t == 0) {
+    if (a.rstd) a.rstd[row] = rstd;
+    if (a.q) a.scale[row] = scale;
+  }
+  const bool zero = !(scale > 0.0f);
+  const Quantizer quant(scale);
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int c = (t + i * THREADS) * 8;
+    if (c >= a.H) break;
+    if (a.sum) *reinterpret_cast<u32x4_t*>(a.sum + at + c) = s[i];
+    float v[8], g[8];
+    tile::unpack8(s[i], v);
+    tile::unpack8(w[i], g);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = v[j] * g[j] * rstd;
+    if (a.y) *reinterpret_cast<u32x4_t*>(a.y + at + c) = tile::pack8(v);
+    if (a.q) {
+      uint32_t p[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        p[j] = zero ? 0u
+                    : (uint32_t)(quant(v[4 * j]) & 255) | (uint32_t)(quant(v[4 * j + 1]) & 255) << 8 |
+                          (uint32_t)(quant(v[4 * j + 2]) & 255) << 16 | (uint32_t)quant(v[4 * j + 3]) << 24;
+      *reinterpret_cast<uint2*>(a.q + at + c) = uint2{p[0], p[1]};
+    }
+  }
+}
+
+// dx row by row, and each group of threads' part of dweight over its rows.
+template <int THREADS, int LOADS>
+__global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
+  constexpr int PER = 256 / THREADS;
+  __shared__ float red_a[2][4];
+  __shared__ uint32_t red_m[2][4];
+  const int t = threadIdx.x % THREADS, part = blockIdx.x * PER + threadIdx.x / THREADS;
+  u32x4_t w[LOADS];
+  float dw[LOADS][8] = {};
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int c = (t + i * THREADS) * 8;
+    w[i] = c < a.H ? *reinterpret_cast<const u32x4_t*>(a.weight + c) : u32x4_t{0, 0, 0, 0};
+  }
+  int turn = 0;
+  for (int row0 = blockIdx.x * PER; row0 < a.T; row0 += a.parts, turn ^= 1) {
+    const int row = row0 + threadIdx.x / THREADS;
+    const bool some = row < a.T;
+    const size_t at = (size_t)row * a.H;
+    const float r = some ? a.rstd[row] : 0.0f;
+    u32x4_t d[LOADS], s[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int c = (t + i * THREADS) * 8;
+      const bool in = some && c < a.H;
+      d[i] = in ? *reinterpret_cast<const u32x4_t*>(a.dy + at + c) : u32x4_t{0, 0, 0, 0};
+      s[i] = in ? *reinterpret_cast<const u32x4_t*>(a.sum + at + c) : u32x4_t{0, 0, 0, 0};
+    }
+    float dot = 0;
+    uint32_t none = 0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      float dv[8], sv[8], wv[8];
+      tile::unpack8(d[i], dv);
+      tile::unpack8(s[i], sv);
+      tile::unpack8(w[i], wv);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float n = sv[j] * r;
+        dw[i][j] += dv[j] * n;
+        dot += dv[j] * wv[j] * n;
+      }
+    }
+    if (!a.dx) continue;
+    reduce<THREADS>(dot, none, red_a[turn], red_m[turn]);
+    const float c0 = dot / a.H;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int c = (t + i * THREADS) * 8;
+      if (!some || c >= a.H) break;
+      float dv[8], sv[8], wv[8];
+      tile::unpack8(d[i], dv);
+      tile::unpack8(s[i], sv);
+      tile::unpack8(w[i], wv);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dv[j] = r * (dv[j] * wv[j] - sv[j] * r * c0);
+      if (a.dsum) {
+        tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.dsum + at + c), sv);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) dv[j] += sv[j];
+      }
+      *reinterpret_cast<u32x4_t*>(a.dx + at + c) = tile::pack8(dv);
+    }
+  }
+  if (!a.dweight) return;
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int c = (t + i * THREADS) * 8;
+    if (c >= a.H) break;
+    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part + (size_t)part * a.H + c);
+    p[0] = f32x4_t{dw[i][0], dw[i][1], dw[i][2], dw[i][3]};
+    p[1] = f32x4_t{dw[i][4], dw[i][5], dw[i][6], dw[i][7]};
+  }
+}
+
+__global__ __launch_bounds__(256) void rms_norm_dweight_kernel(NormGradArgs a) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= a.H) return;
+  float v = 0;
+  for (int i = 0; i < a.parts; ++i) v += a.part[(size_t)i * a.H + c];
+  a.dweight[c] = v;
+}
+
+// fn(constants THREADS and LOADS) for rows of H values
+template <typename Fn>
+void for_width(int H, Fn&& fn) {
+  using std::integral_constant;
+  if (H <= 128) fn(integral_constant<int, 16>(), integral_constant<int, 1>());
+  else if (H <= 512) fn(integral_constant<int, 64>(), integral_constant<int, 1>());
+  else if (H <= 1024) fn(integral_constant<int, 64>(), integral_constant<int, 2>());
+  else if (H <= 2048) fn(integral_constant<int, 256>(), integral_constant<int, 1>());
+  else if (H <= 4096) fn(integral_constant<int, 256>(), integral_constant<int, 2>());
+  else if (H <= 8192) fn(integral_constant<int, 256>(), integral_constant<int, 4>());
+  else fn(integral_constant<int, 256>(), integral_constant<int, 8>());
+}
+
+// Parts of dweight's sum: the groups of threads that share the rows.
+int grad_parts(int T, int H) {
+  int per = 1;
+  for_width(H, [&](auto threads, auto) { per = 256 / threads(); });
+  return std::min(ceil_div(T, per), 1024) * per;
+}
+
+moe_status check_cfg(const moe_rms_norm_config* c) {
+  if (!c) return fail(MOE_ERR_INVALID_ARG, "config is NULL");
+  if (c->rows < 0 || c->rows > (1 << 22)) return fail(MOE_ERR_INVALID_ARG, "rows must be in [0, 2^22]");
+  if (c->hidden < 8 || c->hidden % 8 || c->hidden > 16384)
+    return fail(MOE_ERR_INVALID_ARG, "hidden must be a multiple of 8 in [8, 16384]");
+  if (!(c->eps > 0.0f) || !(c->eps < __builtin_inff())) return fail(MOE_ERR_INVALID_ARG, "eps must be above 0 and finite");
+  return MOE_OK;
+}
+
+size_t ws_size(const moe_rms_norm_config* c) {
+  return 256 + sizeof(float) * (size_t)grad_parts(c->rows, c->hidden) * c->hidden;
+}
+
+}  // namespace
+
+extern "C" {
+
+moe_status moe_rms_norm_forward(const moe_rms_norm_config* cfg, const uint16_t* x, const uint16_t* residual,
+                                const uint16_t* weight, uint16_t* sum, float* rstd, uint16_t* y, int8_t* q,
+                                float* scale, void* stream) {
+  moe_status st = check_cfg(cfg);
+  if (st != MOE_OK) return st;
+  if (cfg->rows == 0) return MOE_OK;
+  if (!x || !weight) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
+  if (!y && !q) return fail(MOE_ERR_INVALID_ARG, "y or q is wanted, or both");
+  if (!q != !scale) return fail(MOE_ERR_INVALID_ARG, "q and scale are wanted both or neither");
+  for (const void* p : {(const void*)x, (const void*)residual, (const void*)weight, (const void*)sum, (const void*)rstd,
+                        (const void*)y, (const void*)q, (const void*)scale})
+    if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
+  const NormArgs a{cfg->rows, cfg->hidden, cfg->eps, x, residual, weight, sum, y, rstd, q, scale};
+  for_width(a.H, [&](auto threads, auto loads) {
+    rms_norm_kernel<threads(), loads()>
+        <<<ceil_div(a.T, 256 / threads()), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+  });
+  HIP_TRY(hipGetLastError());
+  return MOE_OK;
+}
+
+moe_status moe_rms_norm_workspace_size(const moe_rms_norm_config* cfg, size_t* bytes) {
+  moe_status st = check_cfg(cfg);
+  if (st != MOE_OK) return st;
+  if (!bytes) return fail(MOE_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = ws_size(cfg);
+  return MOE_OK;
+}
+
+moe_status moe_rms_norm_backward(const moe_rms_norm_config* cfg, const uint16_t* dy, const uint16_t* dsum,
+                                 const uint16_t* sum, const uint16_t* weight, const float* rstd, uint16_t* dx,
+                                 float* dweight, void* ws, size_t ws_bytes, void* stream) {
+  moe_status st = check_cfg(cfg);
+  if (st != MOE_OK) return st;
+  if (cfg->rows > 0 && (!dy || !sum || !weight || !rstd)) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
+  for (const void* p : {(const void*)dy, (const void*)dsum, (const void*)sum, (const void*)weight, (const void*)rstd,
+                        (const void*)dx, (const void*)dweight})
+    if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
+  if (!ws || ws_bytes < ws_size(cfg))
+    return fail(MOE_ERR_INVALID_ARG, "the workspace holds %zu of %zu bytes", ws ? ws_bytes : 0, ws_size(cfg));
+  if (reinterpret_cast<uintptr_t>(ws) % 256) return fail(MOE_ERR_INVALID_ARG, "the workspace must be 256-byte aligned");
+  NormGradArgs a{cfg->rows, cfg->hidden, dy, dsum, sum, weight, rstd, dx, dweight, static_cast<float*>(ws),
+                 grad_parts(cfg->rows, cfg->hidden)};
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (a.T > 0 && (dx || dweight))
+    for_width(a.H, [&](auto threads, auto loads) {
+      rms_norm_grad_kernel<threads(), loads()><<<a.parts / (256 / threads()), 256, 0, s>>>(a);
+    });
+  if (dweight) rms_norm_dweight_kernel<<<ceil_div(a.H, 256), 256, 0, s>>>(a);
+  HIP_TRY(hipGetLastError());
+  return MOE_OK;
+}
+
+}  // extern "C"
