@@ -647,11 +647,11 @@ moe_status moe_route_loss_backward(const moe_router_config* cfg, const float* lo
 
 /* ---- AdamW over many tensors ---- */
 typedef struct {
-  float lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps > 0 */
-  float grad_scale;            /* gradients are multiplied by it */
-  int32_t step;                /* t, counted from 1 */
-  uint32_t seed;               /* of what is rounded at random */
-  int32_t state_bits;          /* 32 or 8 */
+  double lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps >= 1e-15 */
+  double grad_scale;            /* gradients are multiplied by it */
+  int32_t step;                 /* t, counted from 1 */
+  uint32_t seed;                /* of what is rounded at random */
+  int32_t state_bits;           /* 32 or 8 */
 } moe_adamw_config;
 
 #define MOE_ADAMW_BLOCK 256

@@ -97,7 +97,7 @@ MOE_ADAMW_BLOCK = 256
 
 
 class moe_adamw_config(C.Structure):
-    _fields_ = [(n, C.c_float) for n in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [
+    _fields_ = [(n, C.c_double) for n in ("lr", "beta1", "beta2", "eps", "grad_scale")] + [
         ("step", C.c_int32), ("seed", C.c_uint32), ("state_bits", C.c_int32)]
 
 

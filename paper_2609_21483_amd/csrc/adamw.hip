@@ -10,9 +10,8 @@ using namespace moe;
 
 namespace {
 
-constexpr int PIECE = 16;          // consecutive values of a thread
-constexpr int CHUNK = 256 * PIECE;  // values of a workgroup
-constexpr int LANES = MOE_ADAMW_BLOCK / PIECE;  // threads that share an 8-bit block
+constexpr int VALUES = 16;           // of a thread
+constexpr int CHUNK = 256 * VALUES;  // of a workgroup
 // Tensors of a launch: their addresses are kernel arguments (4 KB at most), so
 // that no table has to reach the device before the step.
 constexpr int MOST = 48;
@@ -32,7 +31,7 @@ struct Tensor {
 
 struct AdamArgs {
   const float* now;
-  float lr, scale, step, log_b1, log_b2, b1, b2, eps;
+  float lr, scale, step, log_b1, log_b2, b1, b2, rest1, rest2, eps;  // rest: 1 - beta
   uint32_t seed;
   int count;           // tensors of this launch
   uint32_t end[MOST];  // chunks of the tensors up to and with each
@@ -52,114 +51,281 @@ __device__ __forceinline__ uint32_t mixed(uint32_t h) {
 
 // ---- 8-bit values -----------------------------------------------------------------
 // x in [0, 448] or [0, 57344] to e4m3 or e5m2, up with probability (distance to
-// the lower neighbour) / (step): 16 random bits are added below the mantissa that
-// stays, or below the unit of the subnormals.
+// the lower neighbour) / (step): 16 random bits r are added below the mantissa
+// that stays.  Below the smallest normal value the steps are those of its
+// binade, so x is rounded as x + that value and 8 (4) steps are taken off.
 __device__ __forceinline__ uint32_t to_e4m3(float x, uint32_t r) {
-  const uint32_t normal = ((__float_as_uint(x) + (r << 4)) >> 20) - (120u << 3);
-  const uint32_t tiny = (uint32_t)(x * 512.0f + (float)r * 0x1p-16f);
-  return min(x < 0x1p-6f ? tiny : normal, 0x7Eu);
+  const bool tiny = x < 0x1p-6f;
+  const uint32_t bits = __float_as_uint(tiny ? x + 0x1p-6f : x) + (r << 4);
+  return min((bits >> 20) - (tiny ? (121u << 3) : (120u << 3)), 0x7Eu);
 }
 __device__ __forceinline__ uint32_t to_e5m2(float x, uint32_t r) {
-  const uint32_t normal = ((__float_as_uint(x) + (r << 5)) >> 21) - (112u << 2);
-  const uint32_t tiny = (uint32_t)(x * 65536.0f + (float)r * 0x1p-16f);
-  return min(x < 0x1p-14f ? tiny : normal, 0x7Bu);
+  const bool tiny = x < 0x1p-14f;
+  const uint32_t bits = __float_as_uint(tiny ? x + 0x1p-14f : x) + (r << 5);
+  return min((bits >> 21) - (tiny ? (113u << 2) : (112u << 2)), 0x7Bu);
+}
+
+// value i of four in e4m3 (M) or e5m2
+template <bool M>
+__device__ __forceinline__ float from_8bit(uint32_t four, int i) {
+  if constexpr (M)
+    return i < 2 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)four, false)[i] : __builtin_amdgcn_cvt_pk_f32_fp8((int)four, true)[i - 2];
+  else
+    return i < 2 ? __builtin_amdgcn_cvt_pk_f32_bf8((int)four, false)[i] : __builtin_amdgcn_cvt_pk_f32_bf8((int)four, true)[i - 2];
+}
+
+// b old + rest x, rounded operation by operation: which of an 8-bit state's two
+// neighbours is taken then does not depend on what a compiler fuses.
+__device__ __forceinline__ float average(float b, float old, float rest, float x) {
+#pragma clang fp contract(off)
+  return b * old + rest * x;
 }
 
 // the scale of a block, from its largest magnitude's bits, and its reciprocal (0: the block is 0)
-__device__ __forceinline__ float scale_of(uint32_t largest, float most, float* inv) {
+__device__ __forceinline__ float scale_of(uint32_t largest, float one_over_most, float* inv) {
   const float a = __uint_as_float(largest);
   *inv = 0;
   if (!(a < __builtin_inff())) return __builtin_nanf("");
   if (a < 0x1p-110f) return 0;
-  const float s = a / most;
+  const float s = a * one_over_most;
   *inv = 1.0f / s;
   return s;
 }
-// the largest over the threads of a block
-__device__ __forceinline__ uint32_t block_max(uint32_t m) {
+
+// GROUP consecutive values in registers as they lie in memory, and in fp32
+template <int GROUP>
+struct Raw {
+  u32x4_t w[GROUP / 4];
+};
+template <int GROUP>
+__device__ __forceinline__ void load_f32(Raw<GROUP>& r, const float* p) {
 #pragma unroll
-  for (int d = LANES / 2; d; d >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-  return m;
+  for (int i = 0; i < GROUP / 4; ++i) r.w[i] = reinterpret_cast<const u32x4_t*>(p)[i];
+}
+template <int GROUP>
+__device__ __forceinline__ void load_bf16(Raw<GROUP>& r, const uint16_t* p) {
+  if constexpr (GROUP == 4) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    r.w[0] = u32x4_t{v.x, v.y, 0, 0};
+  } else {
+#pragma unroll
+    for (int i = 0; i < GROUP / 8; ++i) r.w[i] = reinterpret_cast<const u32x4_t*>(p)[i];
+  }
+}
+template <int GROUP>
+__device__ __forceinline__ float f32_of(const Raw<GROUP>& r, int j) { return __uint_as_float(r.w[j / 4][j % 4]); }
+template <int GROUP>
+__device__ __forceinline__ float bf16_of(const Raw<GROUP>& r, int j) {
+  const uint32_t w = r.w[j / 8][j / 2 % 4];
+  return j % 2 ? bf16_hi(w) : bf16_lo(w);
 }
 
-template <bool BITS8>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
-  int i = 0;
-  while (i + 1 < a.count && blockIdx.x >= a.end[i]) ++i;
-  const Tensor& t = a.t[i];
-  const int64_t first = ((int64_t)blockIdx.x - (i ? a.end[i - 1] : 0)) * CHUNK + threadIdx.x * PIECE;
-  const int have = (int)min((int64_t)PIECE, max((int64_t)0, t.n - first));
+// One workgroup steps CHUNK values of a tensor, in groups of GROUP consecutive
+// ones a thread: 16 where states have 8 bits (one 16-byte load of each, a block's
+// scale from 16 threads), 4 where they have 32.
+// GRAD32: gradients in fp32; MASTER, PARAM: which weights there are.
+template <bool BITS8, bool GRAD32, bool MASTER, bool PARAM>
+__device__ __forceinline__ void step_chunk(const AdamArgs& a, const Tensor& t, int64_t chunk) {
+  constexpr int GROUP = BITS8 ? 16 : 4, GROUPS = VALUES / GROUP;
+  const int lane = threadIdx.x & 63;
+  const int inside = (int)min((int64_t)CHUNK, t.n - chunk);  // values of this chunk
   float lr = a.lr, gs = a.scale, step = a.step;
   if (a.now) {
     lr = a.now[0], gs = a.now[1], step = a.now[2];
     if (gs != gs) return;
     step = step >= 1.0f ? step : 1.0f;
   }
-  const float c1 = -expm1f(step * a.log_b1), c2 = -expm1f(step * a.log_b2);
-
-  float m[PIECE], v[PIECE], w[PIECE];
-  uint32_t m_most = 0, v_most = 0;
-#pragma unroll
-  for (int j = 0; j < PIECE; ++j) {
-    m[j] = v[j] = w[j] = 0;
-    if (j >= have) continue;
-    const int64_t at = first + j;
-    const float g = gs * (t.grad_fp32() ? static_cast<const float*>(t.grad)[at]
-                                      : bf16_to_f32(static_cast<const uint16_t*>(t.grad)[at]));
-    if constexpr (BITS8) {
-      m[j] = __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(t.m)[at], 0) * t.m_scale[at / MOE_ADAMW_BLOCK];
-      v[j] = __builtin_amdgcn_cvt_f32_bf8(static_cast<const uint8_t*>(t.v)[at], 0) * t.v_scale[at / MOE_ADAMW_BLOCK];
-    } else {
-      m[j] = static_cast<const float*>(t.m)[at];
-      v[j] = static_cast<const float*>(t.v)[at];
-    }
-    m[j] = a.b1 * m[j] + (1.0f - a.b1) * g;
-    v[j] = a.b2 * v[j] + (1.0f - a.b2) * (g * g);
-    m_most = max(m_most, __float_as_uint(m[j]) & 0x7fffffffu);
-    v_most = max(v_most, __float_as_uint(v[j]) & 0x7fffffffu);
-    w[j] = t.master ? t.master[at] : bf16_to_f32(t.param[at]);
-    w[j] -= lr * (t.decay * w[j] + (m[j] / c1) / (sqrtf(v[j] / c2) + a.eps));
-  }
-  float ms = 0, vs = 0, mi = 0, vi = 0;
-  if constexpr (BITS8) {
-    ms = scale_of(block_max(m_most), 448.0f, &mi);
-    vs = scale_of(block_max(v_most), 57344.0f, &vi);
-    if (have > 0 && threadIdx.x % LANES == 0) {
-      t.m_scale[first / MOE_ADAMW_BLOCK] = ms;
-      t.v_scale[first / MOE_ADAMW_BLOCK] = vs;
-    }
-  }
+  const float c1 = 1.0f / -expm1f(step * a.log_b1), c2 = 1.0f / -expm1f(step * a.log_b2);
   const uint32_t key = mixed(mixed(a.seed + (uint32_t)step * 0xD22CD251u) + t.place() * 0xA5375919u);
+  const float* grad_f = static_cast<const float*>(t.grad) + chunk;
+  const uint16_t* grad_h = static_cast<const uint16_t*>(t.grad) + chunk;
+  float* master = t.master + chunk;
+  uint16_t* param = t.param + chunk;
+  uint8_t *m8 = static_cast<uint8_t*>(t.m) + chunk, *v8 = static_cast<uint8_t*>(t.v) + chunk;
+  float *m32 = static_cast<float*>(t.m) + chunk, *v32 = static_cast<float*>(t.v) + chunk;
+
+  Raw<GROUP> g[GROUPS], w[GROUPS];
+  u32x4_t m[GROUPS], v[GROUPS];  // 16 states of 8 bits or 4 of 32
+  float ms = 0, vs = 0;
+  const auto at_of = [&](int k) { return ((int)(threadIdx.x >> 6) * GROUPS * 64 + k * 64 + lane) * GROUP; };
+  // A group that the tensor's end cuts is read value by value, zeros behind it
 #pragma unroll
-  for (int j = 0; j < PIECE; ++j) {
-    if (j >= have) continue;
-    const int64_t at = first + j;
-    const uint32_t h = mixed(key + (uint32_t)at * 0x946BAFCDu + (uint32_t)(at >> 32) * 0x8952E2D3u);
-    if (t.master) {
-      t.master[at] = w[j];
-      if (t.param) t.param[at] = (uint16_t)f32_to_bf16(w[j]);
-    } else {
-      t.param[at] = w[j] != w[j] ? 0x7fc0u : (uint16_t)((__float_as_uint(w[j]) + (h * 0x761BCE4Bu >> 16)) >> 16);
+  for (int k = 0; k < GROUPS; ++k) {
+    const int at = at_of(k), have = inside - at;
+    g[k] = w[k] = {};
+    m[k] = v[k] = u32x4_t{0, 0, 0, 0};
+    if (have >= GROUP) {
+      if constexpr (GRAD32) load_f32(g[k], grad_f + at);
+      else load_bf16(g[k], grad_h + at);
+      if constexpr (MASTER) load_f32(w[k], master + at);
+      else load_bf16(w[k], param + at);
+      m[k] = BITS8 ? *reinterpret_cast<const u32x4_t*>(m8 + at) : *reinterpret_cast<const u32x4_t*>(m32 + at);
+      v[k] = BITS8 ? *reinterpret_cast<const u32x4_t*>(v8 + at) : *reinterpret_cast<const u32x4_t*>(v32 + at);
+    } else if (have > 0) {
+#pragma unroll
+      for (int j = 0; j < GROUP; ++j) {
+        if (j >= have) continue;
+        if constexpr (GRAD32) g[k].w[j / 4][j % 4] = __float_as_uint(grad_f[at + j]);
+        else g[k].w[j / 8][j / 2 % 4] |= (uint32_t)grad_h[at + j] << (j % 2 * 16);
+        if constexpr (MASTER) w[k].w[j / 4][j % 4] = __float_as_uint(master[at + j]);
+        else w[k].w[j / 8][j / 2 % 4] |= (uint32_t)param[at + j] << (j % 2 * 16);
+        if constexpr (BITS8) {
+          m[k][j / 4] |= (uint32_t)m8[at + j] << (j % 4 * 8);
+          v[k][j / 4] |= (uint32_t)v8[at + j] << (j % 4 * 8);
+        } else {
+          m[k][j] = __float_as_uint(m32[at + j]);
+          v[k][j] = __float_as_uint(v32[at + j]);
+        }
+      }
     }
+    if (BITS8 && have > 0) {
+      ms = t.m_scale[(chunk + at) / MOE_ADAMW_BLOCK];
+      vs = t.v_scale[(chunk + at) / MOE_ADAMW_BLOCK];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < GROUPS; ++k) {
+    const int at = at_of(k), have = inside - at;
+    float fm[GROUP], fv[GROUP], fw[GROUP];
+    uint32_t m_most = 0, v_most = 0;
+#pragma unroll
+    for (int j = 0; j < GROUP; ++j) {
+      const float gr = gs * (GRAD32 ? f32_of(g[k], j) : bf16_of(g[k], j));
+      if constexpr (BITS8) {
+        fm[j] = from_8bit<true>(m[k][j / 4], j % 4) * ms;
+        fv[j] = from_8bit<false>(v[k][j / 4], j % 4) * vs;
+      } else {
+        fm[j] = __uint_as_float(m[k][j]);
+        fv[j] = __uint_as_float(v[k][j]);
+      }
+      fm[j] = average(a.b1, fm[j], a.rest1, gr);
+      fv[j] = average(a.b2, fv[j], a.rest2, gr * gr);
+      if constexpr (BITS8) {
+        m_most = max(m_most, __float_as_uint(fm[j]) & 0x7fffffffu);
+        v_most = max(v_most, __float_as_uint(fv[j]) & 0x7fffffffu);
+      }
+      // the hardware's root and reciprocal, each within 2^-23 of the exact one
+      const float old = MASTER ? f32_of(w[k], j) : bf16_of(w[k], j);
+      const float den = __builtin_amdgcn_sqrtf(fv[j] * c2) + a.eps;
+      fw[j] = old - lr * (t.decay * old + fm[j] * c1 * __builtin_amdgcn_rcpf(den));
+    }
+    float mi = 0, vi = 0;
     if constexpr (BITS8) {
-      const uint32_t mc = mi > 0 ? to_e4m3(fabsf(m[j]) * mi, h & 0xffffu) | (__float_as_uint(m[j]) >> 31 << 7) : 0u;
-      const uint32_t vc = vi > 0 ? max(to_e5m2(v[j] * vi, h >> 16), v[j] > 0 ? 1u : 0u) : 0u;
-      static_cast<uint8_t*>(t.m)[at] = (uint8_t)mc;
-      static_cast<uint8_t*>(t.v)[at] = (uint8_t)vc;
-    } else {
-      static_cast<float*>(t.m)[at] = m[j];
-      static_cast<float*>(t.v)[at] = v[j];
+#pragma unroll
+      for (int d = MOE_ADAMW_BLOCK / GROUP / 2; d; d >>= 1) {
+        m_most = max(m_most, (uint32_t)__shfl_xor((int)m_most, d));
+        v_most = max(v_most, (uint32_t)__shfl_xor((int)v_most, d));
+      }
+      ms = scale_of(m_most, 1.0f / 448.0f, &mi);
+      vs = scale_of(v_most, 1.0f / 57344.0f, &vi);
+      if (have > 0 && threadIdx.x % (MOE_ADAMW_BLOCK / GROUP) == 0) {
+        t.m_scale[(chunk + at) / MOE_ADAMW_BLOCK] = ms;
+        t.v_scale[(chunk + at) / MOE_ADAMW_BLOCK] = vs;
+      }
     }
+    // random bits, where something is rounded at random
+    uint32_t h[GROUP] = {};
+    if constexpr (BITS8 || !MASTER) {
+      const uint64_t first = (uint64_t)(chunk + at);
+      uint32_t x = key + (uint32_t)first * 0x946BAFCDu + (uint32_t)(first >> 32) * 0x8952E2D3u;
+#pragma unroll
+      for (int j = 0; j < GROUP; ++j, x += 0x946BAFCDu) h[j] = mixed(x);
+    }
+    uint32_t pw[GROUP / 2];  // param's values
+    u32x4_t ow[GROUP / 4];   // master's
+#pragma unroll
+    for (int j = 0; j < GROUP; ++j) ow[j / 4][j % 4] = __float_as_uint(fw[j]);
+#pragma unroll
+    for (int j = 0; j < GROUP; j += 2) {
+      if constexpr (MASTER) {
+        pw[j / 2] = pack_bf16x2(fw[j], fw[j + 1]);
+      } else {
+        uint32_t r[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+          r[n] = fw[j + n] != fw[j + n] ? 0x7fc00000u : __float_as_uint(fw[j + n]) + (h[j + n] * 0x761BCE4Bu >> 16);
+        pw[j / 2] = r[0] >> 16 | (r[1] & 0xffff0000u);
+      }
+    }
+    u32x4_t om{0, 0, 0, 0}, ov{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < GROUP; ++j) {
+      if constexpr (BITS8) {
+        const uint32_t mc = to_e4m3(fabsf(fm[j]) * mi, h[j] & 0xffffu) | (__float_as_uint(fm[j]) >> 24 & 0x80u);
+        // (what is not 0 stays so: its root is divided by)
+        const uint32_t vc = max(to_e5m2(fv[j] * vi, h[j] >> 16), min(__float_as_uint(fv[j]), 1u));
+        om[j / 4] |= mc << (j % 4 * 8);
+        ov[j / 4] |= vc << (j % 4 * 8);
+      } else {
+        om[j] = __float_as_uint(fm[j]);
+        ov[j] = __float_as_uint(fv[j]);
+      }
+    }
+    if constexpr (BITS8) {  // a block that is 0, or NaN
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        om[j] = mi > 0 ? om[j] : 0u;
+        ov[j] = vi > 0 ? ov[j] : 0u;
+      }
+    }
+    if (have >= GROUP) {
+      if constexpr (MASTER) {
+#pragma unroll
+        for (int j = 0; j < GROUP / 4; ++j) reinterpret_cast<u32x4_t*>(master + at)[j] = ow[j];
+      }
+      if constexpr (PARAM) {
+        if constexpr (GROUP == 4) {
+          *reinterpret_cast<uint2*>(param + at) = uint2{pw[0], pw[1]};
+        } else {
+#pragma unroll
+          for (int j = 0; j < GROUP / 8; ++j)
+            reinterpret_cast<u32x4_t*>(param + at)[j] = u32x4_t{pw[4 * j], pw[4 * j + 1], pw[4 * j + 2], pw[4 * j + 3]};
+        }
+      }
+      *(BITS8 ? reinterpret_cast<u32x4_t*>(m8 + at) : reinterpret_cast<u32x4_t*>(m32 + at)) = om;
+      *(BITS8 ? reinterpret_cast<u32x4_t*>(v8 + at) : reinterpret_cast<u32x4_t*>(v32 + at)) = ov;
+    } else if (have > 0) {
+#pragma unroll
+      for (int j = 0; j < GROUP; ++j) {
+        if (j >= have) continue;
+        if constexpr (MASTER) master[at + j] = fw[j];
+        if constexpr (PARAM) param[at + j] = (uint16_t)(pw[j / 2] >> (j % 2 * 16));
+        if constexpr (BITS8) {
+          m8[at + j] = (uint8_t)(om[j / 4] >> (j % 4 * 8));
+          v8[at + j] = (uint8_t)(ov[j / 4] >> (j % 4 * 8));
+        } else {
+          m32[at + j] = __uint_as_float(om[j]);
+          v32[at + j] = __uint_as_float(ov[j]);
+        }
+      }
+    }
+  }
+}
+
+template <bool BITS8>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int i = __popcll(__ballot(lane < a.count && blockIdx.x >= a.end[min(lane, MOST - 1)]));
+  const Tensor& t = a.t[i];
+  const int64_t chunk = (int64_t)(blockIdx.x - (i ? a.end[i - 1] : 0)) * CHUNK;
+  if (t.grad_fp32()) {
+    if (!t.master) step_chunk<BITS8, true, false, true>(a, t, chunk);
+    else if (t.param) step_chunk<BITS8, true, true, true>(a, t, chunk);
+    else step_chunk<BITS8, true, true, false>(a, t, chunk);
+  } else {
+    if (!t.master) step_chunk<BITS8, false, false, true>(a, t, chunk);
+    else if (t.param) step_chunk<BITS8, false, true, true>(a, t, chunk);
+    else step_chunk<BITS8, false, true, false>(a, t, chunk);
   }
 }
 
 moe_status check(const moe_adamw_config* c, const moe_adamw_tensor* tensors, int32_t n) {
   if (!c) return fail(MOE_ERR_INVALID_ARG, "config is NULL");
-  const auto finite = [](float v) { return v - v == 0.0f; };
+  const auto finite = [](double v) { return std::isfinite((float)v); };
   if (!finite(c->lr) || c->lr < 0) return fail(MOE_ERR_INVALID_ARG, "lr must be finite and not below 0");
-  if (!(c->beta1 >= 0.0f && c->beta1 < 1.0f && c->beta2 >= 0.0f && c->beta2 < 1.0f))
+  if (!(c->beta1 >= 0 && c->beta1 < 1 && c->beta2 >= 0 && c->beta2 < 1))
     return fail(MOE_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1)");
-  if (!finite(c->eps) || !(c->eps > 0)) return fail(MOE_ERR_INVALID_ARG, "eps must be above 0 and finite");
+  if (!finite(c->eps) || !(c->eps >= 1e-15)) return fail(MOE_ERR_INVALID_ARG, "eps must be finite and at least 1e-15");
   if (!finite(c->grad_scale)) return fail(MOE_ERR_INVALID_ARG, "grad_scale must be finite");
   if (c->step < 1) return fail(MOE_ERR_INVALID_ARG, "step counts from 1");
   if (c->state_bits != 32 && c->state_bits != 8) return fail(MOE_ERR_INVALID_ARG, "state_bits must be 32 or 8");
@@ -192,9 +358,10 @@ moe_status moe_adamw(const moe_adamw_config* cfg, const moe_adamw_tensor* tensor
   if (reinterpret_cast<uintptr_t>(now) % 4) return fail(MOE_ERR_INVALID_ARG, "now is not aligned to its values");
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   AdamArgs a{};
-  a.now = now, a.lr = cfg->lr, a.scale = cfg->grad_scale, a.step = (float)cfg->step;
-  a.b1 = cfg->beta1, a.b2 = cfg->beta2, a.eps = cfg->eps, a.seed = cfg->seed;
-  a.log_b1 = (float)std::log((double)cfg->beta1), a.log_b2 = (float)std::log((double)cfg->beta2);
+  a.now = now, a.lr = (float)cfg->lr, a.scale = (float)cfg->grad_scale, a.step = (float)cfg->step;
+  a.b1 = (float)cfg->beta1, a.b2 = (float)cfg->beta2, a.eps = (float)cfg->eps, a.seed = cfg->seed;
+  a.rest1 = (float)(1 - cfg->beta1), a.rest2 = (float)(1 - cfg->beta2);
+  a.log_b1 = (float)std::log(cfg->beta1), a.log_b2 = (float)std::log(cfg->beta2);
   bool any = false;
   const auto go = [&] {
     if (a.count == 0) return;

@@ -187,7 +187,7 @@ def rounded_at_random(v, scale, u, bits, least, most, above_zero):
 
 
 def adamw(w, g, m, v, cfg, decay):
-    """The new (w, m, v) in float64 and their bounds before any rounding to fewer bits; cfg: dict of float32 numbers."""
+    """The new (w, m, v) in float64 and their bounds before any rounding to fewer bits; cfg: a dict."""
     b1, b2 = float(cfg["beta1"]), float(cfg["beta2"])
     t = float(cfg["step"])
     c1, c2 = -np.expm1(t * np.log(b1)) if b1 else 1.0, -np.expm1(t * np.log(b2)) if b2 else 1.0
