@@ -95,20 +95,6 @@ struct RowTiles {
     return {__builtin_amdgcn_readlane(group, src), __builtin_amdgcn_readlane(begin, src),
             __builtin_amdgcn_readlane(end, src), __builtin_amdgcn_readlane(tiles, src)};
   }
-
-  // the tiles of the groups before group g
-  __device__ __forceinline__ int before(int g) const {
-    if (!off) return 0;
-    int t = incl - n;
-    const bool mine = g >= g0 && g < g1;
-    if (mine)
-      for (int i = g0, a = first; i < g; ++i) {
-        const int e = max(a, clamp_off(off[i + 1], T));
-        t += ceil_div(e - a, bm);
-        a = e;
-      }
-    return __builtin_amdgcn_readlane(t, __ffsll((unsigned long long)__ballot(mine)) - 1);
-  }
 };
 
 // The group of rank r by its number of rows, the largest first (equal ones in

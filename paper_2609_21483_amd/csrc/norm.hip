@@ -30,6 +30,10 @@ struct NormGradArgs {
   int parts;
 };
 
+// Threads of a workgroup whose rows take THREADS threads each
+template <int THREADS>
+constexpr int group_of = THREADS > 256 ? THREADS : 256;
+
 // Sum and largest of (a, m) over the THREADS threads of a row.  red: a slot for
 // each wavefront; a caller in a loop takes two sets in turn.
 template <int THREADS>
@@ -54,14 +58,28 @@ __device__ __forceinline__ void reduce(float& a, uint32_t& m, float* red_a, uint
   }
 }
 
+template <int THREADS>
+__device__ __forceinline__ float sum_of(float a, float* red) {
+#pragma unroll
+  for (int d = (THREADS < 64 ? THREADS : 64) / 2; d; d >>= 1) a += __shfl_xor(a, d);
+  if constexpr (THREADS > 64) {
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = a;
+    __syncthreads();
+    a = red[0];
+#pragma unroll
+    for (int i = 1; i < THREADS / 64; ++i) a += red[i];
+  }
+  return a;
+}
+
 // One row by THREADS threads, held in registers: LOADS pieces of 8 values each.
 // s w is exact in fp32 (two bf16 values), so y = (s w) r is rounded once, and the
 // largest |y| is the largest |s w| times r.
 template <int THREADS, int LOADS>
-__global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
-  constexpr int PER = 256 / THREADS;  // rows of a workgroup
-  __shared__ float red_a[4];
-  __shared__ uint32_t red_m[4];
+__global__ __launch_bounds__(group_of<THREADS>) void rms_norm_kernel(NormArgs a) {
+  constexpr int PER = group_of<THREADS> / THREADS;  // rows of a workgroup
+  __shared__ float red_a[16];
+  __shared__ uint32_t red_m[16];
   const int t = threadIdx.x % THREADS, row = blockIdx.x * PER + threadIdx.x / THREADS;
   const bool some = row < a.T;
   const size_t at = (size_t)row * a.H;
@@ -133,10 +151,9 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(NormArgs a) {
 
 // dx row by row, and each group of threads' part of dweight over its rows.
 template <int THREADS, int LOADS>
-__global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
-  constexpr int PER = 256 / THREADS;
-  __shared__ float red_a[2][4];
-  __shared__ uint32_t red_m[2][4];
+__global__ __launch_bounds__(group_of<THREADS>) void rms_norm_grad_kernel(NormGradArgs a) {
+  constexpr int PER = group_of<THREADS> / THREADS;
+  __shared__ float red_a[2][16];
   const int t = threadIdx.x % THREADS, part = blockIdx.x * PER + threadIdx.x / THREADS;
   u32x4_t w[LOADS];
   float dw[LOADS][8] = {};
@@ -145,13 +162,13 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
     const int c = (t + i * THREADS) * 8;
     w[i] = c < a.H ? *reinterpret_cast<const u32x4_t*>(a.weight + c) : u32x4_t{0, 0, 0, 0};
   }
-  int turn = 0;
+  int turn = 0;  // two sets of slots in turn: one barrier a row
   for (int row0 = blockIdx.x * PER; row0 < a.T; row0 += a.parts, turn ^= 1) {
     const int row = row0 + threadIdx.x / THREADS;
     const bool some = row < a.T;
     const size_t at = (size_t)row * a.H;
     const float r = some ? a.rstd[row] : 0.0f;
-    u32x4_t d[LOADS], s[LOADS];
+    u32x4_t d[LOADS], s[LOADS], more[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int c = (t + i * THREADS) * 8;
@@ -159,8 +176,13 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
       d[i] = in ? *reinterpret_cast<const u32x4_t*>(a.dy + at + c) : u32x4_t{0, 0, 0, 0};
       s[i] = in ? *reinterpret_cast<const u32x4_t*>(a.sum + at + c) : u32x4_t{0, 0, 0, 0};
     }
+    if (a.dsum && a.dx)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const int c = (t + i * THREADS) * 8;
+        more[i] = some && c < a.H ? *reinterpret_cast<const u32x4_t*>(a.dsum + at + c) : u32x4_t{0, 0, 0, 0};
+      }
     float dot = 0;
-    uint32_t none = 0;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       float dv[8], sv[8], wv[8];
@@ -175,8 +197,7 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
       }
     }
     if (!a.dx) continue;
-    reduce<THREADS>(dot, none, red_a[turn], red_m[turn]);
-    const float c0 = dot / a.H;
+    const float c0 = sum_of<THREADS>(dot, red_a[turn]) / a.H;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int c = (t + i * THREADS) * 8;
@@ -188,7 +209,7 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) dv[j] = r * (dv[j] * wv[j] - sv[j] * r * c0);
       if (a.dsum) {
-        tile::unpack8(*reinterpret_cast<const u32x4_t*>(a.dsum + at + c), sv);
+        tile::unpack8(more[i], sv);
 #pragma unroll
         for (int j = 0; j < 8; ++j) dv[j] += sv[j];
       }
@@ -206,12 +227,23 @@ __global__ __launch_bounds__(256) void rms_norm_grad_kernel(NormGradArgs a) {
   }
 }
 
-__global__ __launch_bounds__(256) void rms_norm_dweight_kernel(NormGradArgs a) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.H) return;
-  float v = 0;
-  for (int i = 0; i < a.parts; ++i) v += a.part[(size_t)i * a.H + c];
-  a.dweight[c] = v;
+// The parts' sum in a fixed order: 32 columns a workgroup, 8 threads side by side
+// and 128 groups of them that take the parts in turn.
+__global__ __launch_bounds__(1024) void rms_norm_dweight_kernel(NormGradArgs a) {
+  __shared__ f32x4_t red[128][8];
+  const int c = blockIdx.x * 32 + threadIdx.x % 8 * 4, first = threadIdx.x / 8;
+  f32x4_t v{0, 0, 0, 0};
+  if (c < a.H) {
+#pragma unroll 8
+    for (int i = first; i < a.parts; i += 128) v += *reinterpret_cast<const f32x4_t*>(a.part + (size_t)i * a.H + c);
+  }
+  red[first][threadIdx.x % 8] = v;
+#pragma unroll
+  for (int n = 64; n; n >>= 1) {
+    __syncthreads();
+    if (first < n) red[first][threadIdx.x % 8] += red[first + n][threadIdx.x % 8];
+  }
+  if (first == 0 && c < a.H) *reinterpret_cast<f32x4_t*>(a.dweight + c) = red[0][threadIdx.x % 8];
 }
 
 // fn(constants THREADS and LOADS) for rows of H values
@@ -223,14 +255,14 @@ void for_width(int H, Fn&& fn) {
   else if (H <= 1024) fn(integral_constant<int, 64>(), integral_constant<int, 2>());
   else if (H <= 2048) fn(integral_constant<int, 256>(), integral_constant<int, 1>());
   else if (H <= 4096) fn(integral_constant<int, 256>(), integral_constant<int, 2>());
-  else if (H <= 8192) fn(integral_constant<int, 256>(), integral_constant<int, 4>());
-  else fn(integral_constant<int, 256>(), integral_constant<int, 8>());
+  else if (H <= 8192) fn(integral_constant<int, 512>(), integral_constant<int, 2>());
+  else fn(integral_constant<int, 1024>(), integral_constant<int, 2>());
 }
 
 // Parts of dweight's sum: the groups of threads that share the rows.
 int grad_parts(int T, int H) {
   int per = 1;
-  for_width(H, [&](auto threads, auto) { per = 256 / threads(); });
+  for_width(H, [&](auto threads, auto) { per = group_of<threads()> / threads(); });
   return std::min(ceil_div(T, per), 1024) * per;
 }
 
@@ -265,8 +297,9 @@ moe_status moe_rms_norm_forward(const moe_rms_norm_config* cfg, const uint16_t* 
     if (!aligned16(p)) return fail(MOE_ERR_INVALID_ARG, "a tensor does not start on a 16-byte boundary");
   const NormArgs a{cfg->rows, cfg->hidden, cfg->eps, x, residual, weight, sum, y, rstd, q, scale};
   for_width(a.H, [&](auto threads, auto loads) {
+    constexpr int group = group_of<threads()>;
     rms_norm_kernel<threads(), loads()>
-        <<<ceil_div(a.T, 256 / threads()), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+        <<<ceil_div(a.T, group / threads()), group, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
   });
   HIP_TRY(hipGetLastError());
   return MOE_OK;
@@ -297,9 +330,10 @@ moe_status moe_rms_norm_backward(const moe_rms_norm_config* cfg, const uint16_t*
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (a.T > 0 && (dx || dweight))
     for_width(a.H, [&](auto threads, auto loads) {
-      rms_norm_grad_kernel<threads(), loads()><<<a.parts / (256 / threads()), 256, 0, s>>>(a);
+      constexpr int group = group_of<threads()>;
+      rms_norm_grad_kernel<threads(), loads()><<<a.parts / (group / threads()), group, 0, s>>>(a);
     });
-  if (dweight) rms_norm_dweight_kernel<<<ceil_div(a.H, 256), 256, 0, s>>>(a);
+  if (dweight) rms_norm_dweight_kernel<<<ceil_div(a.H, 32), 1024, 0, s>>>(a);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }

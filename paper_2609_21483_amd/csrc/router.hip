@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "blocks.h"
 
@@ -62,114 +63,277 @@ __global__ __launch_bounds__(256) void gate_dwg_kernel(GateArgs a) {
 // ---- the routing's losses ---------------------------------------------------------
 struct LossArgs {
   int T, E, K, S, bm;  // bm: rows of a tile
+  int Ep;              // E rounded up to whole 16 bytes
   const int32_t *off, *idx;
   const float *logits, *topk_w, *dtopk_w, *dloss, *in_lse;
   const int32_t* in_counts;
   int32_t* counts;
   float *lse, *loss, *dlogits;
-  float *part, *zpart, *seq;  // workspace: softmax sums [tiles][E], sums of lse^2 [tiles], [S][2]
-  int32_t* cpart;             // and counts [tiles][E]
+  // workspace: of each tile the sums of the softmax [tiles][Ep], the counts and the sum of lse^2; of each sequence and
+  // 32 of its experts the part of the balance loss, and of each sequence the sum of lse^2; workgroups that are done
+  float *part, *zpart, *seq, *zseq;
+  int32_t *cpart, *done;
 };
 
-constexpr int PER = MAX_E / 64;  // experts of a lane: lane + 64 i
+// The sequences' rows and tiles.  Every lane of the wavefront takes part and gets
+// the same answers; each holds up to 8 consecutive sequences.
+struct SeqTiles {
+  const int32_t* off;
+  int T, bm, g0, g1, first, before, n;  // first: where this lane's sequences start; before: the tiles ahead of its n
+  int total, live, rows;                // tiles, sequences that have rows, and their rows
+  struct Seq {
+    int g, b, e, tile;  // rows [b, e) and the first tile
+  };
 
-// A tile's rows are the four wavefronts' in turn.
+  __device__ __forceinline__ SeqTiles(const int32_t* off_, int S, int T_, int bm_) : off(off_), T(T_), bm(bm_) {
+    if (!off) {
+      total = ceil_div(T, bm), live = 1, rows = T;
+      return;
+    }
+    const int lane = threadIdx.x & 63, per = ceil_div(S, 64);
+    g0 = min(lane * per, S), g1 = min(g0 + per, S);
+    int m = 0;
+    for (int g = g0; g < g1; ++g) m = max(m, clamp_off(off[g], T));
+    const int own = g0 < S ? clamp_off(off[g0], T) : 0;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(m, d);
+      if (lane >= d) m = max(m, o);
+    }
+    m = __shfl_up(m, 1);
+    first = max(lane ? m : 0, own);
+    int at = first, sum = 0;  // tiles, and sequences with rows in the upper bits
+    for (int g = g0; g < g1; ++g) {
+      const int e = max(at, clamp_off(off[g + 1], T));
+      sum += ceil_div(e - at, bm) + (e > at ? 1 << 21 : 0);
+      at = e;
+    }
+    n = sum & ((1 << 21) - 1);
+    // (this lane's last row: rows follow each other without gaps)
+    const int last = (S - 1) / per;
+    rows = __builtin_amdgcn_readlane(at, last) - __builtin_amdgcn_readfirstlane(first);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(sum, d);
+      if (lane >= d) sum += o;
+    }
+    before = (sum & ((1 << 21) - 1)) - n;
+    sum = __builtin_amdgcn_readlane(sum, 63);
+    total = sum & ((1 << 21) - 1);
+    live = sum >> 21;
+  }
+
+  // the sequence for which `is` holds of its number and its tiles' range; one lane has it
+  template <typename Fn>
+  __device__ __forceinline__ Seq find(bool mine, Fn&& is) const {
+    Seq s{};
+    if (mine) {
+      int at = first, tile = before;
+      for (int g = g0; g < g1; ++g) {
+        const int e = max(at, clamp_off(off[g + 1], T)), k = ceil_div(e - at, bm);
+        if (is(g, tile, k)) s = {g, at, e, tile};
+        at = e;
+        tile += k;
+      }
+    }
+    const int src = __ffsll((unsigned long long)__ballot(mine)) - 1;
+    return {__builtin_amdgcn_readlane(s.g, src), __builtin_amdgcn_readlane(s.b, src), __builtin_amdgcn_readlane(s.e, src),
+            __builtin_amdgcn_readlane(s.tile, src)};
+  }
+  __device__ __forceinline__ Seq of_tile(int t) const {  // t < total
+    if (!off) return {0, 0, T, 0};
+    return find(t >= before && t < before + n, [t](int, int tile, int k) { return t >= tile && t < tile + k; });
+  }
+  __device__ __forceinline__ Seq of(int g) const {
+    if (!off) return {0, 0, T, 0};
+    return find(g >= g0 && g < g1, [g](int i, int, int) { return i == g; });
+  }
+};
+
+// A row of logits in the registers of LPR lanes, N values each: 16-byte pieces
+// (VEC, where rows start on 16 bytes) or single values side by side.
+template <int LPR_, int N_, bool VEC>
+struct Row {
+  static constexpr int LPR = LPR_, N = N_, AT_ONCE = 64 / LPR;  // AT_ONCE: rows of a wavefront
+  static __device__ __forceinline__ int column(int l, int i) { return VEC ? (i / 4 * LPR + l) * 4 + i % 4 : i * LPR + l; }
+  static __device__ __forceinline__ void load(float (&v)[N], const float* row, int l, int E, bool some) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4) {
+        f32x4_t t{-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+        if (some && column(l, i) < E) t = *reinterpret_cast<const f32x4_t*>(row + column(l, i));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i + j] = t[j];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = some && column(l, i) < E ? row[column(l, i)] : -__builtin_inff();
+    }
+  }
+  static __device__ __forceinline__ void store(const float (&v)[N], float* row, int l, int E) {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4)
+        if (column(l, i) < E) *reinterpret_cast<f32x4_t*>(row + column(l, i)) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (column(l, i) < E) row[column(l, i)] = v[i];
+    }
+  }
+  static __device__ __forceinline__ float sum(float v) {
+#pragma unroll
+    for (int d = LPR / 2; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+  }
+};
+
+// A tile's rows are the four wavefronts' in turn; the next row's logits are loaded
+// before a row is worked on.
+template <typename R>
 __global__ __launch_bounds__(256) void route_loss_kernel(LossArgs a) {
   __shared__ int hist[MAX_E];
-  __shared__ float sums[4][MAX_E], zs[4];
-  const RowTiles list(a.off, a.S, a.T, a.bm);
+  __shared__ float sums[256 * R::N], zs[4 * R::AT_ONCE];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
+  const SeqTiles list(a.off, a.S, a.T, a.bm);
   if ((int)blockIdx.x >= list.total) return;
-  const RowTile rt = list.at(blockIdx.x);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int i = threadIdx.x; i < MAX_E; i += 256) hist[i] = 0;
+  const SeqTiles::Seq seq = list.of_tile(blockIdx.x);
+  const int begin = seq.b + ((int)blockIdx.x - seq.tile) * a.bm, end = min(begin + a.bm, seq.e);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane % R::LPR, sub = lane / R::LPR;
+  float p[R::N] = {}, z = 0, next[R::N];
+  int base = begin + wave * R::AT_ONCE;
+  R::load(next, a.logits + (size_t)(base + sub) * a.E, l, a.E, base + sub < end);
+  for (int i = threadIdx.x; i < a.Ep; i += 256) hist[i] = 0;
   __syncthreads();
-  for (int i = threadIdx.x; i < (rt.end - rt.begin) * a.K; i += 256) {
-    const int e = a.idx[(size_t)rt.begin * a.K + i];
+  for (int i = threadIdx.x; i < (end - begin) * a.K; i += 256) {
+    const int e = a.idx[(size_t)begin * a.K + i];
     if (e >= 0 && e < a.E) atomicAdd(&hist[e], 1);
   }
-  float p[PER] = {}, z = 0;
-  for (int row = rt.begin + wave; row < rt.end; row += 4) {
-    float l[PER], top = -__builtin_inff(), total = 0;
+  for (; base < end; base += 4 * R::AT_ONCE) {
+    const int row = base + sub, far = row + 4 * R::AT_ONCE;
+    float v[R::N], top = -__builtin_inff(), total = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = lane + 64 * i;
-      l[i] = e < a.E ? a.logits[(size_t)row * a.E + e] : -__builtin_inff();
-      top = fmaxf(top, l[i]);
+    for (int i = 0; i < R::N; ++i) {
+      v[i] = next[i];
+      top = fmaxf(top, v[i]);
     }
+    R::load(next, a.logits + (size_t)far * a.E, l, a.E, far < end);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    for (int d = R::LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     if (top == -__builtin_inff()) top = 0;  // nothing can be chosen: every exponential is 0
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      l[i] = __expf(l[i] - top);
-      total += l[i];
+    for (int i = 0; i < R::N; ++i) {
+      v[i] = __expf(v[i] - top);
+      total += v[i];
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+    total = R::sum(total);
     const float lse = logf(total) + top, inv = total == 0 ? 0 : 1.0f / total;
-    if (lane == 0) a.lse[row] = lse;
-    z += total == 0 ? 0 : lse * lse;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) p[i] += l[i] * inv;
-  }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) sums[wave][lane + 64 * i] = p[i];
-  if (lane == 0) zs[wave] = z;
-  __syncthreads();
-  for (int e = threadIdx.x; e < a.E; e += 256) {
-    a.part[(size_t)blockIdx.x * a.E + e] = sums[0][e] + sums[1][e] + sums[2][e] + sums[3][e];
-    a.cpart[(size_t)blockIdx.x * a.E + e] = hist[e];
-  }
-  if (threadIdx.x == 0) a.zpart[blockIdx.x] = zs[0] + zs[1] + zs[2] + zs[3];
-}
-
-// A sequence's counts and its parts of the losses, from its tiles in order.
-__global__ __launch_bounds__(512) void route_loss_seq_kernel(LossArgs a) {
-  __shared__ float red[2][8];
-  const int g = blockIdx.x, e = threadIdx.x, lane = threadIdx.x & 63;
-  const RowTiles list(a.off, a.S, a.T, a.bm);
-  int b, end;
-  group_rows(a.off, a.T, g, &b, &end);
-  const int first = list.before(g), tiles = ceil_div(end - b, a.bm);
-  float p = 0, z = 0;
-  int c = 0;
-  if (e < a.E) {
-    for (int t = first; t < first + tiles; ++t) {
-      p += a.part[(size_t)t * a.E + e];
-      c += a.cpart[(size_t)t * a.E + e];
+    if (l == 0 && row < end) {
+      a.lse[row] = lse;
+      z += total == 0 ? 0 : lse * lse;
     }
-    a.counts[(size_t)g * a.E + e] = c;
-  }
-  for (int t = first + threadIdx.x; t < first + tiles; t += 512) z += a.zpart[t];
-  float v = p * (float)c;
 #pragma unroll
-  for (int d = 32; d; d >>= 1) {
-    v += __shfl_xor(v, d);
-    z += __shfl_xor(z, d);
+    for (int i = 0; i < R::N; ++i) p[i] += v[i] * inv;
   }
-  if (lane == 0) red[0][e >> 6] = v, red[1][e >> 6] = z;
+  // [rows at once][column]
+  constexpr int W = R::LPR * R::N;
+#pragma unroll
+  for (int i = 0; i < R::N; ++i) sums[(wave * R::AT_ONCE + sub) * W + R::column(l, i)] = p[i];
+  if (l == 0) zs[wave * R::AT_ONCE + sub] = z;
   __syncthreads();
-  if (threadIdx.x) return;
-  for (int i = 1; i < 8; ++i) v += red[0][i], z += red[1][i];
-  const float n = (float)(end - b);
-  a.seq[2 * g] = tiles ? v * a.E / (a.K * n * n) : 0.0f;
-  a.seq[2 * g + 1] = z;
+  for (int e = threadIdx.x; e < a.Ep; e += 256) {
+    float v = sums[e];
+#pragma unroll
+    for (int i = 1; i < 4 * R::AT_ONCE; ++i) v += sums[i * W + e];
+    a.part[(size_t)blockIdx.x * a.Ep + e] = v;
+    a.cpart[(size_t)blockIdx.x * a.Ep + e] = hist[e];
+  }
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int i = 1; i < 4 * R::AT_ONCE; ++i) z += zs[i];
+    a.zpart[blockIdx.x] = z;
+  }
 }
 
-__global__ __launch_bounds__(64) void route_loss_mean_kernel(LossArgs a) {
-  int b, e;
-  covered_rows(a.off, a.S, a.T, &b, &e);
-  const int live = RowTiles(a.off, a.S, a.T, a.T).total;
-  float v = 0, z = 0;
-  for (int g = threadIdx.x; g < a.S; g += 64) v += a.seq[2 * g], z += a.seq[2 * g + 1];
+// Counts of a sequence's 32 experts from blockIdx.y * 32 on and their part of its
+// balance loss, its tiles added in a fixed order: 8 threads side by side, 128 groups
+// of them take the tiles in turn.  The last workgroup adds all parts up.
+__global__ __launch_bounds__(1024) void route_loss_seq_kernel(LossArgs a) {
+  __shared__ f32x4_t ps[128][8];
+  __shared__ u32x4_t cs[128][8];
+  __shared__ float zs[16], vs[16];
+  __shared__ int last;
+  const int g = blockIdx.x, q = threadIdx.x % 8, first = threadIdx.x / 8, c = blockIdx.y * 32 + q * 4;
+  const SeqTiles list(a.off, a.S, a.T, a.bm);
+  const SeqTiles::Seq seq = list.of(g);
+  const int tiles = ceil_div(seq.e - seq.b, a.bm);
+  f32x4_t p{0, 0, 0, 0};
+  u32x4_t n{0, 0, 0, 0};
+  if (c < a.Ep)
+#pragma unroll 8
+    for (int t = first; t < tiles; t += 128) {
+      p += *reinterpret_cast<const f32x4_t*>(a.part + (size_t)(seq.tile + t) * a.Ep + c);
+      n += *reinterpret_cast<const u32x4_t*>(a.cpart + (size_t)(seq.tile + t) * a.Ep + c);
+    }
+  float z = 0;
+  if (blockIdx.y == 0)
+    for (int t = threadIdx.x; t < tiles; t += 1024) z += a.zpart[seq.tile + t];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) z += __shfl_xor(z, d);
+  if (threadIdx.x % 64 == 0) zs[threadIdx.x / 64] = z;
+  ps[first][q] = p;
+  cs[first][q] = n;
+  for (int k = 64; k; k >>= 1) {
+    __syncthreads();
+    if (first < k) {
+      ps[first][q] += ps[first + k][q];
+      cs[first][q] += cs[first + k][q];
+    }
+  }
+  const float rows = (float)(seq.e - seq.b);
+  if (threadIdx.x < 8) {
+    float v = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (c + j < a.E) a.counts[(size_t)g * a.E + c + j] = (int)cs[0][q][j];
+      v += ps[0][q][j] * (float)cs[0][q][j];
+    }
+#pragma unroll
+    for (int d = 4; d; d >>= 1) v += __shfl_xor(v, d);
+    if (threadIdx.x == 0) {
+      const auto put = [](float* at, float value) { __hip_atomic_store(at, value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+      put(a.seq + g * gridDim.y + blockIdx.y, tiles ? v * a.E / (a.K * rows * rows) : 0.0f);
+      if (blockIdx.y == 0) {
+        for (int i = 1; i < 16; ++i) z += zs[i];
+        put(a.zseq + g, z);
+      }
+      last = __hip_atomic_fetch_add(a.done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)(gridDim.x * gridDim.y) - 1;
+    }
+  }
+  __syncthreads();
+  if (!last) return;
+  const auto get = [](const float* at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  float v = 0;
+  z = 0;
+  for (int i = threadIdx.x; i < (int)(gridDim.x * gridDim.y); i += 1024) v += get(a.seq + i);
+  if ((int)threadIdx.x < a.S) z = get(a.zseq + threadIdx.x);
 #pragma unroll
   for (int d = 32; d; d >>= 1) {
     v += __shfl_xor(v, d);
     z += __shfl_xor(z, d);
   }
+  if (threadIdx.x % 64 == 0) {
+    vs[threadIdx.x / 64] = v;
+    zs[threadIdx.x / 64] = z;
+  }
+  __syncthreads();
   if (threadIdx.x) return;
-  a.loss[0] = live ? v / live : 0.0f;
-  a.loss[1] = live ? z / (e - b) : 0.0f;
+  for (int i = 1; i < 16; ++i) {
+    v += vs[i];
+    z += zs[i];
+  }
+  a.loss[0] = list.live ? v / list.live : 0.0f;
+  a.loss[1] = list.live ? z / list.rows : 0.0f;
 }
 
 __global__ __launch_bounds__(256) void route_loss_none_kernel(LossArgs a) {
@@ -177,50 +341,83 @@ __global__ __launch_bounds__(256) void route_loss_none_kernel(LossArgs a) {
   if (threadIdx.x < 2) a.loss[threadIdx.x] = 0;
 }
 
+template <typename R>
 __global__ __launch_bounds__(256) void route_loss_grad_kernel(LossArgs a) {
-  const RowTiles list(a.off, a.S, a.T, a.bm);
+  const SeqTiles list(a.off, a.S, a.T, a.bm);
   if ((int)blockIdx.x >= list.total) return;
-  const RowTile rt = list.at(blockIdx.x);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int b, end, n0, n1;
-  group_rows(a.off, a.T, rt.group, &b, &end);
-  covered_rows(a.off, a.S, a.T, &n0, &n1);
-  const float n = (float)(end - b), live = (float)RowTiles(a.off, a.S, a.T, a.T).total;
-  const float db = a.dloss ? a.dloss[0] * a.E / (a.K * n * n * live) : 0.0f;
-  const float dz = a.dloss ? 2.0f * a.dloss[1] / (n1 - n0) : 0.0f;
-  float c[PER];
+  const SeqTiles::Seq seq = list.of_tile(blockIdx.x);
+  const int begin = seq.b + ((int)blockIdx.x - seq.tile) * a.bm, end = min(begin + a.bm, seq.e);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane % R::LPR, sub = lane / R::LPR;
+  struct Given {  // what is read of a row: its logits, lse, and of choice l (where l < K) expert, weight and gradient
+    float v[R::N], lse, w, dw;
+    int e;
+  };
+  const auto load = [&](Given& r, int row) {
+    const bool some = row < end;
+    R::load(r.v, a.logits + (size_t)row * a.E, l, a.E, some);
+    r.lse = some ? a.in_lse[row] : 0.0f;
+    const bool choice = some && a.dtopk_w && l < a.K;
+    r.e = choice ? a.idx[(size_t)row * a.K + l] : -1;
+    r.w = choice ? a.topk_w[(size_t)row * a.K + l] : 0.0f;
+    r.dw = choice ? a.dtopk_w[(size_t)row * a.K + l] : 0.0f;
+  };
+  Given next;
+  int base = begin + wave * R::AT_ONCE;
+  load(next, base + sub);
+  const float n = (float)(seq.e - seq.b);
+  const float db = a.dloss ? a.dloss[0] * a.E / (a.K * n * n * list.live) : 0.0f;
+  const float dz = a.dloss ? 2.0f * a.dloss[1] / list.rows : 0.0f;
+  float c[R::N];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int e = lane + 64 * i;
-    c[i] = e < a.E ? (float)a.in_counts[(size_t)rt.group * a.E + e] * db : 0.0f;
+  for (int i = 0; i < R::N; ++i) {
+    const int e = R::column(l, i);
+    c[i] = e < a.E ? (float)a.in_counts[(size_t)seq.g * a.E + e] * db : 0.0f;
   }
-  for (int row = rt.begin + wave; row < rt.end; row += 4) {
-    const float lse = a.in_lse[row];
-    float p[PER], dot = 0;
+  for (; base < end; base += 4 * R::AT_ONCE) {
+    const Given r = next;
+    const int row = base + sub;
+    load(next, row + 4 * R::AT_ONCE);
+    const bool dead = r.lse == -__builtin_inff();  // a row of -inf alone: nothing can be chosen
+    float p[R::N], dot = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = lane + 64 * i;
-      // (a row of -inf alone: nothing can be chosen)
-      p[i] = e < a.E && lse != -__builtin_inff() ? __expf(a.logits[(size_t)row * a.E + e] - lse) : 0.0f;
+    for (int i = 0; i < R::N; ++i) {
+      p[i] = dead ? 0.0f : __expf(r.v[i] - r.lse);
       dot += c[i] * p[i];
     }
+    dot = R::sum(dot);
+    const float rest = (dead ? 0.0f : dz * r.lse) - dot;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) dot += __shfl_xor(dot, d);
-    float wdw = 0;
-    if (a.dtopk_w)
-      for (int j = 0; j < a.K; ++j) wdw += a.topk_w[(size_t)row * a.K + j] * a.dtopk_w[(size_t)row * a.K + j];
-    const float zl = lse == -__builtin_inff() ? 0.0f : dz * lse;
+    for (int i = 0; i < R::N; ++i) p[i] *= c[i] + rest;
+    if (a.dtopk_w) {
+      // (choices are in the row's first 8 lanes)
+      float all = r.w * r.dw;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = lane + 64 * i;
-      float v = p[i] * (c[i] - dot + zl);
-      if (a.dtopk_w)
-        for (int j = 0; j < a.K; ++j)
-          if (a.idx[(size_t)row * a.K + j] == e)
-            v += a.topk_w[(size_t)row * a.K + j] * (a.dtopk_w[(size_t)row * a.K + j] - wdw);
-      if (e < a.E) a.dlogits[(size_t)row * a.E + e] = v;
+      for (int d = 4; d; d >>= 1) all += __shfl_xor(all, d);
+      const float t = r.w * (r.dw - all);
+      for (int j = 0; j < a.K; ++j) {
+        const float tj = __shfl(t, sub * R::LPR + j);
+        const int ej = __shfl(r.e, sub * R::LPR + j);
+#pragma unroll
+        for (int i = 0; i < R::N; ++i) p[i] += R::column(l, i) == ej ? tj : 0.0f;
+      }
     }
+    if (row < end) R::store(p, a.dlogits + (size_t)row * a.E, l, a.E);
   }
+}
+
+// fn(a Row that holds E logits)
+template <typename Fn>
+void for_row(int E, Fn&& fn) {
+  const auto of = [&](auto vec) {
+    constexpr bool V = vec();
+    if (E <= 32) fn(Row<8, 4, V>());
+    else if (E <= 64) fn(Row<16, 4, V>());
+    else if (E <= 128) fn(Row<32, 4, V>());
+    else if (E <= 256) fn(Row<64, 4, V>());
+    else fn(Row<64, 8, V>());
+  };
+  if (E % 4 == 0) of(std::true_type());
+  else of(std::false_type());
 }
 
 // ---- host ---------------------------------------------------------------------------
@@ -268,25 +465,29 @@ GateArgs gate_args(const moe_router_config* c, const int32_t* off) {
   return a;
 }
 
-// About 1024 tiles of a long batch, whose sums fit the caches, and 16 rows at least
+// About 1024 tiles of a long batch, whose sums fit the caches; 32 rows at least
+// (the four wavefronts' 4 to 32 at once).
 LossArgs loss_args(const moe_router_config* c, const int32_t* off) {
   LossArgs a{};
   a.T = c->rows, a.E = c->n_experts, a.K = c->top_k, a.S = c->n_seqs, a.off = off;
-  a.bm = std::max(16, ceil_div(a.T, 1024));
+  a.Ep = ceil_div(a.E, 4) * 4;
+  a.bm = std::max(32, ceil_div(a.T, 1024));
   return a;
 }
 
-// Workspace: the tiles' sums and counts, their sums of lse^2, the sequences' losses.
+// Workspace: what LossArgs says, one after the other.
 struct LossSpace {
-  size_t part, cpart, zpart, seq, total;
+  size_t part, cpart, zpart, seq, zseq, done, total;
 };
 LossSpace loss_space(const LossArgs& a) {
   const size_t tiles = max_row_tiles(a.T, a.S, a.bm);
   LossSpace w{};
-  w.cpart = align_up(tiles * a.E * sizeof(float), 256);
-  w.zpart = w.cpart + align_up(tiles * a.E * sizeof(int32_t), 256);
+  w.cpart = align_up(tiles * a.Ep * sizeof(float), 256);
+  w.zpart = w.cpart + align_up(tiles * a.Ep * sizeof(int32_t), 256);
   w.seq = w.zpart + align_up(tiles * sizeof(float), 256);
-  w.total = w.seq + align_up(2 * a.S * sizeof(float), 256);
+  w.zseq = w.seq + align_up(ceil_div(a.Ep, 32) * a.S * sizeof(float), 256);
+  w.done = w.zseq + align_up(a.S * sizeof(float), 256);
+  w.total = w.done + 256;
   return w;
 }
 
@@ -364,13 +565,13 @@ moe_status moe_route_loss(const moe_router_config* cfg, const float* logits, con
   char* at = static_cast<char*>(ws);
   a.part = reinterpret_cast<float*>(at + w.part), a.cpart = reinterpret_cast<int32_t*>(at + w.cpart);
   a.zpart = reinterpret_cast<float*>(at + w.zpart), a.seq = reinterpret_cast<float*>(at + w.seq);
+  a.zseq = reinterpret_cast<float*>(at + w.zseq), a.done = reinterpret_cast<int32_t*>(at + w.done);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (a.T == 0) {
     route_loss_none_kernel<<<1, 256, 0, s>>>(a);
   } else {
-    route_loss_kernel<<<max_row_tiles(a.T, a.S, a.bm), 256, 0, s>>>(a);
-    route_loss_seq_kernel<<<a.S, 512, 0, s>>>(a);
-    route_loss_mean_kernel<<<1, 64, 0, s>>>(a);
+    for_row(a.E, [&](auto row) { route_loss_kernel<decltype(row)><<<max_row_tiles(a.T, a.S, a.bm), 256, 0, s>>>(a); });
+    route_loss_seq_kernel<<<dim3(a.S, ceil_div(a.Ep, 32)), 1024, 0, s>>>(a);
   }
   HIP_TRY(hipGetLastError());
   return MOE_OK;
@@ -391,7 +592,10 @@ moe_status moe_route_loss_backward(const moe_router_config* cfg, const float* lo
   LossArgs a = loss_args(cfg, seq_off);
   a.logits = logits, a.idx = topk_idx, a.topk_w = topk_w, a.in_counts = counts, a.in_lse = lse, a.dloss = dloss;
   a.dtopk_w = dtopk_w, a.dlogits = dlogits;
-  route_loss_grad_kernel<<<max_row_tiles(a.T, a.S, a.bm), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+  for_row(a.E, [&](auto row) {
+    route_loss_grad_kernel<decltype(row)>
+        <<<max_row_tiles(a.T, a.S, a.bm), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+  });
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }
