@@ -5,58 +5,240 @@
 #include <type_traits>
 
 #include "blocks.h"
+#include "tile.h"
 
 using namespace moe;
 
 namespace {
 
 // ---- the gate's products ----------------------------------------------------------
+// logits = x wg, dx = d wg^T and dwg = x^T d on the tiles of the products over row
+// groups, over the rows that some sequence has.  The tiles want whole 16 bytes, so
+// a gate whose rows are none is copied with zeros behind each row; dlogits are
+// rounded to bf16 for both products that take them, with zeros up to a multiple of
+// 64, the depth of a stage.
 struct GateArgs {
   int T, H, E, S;
+  int Ep;  // columns of the gate as the product reads it
   const int32_t* off;
   const uint16_t *x, *wg;
   const float *bias, *dlogits;
   float *logits, *dbias;
   uint16_t *dx, *dwg;
+  uint16_t *gate, *d;  // workspace: the gate [H][Ep] where it is copied, dlogits [T][Ep]
+  float *part, *bpart;  // partial sums: of a split product, and of dbias [dbias_parts][E]
+  int split, bias_parts;
 };
 
-__device__ __forceinline__ float rounded(float v) { return bf16_to_f32((uint16_t)f32_to_bf16(v)); }
+__device__ __forceinline__ const char* bytes(const uint16_t* p) { return reinterpret_cast<const char*>(p); }
 
-__global__ __launch_bounds__(256) void gate_logits_kernel(GateArgs a) {
+// The rows that some sequence has, as one group's tiles.
+struct Rows {
   int b, e;
-  covered_rows(a.off, a.S, a.T, &b, &e);
-  const int t = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
-  if (t < b || t >= e || n >= a.E) return;
-  float v = 0;
-  for (int h = 0; h < a.H; ++h) v += bf16_to_f32(a.x[(size_t)t * a.H + h]) * bf16_to_f32(a.wg[(size_t)h * a.E + n]);
-  a.logits[(size_t)t * a.E + n] = a.bias ? v + a.bias[n] : v;
-}
+  __device__ __forceinline__ explicit Rows(const GateArgs& a) { covered_rows(a.off, a.S, a.T, &b, &e); }
+};
 
-__global__ __launch_bounds__(256) void gate_dx_kernel(GateArgs a) {
-  int b, e;
-  covered_rows(a.off, a.S, a.T, &b, &e);
-  const int t = blockIdx.x, h = blockIdx.y * 256 + threadIdx.x;
-  if (t < b || t >= e || h >= a.H) return;
-  float v = 0;
-  for (int n = 0; n < a.E; ++n) v += rounded(a.dlogits[(size_t)t * a.E + n]) * bf16_to_f32(a.wg[(size_t)h * a.E + n]);
-  a.dx[(size_t)t * a.H + h] = (uint16_t)f32_to_bf16(v);
-}
-
-// dwg, and dbias as one more row of it (h = H)
-__global__ __launch_bounds__(256) void gate_dwg_kernel(GateArgs a) {
-  int b, e;
-  covered_rows(a.off, a.S, a.T, &b, &e);
-  const int h = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
-  if (n >= a.E || (h < a.H && !a.dwg)) return;  // (x may be missing where dwg is not wanted)
-  float v = 0;
-  for (int t = b; t < e; ++t) {
-    const float d = a.dlogits[(size_t)t * a.E + n];
-    v += h < a.H ? bf16_to_f32(a.x[(size_t)t * a.H + h]) * rounded(d) : d;
+// The gate with rows of Ep values
+__global__ __launch_bounds__(256) void gate_copy_kernel(GateArgs a) {
+  const int i = blockIdx.x * 256 + threadIdx.x, h = i / (a.Ep / 8), c = i % (a.Ep / 8) * 8;
+  if (h >= a.H) return;
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t lo = c + 2 * j < a.E ? a.wg[(size_t)h * a.E + c + 2 * j] : 0;
+    const uint32_t hi = c + 2 * j + 1 < a.E ? a.wg[(size_t)h * a.E + c + 2 * j + 1] : 0;
+    w[j] = lo | hi << 16;
   }
-  if (h == a.H) {
-    if (a.dbias) a.dbias[n] = v;
-  } else if (a.dwg) {
-    a.dwg[(size_t)h * a.E + n] = (uint16_t)f32_to_bf16(v);
+  *reinterpret_cast<u32x4_t*>(a.gate + (size_t)h * a.Ep + c) = u32x4_t{w[0], w[1], w[2], w[3]};
+}
+
+// dlogits in bf16 with rows of Ep values (where dx or dwg is wanted), and the parts
+// of dbias: a workgroup takes 64 columns and its share of the rows, 16 threads side
+// by side with 4 columns each.
+__global__ __launch_bounds__(256) void gate_round_kernel(GateArgs a) {
+  __shared__ f32x4_t red[16][16];
+  const Rows r(a);
+  const int n = ceil_div(r.e - r.b, a.bias_parts);
+  const int begin = r.b + blockIdx.x * n, end = min(begin + n, r.e);
+  const int c = blockIdx.y * 64 + threadIdx.x % 16 * 4, first = threadIdx.x / 16;
+  f32x4_t sum{0, 0, 0, 0};
+#pragma unroll 4
+  for (int row = begin + first; row < end; row += 16) {
+    const float* p = a.dlogits + (size_t)row * a.E + c;
+    f32x4_t v{0, 0, 0, 0};
+    if (a.E % 4 == 0) {
+      if (c < a.E) v = *reinterpret_cast<const f32x4_t*>(p);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j < a.E) v[j] = p[j];
+    }
+    sum += v;
+    if (a.d) *reinterpret_cast<uint2*>(a.d + (size_t)row * a.Ep + c) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  }
+  if (!a.dbias) return;
+  red[first][threadIdx.x % 16] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 16) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) sum += red[i][threadIdx.x];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < a.E) a.bpart[(size_t)blockIdx.x * a.E + c + j] = sum[j];
+}
+__global__ __launch_bounds__(64) void gate_dbias_kernel(GateArgs a) {
+  const int c = blockIdx.x * 64 + threadIdx.x;
+  if (c >= a.E) return;
+  float v = 0;
+#pragma unroll 8
+  for (int i = 0; i < a.bias_parts; ++i) v += a.bpart[(size_t)i * a.E + c];
+  a.dbias[c] = v;
+}
+
+// 8 logits of a row from column c on, from their sums
+__device__ __forceinline__ void put_logits(const GateArgs& a, size_t row, int c, const float* v) {
+  float* out = a.logits + row * a.E + c;
+  if (a.E % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+      if (c + i >= a.E) break;
+      f32x4_t t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+      if (a.bias) t += *reinterpret_cast<const f32x4_t*>(a.bias + c + i);
+      *reinterpret_cast<f32x4_t*>(out + i) = t;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c + i < a.E) out[i] = a.bias ? v[i] + a.bias[c + i] : v[i];
+  }
+}
+// The same, or the partial sums [split][T][Ep] where the product is split.
+__device__ __forceinline__ void put(const GateArgs& a, int part, size_t row, int c, const uint32_t* v) {
+  if (c >= a.Ep) return;
+  if (a.split > 1) {
+    float* p = a.part + ((size_t)part * a.T + row) * a.Ep + c;
+    reinterpret_cast<u32x4_t*>(p)[0] = u32x4_t{v[0], v[1], v[2], v[3]};
+    reinterpret_cast<u32x4_t*>(p)[1] = u32x4_t{v[4], v[5], v[6], v[7]};
+    return;
+  }
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i]);
+  put_logits(a, row, c, f);
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::THREADS) void gate_logits_kernel(GateArgs a) {
+  using Tl = tile::Tile<S, false, false, true>;
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const Rows r(a);
+  const int nt = ceil_div(a.Ep, Tl::BN), stages = a.H / 64;
+  int m, n;
+  if (!tile::pick(blockIdx.x, ceil_div(r.e - r.b, Tl::BM), nt * a.split, &m, &n)) return;
+  const int part = n / nt, n0 = n % nt * Tl::BN, row = r.b + m * Tl::BM, rows = min(r.e - row, Tl::BM);
+  const int k0 = stages * part / a.split * 64, k1 = stages * (part + 1) / a.split * 64;
+  const tile::Operand A{bytes(a.x + (size_t)row * a.H + k0), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
+  const tile::Operand B{bytes(a.gate + (size_t)k0 * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
+  Tl::template epilogue<false>(acc, lds, rows, [&](int i, int c, const auto& v) { put(a, part, row + i, n0 + c, v); });
+}
+
+template <int NW>
+__global__ __launch_bounds__(NW * 64) void gate_logits_few_kernel(GateArgs a) {
+  using Fw = tile::Few<NW, false, true, false>;
+  __shared__ __attribute__((aligned(1024))) char lds[Fw::LDS];
+  const Rows r(a);
+  const int nt = ceil_div(a.Ep, Fw::COLS), steps = a.H / Fw::KE, mt = ceil_div(r.e - r.b, Fw::BM);
+  int m, n;
+  if (!tile::pick(blockIdx.x, mt, nt * a.split, &m, &n)) return;
+  const int part = n / nt, n0 = n % nt * Fw::COLS, row = r.b + m * Fw::BM;
+  const tile::Operand A{bytes(a.x + (size_t)row * a.H), nullptr, (uint32_t)a.H * 2, min(r.e - row, Fw::BM), 0, 0};
+  const tile::Operand B{bytes(a.gate), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
+  Fw::run(lds, A, B, steps * part / a.split, steps * (part + 1) / a.split, mt == 1,
+          [&](int i, int c, const auto& v) { put(a, part, row + i, n0 + c, v); });
+}
+
+__global__ __launch_bounds__(256) void gate_logits_sum_kernel(GateArgs a) {
+  const Rows r(a);
+  const long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 8, row = i / a.Ep, c = i % a.Ep;
+  if (row < r.b || row >= r.e) return;
+  float v[8] = {};
+  for (int s = 0; s < a.split; ++s) {
+    const float* p = a.part + ((size_t)s * a.T + row) * a.Ep + c;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += p[j];
+  }
+  put_logits(a, row, (int)c, v);
+}
+
+__device__ __forceinline__ void store8(uint16_t* p, const uint32_t* v) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i]);
+  *reinterpret_cast<u32x4_t*>(p) = tile::pack8(f);
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::THREADS) void gate_dx_kernel(GateArgs a) {
+  using Tl = tile::Tile<S, false, false, false>;
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const Rows r(a);
+  int m, n;
+  if (!tile::pick(blockIdx.x, ceil_div(r.e - r.b, Tl::BM), ceil_div(a.H, Tl::BN), &m, &n)) return;
+  const int n0 = n * Tl::BN, row = r.b + m * Tl::BM, rows = min(r.e - row, Tl::BM);
+  const tile::Operand A{bytes(a.d + (size_t)row * a.Ep), nullptr, (uint32_t)a.Ep * 2, rows, 0, 0};
+  const tile::Operand B{bytes(a.gate + (size_t)n0 * a.Ep), nullptr, (uint32_t)a.Ep * 2, a.H - n0, 0, 0};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, a.Ep, A, B, 0);
+  Tl::template epilogue<false>(acc, lds, rows, [&](int i, int c, const auto& v) {
+    if (n0 + c < a.H) store8(a.dx + (size_t)(row + i) * a.H + n0 + c, v);
+  });
+}
+
+// dwg: tiles of 128 or 256 columns of x by the experts, the rows their depth.
+// Parts of the rows follow each other, so that the tiles that read the same rows of
+// dlogits run on one XCD.
+template <typename S>
+__global__ __launch_bounds__(S::THREADS) void gate_dwg_kernel(GateArgs a) {
+  using Tl = tile::Tile<S, false, true, true>;
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const Rows r(a);
+  const int mt = ceil_div(a.H, Tl::BM), nt = ceil_div(a.E, Tl::BN), per = mt * nt, run = ceil_div(per * a.split, NXCD);
+  const int w = blockIdx.x % NXCD * run + blockIdx.x / NXCD;
+  if ((int)blockIdx.x / NXCD >= run || w >= per * a.split) return;
+  const int part = w / per, m0 = w % per % mt * Tl::BM, n0 = w % per / mt * Tl::BN;
+  const int stages = ceil_div(r.e - r.b, 64);
+  const int k0 = stages * part / a.split * 64, k1 = min(stages * (part + 1) / a.split * 64, r.e - r.b);
+  const tile::Operand A{bytes(a.x + (size_t)(r.b + k0) * a.H), nullptr, (uint32_t)a.H * 2, 0, m0, a.H};
+  const tile::Operand B{bytes(a.d + (size_t)(r.b + k0) * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
+  float* sums = a.part + (size_t)part * a.H * a.Ep;
+  Tl::template epilogue<false>(acc, lds, min(Tl::BM, a.H - m0), [&](int i, int c, const uint32_t (&v)[8]) {
+    c += n0;
+    if (c >= a.Ep) return;
+    u32x4_t* o = reinterpret_cast<u32x4_t*>(sums + (size_t)(m0 + i) * a.Ep + c);
+    o[0] = u32x4_t{v[0], v[1], v[2], v[3]};
+    o[1] = u32x4_t{v[4], v[5], v[6], v[7]};
+  });
+}
+__global__ __launch_bounds__(256) void gate_dwg_sum_kernel(GateArgs a) {
+  const int i = blockIdx.x * 256 + threadIdx.x, h = i / (a.Ep / 4), c = i % (a.Ep / 4) * 4;
+  if (h >= a.H || c >= a.E) return;
+  f32x4_t v{0, 0, 0, 0};
+#pragma unroll 4
+  for (int s = 0; s < a.split; ++s) v += *reinterpret_cast<const f32x4_t*>(a.part + ((size_t)s * a.H + h) * a.Ep + c);
+  uint16_t* out = a.dwg + (size_t)h * a.E + c;
+  if (a.E % 4 == 0) {
+    *reinterpret_cast<uint2*>(out) = uint2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c + j < a.E) out[j] = (uint16_t)f32_to_bf16(v[j]);
   }
 }
 
@@ -459,12 +641,6 @@ moe_status check_ws(const void* ws, size_t bytes, size_t need) {
   return MOE_OK;
 }
 
-GateArgs gate_args(const moe_router_config* c, const int32_t* off) {
-  GateArgs a{};
-  a.T = c->rows, a.H = c->hidden, a.E = c->n_experts, a.S = c->n_seqs, a.off = off;
-  return a;
-}
-
 // About 1024 tiles of a long batch, whose sums fit the caches; 32 rows at least
 // (the four wavefronts' 4 to 32 at once).
 LossArgs loss_args(const moe_router_config* c, const int32_t* off) {
@@ -491,7 +667,67 @@ LossSpace loss_space(const LossArgs& a) {
   return w;
 }
 
-size_t gate_ws(const moe_router_config*, bool) { return 256; }
+// How the gate's products are computed, from the config alone.
+struct GatePlan {
+  int Ep;           // columns of the gate
+  bool copied;      // the gate is copied to have them
+  tile::Plan prod;  // logits, or dx
+  tile::Plan::Kind dwg;
+  int dwg_split, bias_parts;
+};
+GatePlan logits_plan(const moe_router_config* c) {
+  GatePlan p{};
+  p.Ep = ceil_div(c->n_experts, 8) * 8;
+  p.copied = p.Ep != c->n_experts;
+  p.prod = tile::plan_of(c->rows, 1, p.Ep, 1, c->hidden / 64, true);
+  return p;
+}
+GatePlan grad_plan(const moe_router_config* c) {
+  GatePlan p{};
+  p.Ep = ceil_div(c->n_experts, 64) * 64;
+  p.copied = p.Ep != c->n_experts;
+  p.prod = tile::plan_of(c->rows, 1, c->hidden, 1, p.Ep / 64, false);
+  p.prod.split = 1;
+  const int stages = std::max(1, ceil_div(c->rows, 64));
+  p.dwg = p.Ep > 128 ? tile::Plan::WIDE : tile::Plan::SMALL;
+  const int bm = p.dwg == tile::Plan::WIDE ? 256 : 128, tiles = ceil_div(c->hidden, bm) * ceil_div(p.Ep, bm);
+  const int fill = p.dwg == tile::Plan::WIDE ? 256 : 512;
+  p.dwg_split = std::max(1, std::min(stages, fill / tiles));
+  p.bias_parts = std::max(1, std::min(512, ceil_div(c->rows, 16)));
+  return p;
+}
+
+// Workspace: the gate's copy, dlogits in bf16, dbias's parts, then the products' partial sums.
+struct GateSpace {
+  size_t gate, d, bpart, part, total;
+};
+GateSpace gate_space(const moe_router_config* c, bool backward) {
+  const GatePlan p = backward ? grad_plan(c) : logits_plan(c);
+  GateSpace w{};
+  w.d = p.copied ? align_up(sizeof(uint16_t) * c->hidden * p.Ep, 256) : 0;
+  w.bpart = w.d + (backward ? align_up(sizeof(uint16_t) * (size_t)c->rows * p.Ep, 256) : 0);
+  w.part = w.bpart + (backward ? align_up(sizeof(float) * p.bias_parts * c->n_experts, 256) : 0);
+  const size_t logits = p.prod.split > 1 ? sizeof(float) * (size_t)p.prod.split * c->rows * p.Ep : 0;
+  w.total = w.part + (backward ? sizeof(float) * (size_t)p.dwg_split * c->hidden * p.Ep : logits) + 256;
+  return w;
+}
+size_t gate_ws(const moe_router_config* c, bool backward) { return gate_space(c, backward).total; }
+
+GateArgs gate_args(const moe_router_config* c, const int32_t* off, const uint16_t* wg, bool backward, void* ws, hipStream_t s,
+                   bool gate_read) {
+  const GatePlan p = backward ? grad_plan(c) : logits_plan(c);
+  const GateSpace w = gate_space(c, backward);
+  char* at = static_cast<char*>(ws);
+  GateArgs a{};
+  a.T = c->rows, a.H = c->hidden, a.E = c->n_experts, a.S = c->n_seqs, a.off = off;
+  a.Ep = p.Ep, a.wg = wg;
+  a.d = reinterpret_cast<uint16_t*>(at + w.d);
+  a.bpart = reinterpret_cast<float*>(at + w.bpart), a.part = reinterpret_cast<float*>(at + w.part);
+  a.bias_parts = p.bias_parts;
+  a.gate = p.copied ? reinterpret_cast<uint16_t*>(at) : const_cast<uint16_t*>(wg);
+  if (p.copied && gate_read) gate_copy_kernel<<<ceil_div(a.H * (a.Ep / 8), 256), 256, 0, s>>>(a);
+  return a;
+}
 
 }  // namespace
 
@@ -515,9 +751,22 @@ moe_status moe_gate_logits(const moe_router_config* cfg, const uint16_t* x, cons
   if ((st = check_off(cfg, seq_off)) != MOE_OK) return st;
   if ((st = check_tensors({x, wg, logit_bias, logits})) != MOE_OK) return st;
   if ((st = check_ws(ws, ws_bytes, gate_ws(cfg, false))) != MOE_OK) return st;
-  GateArgs a = gate_args(cfg, seq_off);
-  a.x = x, a.wg = wg, a.bias = logit_bias, a.logits = logits;
-  gate_logits_kernel<<<dim3(a.T, ceil_div(a.E, 256)), 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(a);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  GateArgs a = gate_args(cfg, seq_off, wg, false, ws, s, true);
+  a.x = x, a.bias = logit_bias, a.logits = logits;
+  const tile::Plan p = logits_plan(cfg).prod;
+  a.split = p.split;
+  const auto go = [&](auto kernel, int bm, int bn, int threads) {
+    kernel<<<tile::grid_of(ceil_div(a.T, bm), ceil_div(a.Ep, bn) * a.split), threads, 0, s>>>(a);
+  };
+  using tile::Small, tile::Wide;
+  switch (p.kind) {
+    case tile::Plan::FEW4: go(gate_logits_few_kernel<4>, 32, 64, 256); break;
+    case tile::Plan::FEW8: go(gate_logits_few_kernel<8>, 32, 64, 512); break;
+    case tile::Plan::SMALL: go(gate_logits_kernel<Small>, Small::BM, Small::BN, Small::THREADS); break;
+    case tile::Plan::WIDE: go(gate_logits_kernel<Wide>, Wide::BM, Wide::BN, Wide::THREADS); break;
+  }
+  if (a.split > 1) gate_logits_sum_kernel<<<(int)(((long long)a.T * a.Ep / 8 + 255) / 256), 256, 0, s>>>(a);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }
@@ -532,11 +781,32 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   if ((st = check_off(cfg, seq_off)) != MOE_OK) return st;
   if ((st = check_tensors({dlogits, x, wg, dx, dwg, dbias})) != MOE_OK) return st;
   if ((st = check_ws(ws, ws_bytes, gate_ws(cfg, true))) != MOE_OK) return st;
-  GateArgs a = gate_args(cfg, seq_off);
-  a.x = x, a.wg = wg, a.dlogits = dlogits, a.dx = dx, a.dwg = dwg, a.dbias = dbias;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if (dx && a.T > 0) gate_dx_kernel<<<dim3(a.T, ceil_div(a.H, 256)), 256, 0, s>>>(a);
-  if (dwg || dbias) gate_dwg_kernel<<<dim3(a.H + 1, ceil_div(a.E, 256)), 256, 0, s>>>(a);
+  if (!dx && !dwg && !dbias) return MOE_OK;
+  if (cfg->rows == 0) dx = nullptr;
+  GateArgs a = gate_args(cfg, seq_off, wg, true, ws, s, dx != nullptr);
+  a.x = x, a.dlogits = dlogits, a.dx = dx, a.dwg = dwg, a.dbias = dbias;
+  if (!dx && !dwg) a.d = nullptr;
+  gate_round_kernel<<<dim3(a.bias_parts, a.Ep / 64), 256, 0, s>>>(a);
+  if (dbias) gate_dbias_kernel<<<ceil_div(a.E, 64), 64, 0, s>>>(a);
+  const GatePlan p = grad_plan(cfg);
+  using tile::Small, tile::Wide;
+  if (dx) {
+    const auto go = [&](auto kernel, int bm, int bn, int threads) {
+      kernel<<<tile::grid_of(ceil_div(a.T, bm), ceil_div(a.H, bn)), threads, 0, s>>>(a);
+    };
+    if (p.prod.kind == tile::Plan::WIDE) go(gate_dx_kernel<Wide>, Wide::BM, Wide::BN, Wide::THREADS);
+    else go(gate_dx_kernel<Small>, Small::BM, Small::BN, Small::THREADS);
+  }
+  if (dwg) {
+    a.split = p.dwg_split;
+    const auto go = [&](auto kernel, int bm, int bn, int threads) {
+      kernel<<<ceil_div(ceil_div(a.H, bm) * ceil_div(a.E, bn) * a.split, NXCD) * NXCD, threads, 0, s>>>(a);
+    };
+    if (p.dwg == tile::Plan::WIDE) go(gate_dwg_kernel<Wide>, Wide::BM, Wide::BN, Wide::THREADS);
+    else go(gate_dwg_kernel<Small>, Small::BM, Small::BN, Small::THREADS);
+    gate_dwg_sum_kernel<<<ceil_div(a.H * (a.Ep / 4), 256), 256, 0, s>>>(a);
+  }
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }
