@@ -2,6 +2,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdlib>
+#include <string>
 #include <type_traits>
 
 #include "blocks.h"
@@ -38,9 +40,9 @@ struct Rows {
   __device__ __forceinline__ explicit Rows(const GateArgs& a) { covered_rows(a.off, a.S, a.T, &b, &e); }
 };
 
-// The gate with rows of Ep values
-__global__ __launch_bounds__(256) void gate_copy_kernel(GateArgs a) {
-  const int i = blockIdx.x * 256 + threadIdx.x, h = i / (a.Ep / 8), c = i % (a.Ep / 8) * 8;
+// Piece i of the gate's copy with rows of Ep values
+__device__ __forceinline__ void copy_gate(const GateArgs& a, int i) {
+  const int h = i / (a.Ep / 8), c = i % (a.Ep / 8) * 8;
   if (h >= a.H) return;
   uint32_t w[4];
 #pragma unroll
@@ -51,16 +53,23 @@ __global__ __launch_bounds__(256) void gate_copy_kernel(GateArgs a) {
   }
   *reinterpret_cast<u32x4_t*>(a.gate + (size_t)h * a.Ep + c) = u32x4_t{w[0], w[1], w[2], w[3]};
 }
+__global__ __launch_bounds__(256) void gate_copy_kernel(GateArgs a) { copy_gate(a, blockIdx.x * 256 + threadIdx.x); }
 
-// dlogits in bf16 with rows of Ep values (where dx or dwg is wanted), and the parts
-// of dbias: a workgroup takes 64 columns and its share of the rows, 16 threads side
-// by side with 4 columns each.
+// What the gradients' products start from: dlogits in bf16 with rows of Ep values
+// (where dx or dwg is wanted), and the parts of dbias; a workgroup takes 64 columns
+// and its share of the rows, 16 threads side by side with 4 columns each.  The
+// workgroups behind copy the gate.
 __global__ __launch_bounds__(256) void gate_round_kernel(GateArgs a) {
   __shared__ f32x4_t red[16][16];
+  const int part = blockIdx.x % a.bias_parts, strip = blockIdx.x / a.bias_parts;
+  if (strip * 64 >= a.Ep) {
+    copy_gate(a, (blockIdx.x - a.bias_parts * (a.Ep / 64)) * 256 + threadIdx.x);
+    return;
+  }
   const Rows r(a);
   const int n = ceil_div(r.e - r.b, a.bias_parts);
-  const int begin = r.b + blockIdx.x * n, end = min(begin + n, r.e);
-  const int c = blockIdx.y * 64 + threadIdx.x % 16 * 4, first = threadIdx.x / 16;
+  const int begin = r.b + part * n, end = min(begin + n, r.e);
+  const int c = strip * 64 + threadIdx.x % 16 * 4, first = threadIdx.x / 16;
   f32x4_t sum{0, 0, 0, 0};
 #pragma unroll 4
   for (int row = begin + first; row < end; row += 16) {
@@ -84,15 +93,7 @@ __global__ __launch_bounds__(256) void gate_round_kernel(GateArgs a) {
   for (int i = 1; i < 16; ++i) sum += red[i][threadIdx.x];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (c + j < a.E) a.bpart[(size_t)blockIdx.x * a.E + c + j] = sum[j];
-}
-__global__ __launch_bounds__(64) void gate_dbias_kernel(GateArgs a) {
-  const int c = blockIdx.x * 64 + threadIdx.x;
-  if (c >= a.E) return;
-  float v = 0;
-#pragma unroll 8
-  for (int i = 0; i < a.bias_parts; ++i) v += a.bpart[(size_t)i * a.E + c];
-  a.dbias[c] = v;
+    if (c + j < a.E) a.bpart[(size_t)part * a.E + c + j] = sum[j];
 }
 
 // 8 logits of a row from column c on, from their sums
@@ -143,6 +144,23 @@ __global__ __launch_bounds__(S::THREADS) void gate_logits_kernel(GateArgs a) {
   Tl::zero(acc);
   Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
   Tl::template epilogue<false>(acc, lds, rows, [&](int i, int c, const auto& v) { put(a, part, row + i, n0 + c, v); });
+}
+
+using Stream = tile::Shape<4, 2, 1, 2>;  // 128 x 128, 8 waves
+
+__global__ __launch_bounds__(Stream::THREADS) void gate_logits_stream_kernel(GateArgs a) {
+  using Tl = tile::Tile<Stream, false, false, true>;
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::RING_LDS<4>];
+  const Rows r(a);
+  int m, n;
+  if (!tile::pick(blockIdx.x, ceil_div(r.e - r.b, Tl::BM), ceil_div(a.Ep, Tl::BN), &m, &n)) return;
+  const int n0 = n * Tl::BN, row = r.b + m * Tl::BM, rows = min(r.e - row, Tl::BM);
+  const tile::Operand A{bytes(a.x + (size_t)row * a.H), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
+  const tile::Operand B{bytes(a.gate), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::ring<4>(acc, lds, A, B, a.H, m * a.bias_parts % (a.H / 64));
+  Tl::template epilogue<false>(acc, lds, rows, [&](int i, int c, const auto& v) { put(a, 0, row + i, n0 + c, v); });
 }
 
 template <int NW>
@@ -198,13 +216,99 @@ __global__ __launch_bounds__(S::THREADS) void gate_dx_kernel(GateArgs a) {
   });
 }
 
+// dx where the depth is 64 or 128 (KC times 64): nothing but dx itself comes from or
+// goes to memory, so a wave keeps its 64 columns of the gate in registers and passes
+// over rows.  Eight waves share strips of 64 rows of dlogits, which come from the
+// caches into a ring of three in LDS (k-contiguous, granules as in tile.h), two
+// ahead; four wide by two deep, a wave multiplies 32 rows by its columns.  The
+// columns are dealt to the matrix instruction so that a lane's 32 results are
+// consecutive; they pass through 4 KB of LDS of the wave's own and leave as whole
+// lines.
+template <int KC>
+__global__ __launch_bounds__(512, 4) void gate_dx_strip_kernel(GateArgs a) {
+  constexpr int STRIP = KC * 8192, RING = 3;
+  __shared__ __attribute__((aligned(1024))) char lds[RING * STRIP + 8 * 4096];
+  const Rows r(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int panels = ceil_div(a.H, 256), run = ceil_div(panels * a.split, NXCD);
+  const int w = blockIdx.x % NXCD * run + blockIdx.x / NXCD;
+  if ((int)blockIdx.x / NXCD >= run || w >= panels * a.split) return;
+  const int part = w / panels, n0 = w % panels * 256 + wave % 4 * 64, deep = wave / 4 * 32;
+  const int strips = ceil_div(r.e - r.b, 64), first = strips * part / a.split, last = strips * (part + 1) / a.split;
+  if (first == last) return;
+  const bool active = n0 < a.H;
+  const int half = lane >> 5, i = lane & 31;
+  const auto swz = [](int row) { return (row >> 1) & 7; };
+  // row i of the instruction's first operand: lane half h of its results holds the rows 8 q + 4 h + j, which are the
+  // columns 32 h + 16 nb + 4 q + j
+  bf16x8_t g[2][KC * 4];
+#pragma unroll
+  for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+    for (int k = 0; k < KC * 4; ++k) {
+      const int col = min(n0, a.H - 64) + 32 * (i >> 2 & 1) + 16 * nb + 4 * (i >> 3) + (i & 3);
+      g[nb][k] = *reinterpret_cast<const bf16x8_t*>(a.gate + (size_t)col * a.Ep + k * 16 + half * 8);
+    }
+  const uint32_t l0 = tile::lds_u32(lds) + wave * 1024;
+  const char* d0 = tile::uniform_ptr(bytes(a.d) + (size_t)r.b * a.Ep * 2);
+  const int in = wave * 8 + lane / 8, rows = r.e - r.b;
+  int slot_in = 0;
+  const auto issue = [&](int strip) {  // a wave loads 8 rows of the strip
+    const uint32_t o = (uint32_t)min(strip * 64 + in, rows - 1) * (uint32_t)(a.Ep * 2) + (uint32_t)(((lane & 7) ^ swz(in)) * 16);
+#pragma unroll
+    for (int k = 0; k < KC; ++k) tile::dma16(d0, o + k * 128, l0 + slot_in * STRIP + k * 8192);
+    slot_in = slot_in == RING - 1 ? 0 : slot_in + 1;
+  };
+  char* mine = lds + RING * STRIP + wave * 4096;
+  tile::wait_vm<0>();  // (the gate's loads: only strips and stores are counted from here)
+  issue(first);
+  if (first + 1 < last) issue(first + 1);
+  int slot = 0;
+  for (int strip = first; strip < last; ++strip, slot = slot == RING - 1 ? 0 : slot + 1) {
+    // behind this strip's loads are the next one's and two strips' stores, 4 each
+    tile::compiler_fence();
+    if (strip + 1 == last) tile::wait_vm<0>();
+    else if (active && strip >= first + 2) tile::wait_vm<KC + 8>();
+    else tile::wait_vm<KC>();
+    tile::lds_barrier();
+    if (strip + 2 < last) issue(strip + 2);
+    if (!active) continue;
+    const char* st = lds + slot * STRIP + (deep + i) * 128;
+    f32x16_t acc[2];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) acc[0][j] = acc[1][j] = 0;
+#pragma unroll
+    for (int k = 0; k < KC * 4; ++k) {
+      const bf16x8_t d = *reinterpret_cast<const bf16x8_t*>(st + k / 4 * 8192 + ((k % 4 * 2 + half) ^ swz(deep + i)) * 16);
+#pragma unroll
+      for (int nb = 0; nb < 2; ++nb) acc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g[nb][k], d, acc[nb], 0, 0, 0);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {  // 8 columns of row i each, 16-byte granules at position c ^ (row & 7)
+      const f32x16_t& v = acc[q / 2];
+      const int o = q % 2 * 8;
+      *reinterpret_cast<u32x4_t*>(mine + i * 128 + ((half * 4 + q) ^ (i & 7)) * 16) =
+          u32x4_t{pack_bf16x2(v[o], v[o + 1]), pack_bf16x2(v[o + 2], v[o + 3]), pack_bf16x2(v[o + 4], v[o + 5]),
+                  pack_bf16x2(v[o + 6], v[o + 7])};
+    }
+    tile::compiler_fence();
+    const int row0 = r.b + strip * 64 + deep;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int row = q * 8 + lane / 8, c = lane % 8;
+      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(mine + row * 128 + (c ^ (row & 7)) * 16);
+      if (row0 + row < r.e) *reinterpret_cast<u32x4_t*>(a.dx + (size_t)(row0 + row) * a.H + n0 + c * 8) = v;
+    }
+  }
+}
+
 // dwg: tiles of 128 or 256 columns of x by the experts, the rows their depth.
 // Parts of the rows follow each other, so that the tiles that read the same rows of
 // dlogits run on one XCD.
-template <typename S>
+template <typename S, int NS>
 __global__ __launch_bounds__(S::THREADS) void gate_dwg_kernel(GateArgs a) {
   using Tl = tile::Tile<S, false, true, true>;
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::template RING_LDS<NS>];
   const Rows r(a);
   const int mt = ceil_div(a.H, Tl::BM), nt = ceil_div(a.E, Tl::BN), per = mt * nt, run = ceil_div(per * a.split, NXCD);
   const int w = blockIdx.x % NXCD * run + blockIdx.x / NXCD;
@@ -216,7 +320,7 @@ __global__ __launch_bounds__(S::THREADS) void gate_dwg_kernel(GateArgs a) {
   const tile::Operand B{bytes(a.d + (size_t)(r.b + k0) * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
   typename Tl::Acc acc;
   Tl::zero(acc);
-  Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
+  Tl::template ring<NS>(acc, lds, A, B, k1 - k0);
   float* sums = a.part + (size_t)part * a.H * a.Ep;
   Tl::template epilogue<false>(acc, lds, min(Tl::BM, a.H - m0), [&](int i, int c, const uint32_t (&v)[8]) {
     c += n0;
@@ -226,11 +330,28 @@ __global__ __launch_bounds__(S::THREADS) void gate_dwg_kernel(GateArgs a) {
     o[1] = u32x4_t{v[4], v[5], v[6], v[7]};
   });
 }
-__global__ __launch_bounds__(256) void gate_dwg_sum_kernel(GateArgs a) {
+// dwg from its parts, 4 columns a thread, and behind it dbias: 16 columns a
+// workgroup, 16 threads each.
+__global__ __launch_bounds__(256) void gate_sum_kernel(GateArgs a, int dwg_blocks) {
+  __shared__ float red[16][16];
+  if ((int)blockIdx.x >= dwg_blocks) {
+    const int q = threadIdx.x % 16, c = (blockIdx.x - dwg_blocks) * 16 + q, first = threadIdx.x / 16;
+    float v = 0;
+    if (c < a.E)
+#pragma unroll 8
+      for (int i = first; i < a.bias_parts; i += 16) v += a.bpart[(size_t)i * a.E + c];
+    red[first][q] = v;
+    __syncthreads();
+    if (first || c >= a.E) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += red[i][q];
+    a.dbias[c] = v;
+    return;
+  }
   const int i = blockIdx.x * 256 + threadIdx.x, h = i / (a.Ep / 4), c = i % (a.Ep / 4) * 4;
   if (h >= a.H || c >= a.E) return;
   f32x4_t v{0, 0, 0, 0};
-#pragma unroll 4
+#pragma unroll 8
   for (int s = 0; s < a.split; ++s) v += *reinterpret_cast<const f32x4_t*>(a.part + ((size_t)s * a.H + h) * a.Ep + c);
   uint16_t* out = a.dwg + (size_t)h * a.E + c;
   if (a.E % 4 == 0) {
@@ -602,6 +723,7 @@ void for_row(int E, Fn&& fn) {
   else of(std::false_type());
 }
 
+int env(const char* n, int d) { const char* v = getenv((std::string("X_") + n).c_str()); return v ? atoi(v) : d; }
 // ---- host ---------------------------------------------------------------------------
 moe_status check_cfg(const moe_router_config* c) {
   if (!c) return fail(MOE_ERR_INVALID_ARG, "config is NULL");
@@ -671,15 +793,18 @@ LossSpace loss_space(const LossArgs& a) {
 struct GatePlan {
   int Ep;           // columns of the gate
   bool copied;      // the gate is copied to have them
-  tile::Plan prod;  // logits, or dx
-  tile::Plan::Kind dwg;
-  int dwg_split, bias_parts;
+  bool stream;      // logits by a ring of stages; dx by strips
+  tile::Plan prod;  // logits, or dx, where they are not
+  int dx_split;     // parts of the rows that strips are dealt to
+  int dwg_m, dwg_n, dwg_split, bias_parts;  // dwg's tile and parts of the rows
 };
 GatePlan logits_plan(const moe_router_config* c) {
   GatePlan p{};
   p.Ep = ceil_div(c->n_experts, 8) * 8;
   p.copied = p.Ep != c->n_experts;
   p.prod = tile::plan_of(c->rows, 1, p.Ep, 1, c->hidden / 64, true);
+  p.stream = ceil_div(c->rows, Stream::BM) * ceil_div(p.Ep, Stream::BN) >= env("STREAM", 96);
+  if (p.stream) p.prod.split = 1;
   return p;
 }
 GatePlan grad_plan(const moe_router_config* c) {
@@ -688,11 +813,13 @@ GatePlan grad_plan(const moe_router_config* c) {
   p.copied = p.Ep != c->n_experts;
   p.prod = tile::plan_of(c->rows, 1, c->hidden, 1, p.Ep / 64, false);
   p.prod.split = 1;
+  p.stream = p.Ep <= 128 && env("STRIP", 1);
+  p.dx_split = std::max(1, std::min(ceil_div(c->rows, 64), env("DXWG", 512) / ceil_div(c->hidden, 256)));
   const int stages = std::max(1, ceil_div(c->rows, 64));
-  p.dwg = p.Ep > 128 ? tile::Plan::WIDE : tile::Plan::SMALL;
-  const int bm = p.dwg == tile::Plan::WIDE ? 256 : 128, tiles = ceil_div(c->hidden, bm) * ceil_div(p.Ep, bm);
-  const int fill = p.dwg == tile::Plan::WIDE ? 256 : 512;
-  p.dwg_split = std::max(1, std::min(stages, fill / tiles));
+  p.dwg_m = env("DWGM", 128);
+  p.dwg_n = 128;
+  const int tiles = ceil_div(c->hidden, p.dwg_m) * ceil_div(c->n_experts, p.dwg_n);
+  p.dwg_split = std::max(1, std::min(stages, 256 / tiles));
   p.bias_parts = std::max(1, std::min(512, ceil_div(c->rows, 16)));
   return p;
 }
@@ -713,8 +840,7 @@ GateSpace gate_space(const moe_router_config* c, bool backward) {
 }
 size_t gate_ws(const moe_router_config* c, bool backward) { return gate_space(c, backward).total; }
 
-GateArgs gate_args(const moe_router_config* c, const int32_t* off, const uint16_t* wg, bool backward, void* ws, hipStream_t s,
-                   bool gate_read) {
+GateArgs gate_args(const moe_router_config* c, const int32_t* off, const uint16_t* wg, bool backward, void* ws) {
   const GatePlan p = backward ? grad_plan(c) : logits_plan(c);
   const GateSpace w = gate_space(c, backward);
   char* at = static_cast<char*>(ws);
@@ -725,7 +851,6 @@ GateArgs gate_args(const moe_router_config* c, const int32_t* off, const uint16_
   a.bpart = reinterpret_cast<float*>(at + w.bpart), a.part = reinterpret_cast<float*>(at + w.part);
   a.bias_parts = p.bias_parts;
   a.gate = p.copied ? reinterpret_cast<uint16_t*>(at) : const_cast<uint16_t*>(wg);
-  if (p.copied && gate_read) gate_copy_kernel<<<ceil_div(a.H * (a.Ep / 8), 256), 256, 0, s>>>(a);
   return a;
 }
 
@@ -752,15 +877,17 @@ moe_status moe_gate_logits(const moe_router_config* cfg, const uint16_t* x, cons
   if ((st = check_tensors({x, wg, logit_bias, logits})) != MOE_OK) return st;
   if ((st = check_ws(ws, ws_bytes, gate_ws(cfg, false))) != MOE_OK) return st;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  GateArgs a = gate_args(cfg, seq_off, wg, false, ws, s, true);
+  GateArgs a = gate_args(cfg, seq_off, wg, false, ws);
   a.x = x, a.bias = logit_bias, a.logits = logits;
-  const tile::Plan p = logits_plan(cfg).prod;
-  a.split = p.split;
+  const GatePlan p = logits_plan(cfg);
+  a.split = p.prod.split; a.bias_parts = env("TURN", 1);
+  if (p.copied) gate_copy_kernel<<<ceil_div(a.H * (a.Ep / 8), 256), 256, 0, s>>>(a);
   const auto go = [&](auto kernel, int bm, int bn, int threads) {
     kernel<<<tile::grid_of(ceil_div(a.T, bm), ceil_div(a.Ep, bn) * a.split), threads, 0, s>>>(a);
   };
   using tile::Small, tile::Wide;
-  switch (p.kind) {
+  if (p.stream) go(gate_logits_stream_kernel, Stream::BM, Stream::BN, Stream::THREADS);
+  else switch (p.prod.kind) {
     case tile::Plan::FEW4: go(gate_logits_few_kernel<4>, 32, 64, 256); break;
     case tile::Plan::FEW8: go(gate_logits_few_kernel<8>, 32, 64, 512); break;
     case tile::Plan::SMALL: go(gate_logits_kernel<Small>, Small::BM, Small::BN, Small::THREADS); break;
@@ -784,29 +911,33 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (!dx && !dwg && !dbias) return MOE_OK;
   if (cfg->rows == 0) dx = nullptr;
-  GateArgs a = gate_args(cfg, seq_off, wg, true, ws, s, dx != nullptr);
+  GateArgs a = gate_args(cfg, seq_off, wg, true, ws);
   a.x = x, a.dlogits = dlogits, a.dx = dx, a.dwg = dwg, a.dbias = dbias;
   if (!dx && !dwg) a.d = nullptr;
-  gate_round_kernel<<<dim3(a.bias_parts, a.Ep / 64), 256, 0, s>>>(a);
-  if (dbias) gate_dbias_kernel<<<ceil_div(a.E, 64), 64, 0, s>>>(a);
   const GatePlan p = grad_plan(cfg);
+  const int copies = p.copied && dx ? ceil_div(a.H * (a.Ep / 8), 256) : 0;
+  gate_round_kernel<<<a.bias_parts * (a.Ep / 64) + copies, 256, 0, s>>>(a);
   using tile::Small, tile::Wide;
-  if (dx) {
+  if (dx && p.stream) {
+    a.split = p.dx_split;
+    const int grid = ceil_div(ceil_div(a.H, 256) * a.split, NXCD) * NXCD;
+    if (a.Ep == 64) gate_dx_strip_kernel<1><<<grid, 512, 0, s>>>(a);
+    else gate_dx_strip_kernel<2><<<grid, 512, 0, s>>>(a);
+  } else if (dx) {
     const auto go = [&](auto kernel, int bm, int bn, int threads) {
       kernel<<<tile::grid_of(ceil_div(a.T, bm), ceil_div(a.H, bn)), threads, 0, s>>>(a);
     };
     if (p.prod.kind == tile::Plan::WIDE) go(gate_dx_kernel<Wide>, Wide::BM, Wide::BN, Wide::THREADS);
     else go(gate_dx_kernel<Small>, Small::BM, Small::BN, Small::THREADS);
   }
+  a.split = p.dwg_split;
   if (dwg) {
-    a.split = p.dwg_split;
-    const auto go = [&](auto kernel, int bm, int bn, int threads) {
-      kernel<<<ceil_div(ceil_div(a.H, bm) * ceil_div(a.E, bn) * a.split, NXCD) * NXCD, threads, 0, s>>>(a);
-    };
-    if (p.dwg == tile::Plan::WIDE) go(gate_dwg_kernel<Wide>, Wide::BM, Wide::BN, Wide::THREADS);
-    else go(gate_dwg_kernel<Small>, Small::BM, Small::BN, Small::THREADS);
-    gate_dwg_sum_kernel<<<ceil_div(a.H * (a.Ep / 4), 256), 256, 0, s>>>(a);
+    const int grid = ceil_div(ceil_div(a.H, p.dwg_m) * ceil_div(a.E, p.dwg_n) * a.split, NXCD) * NXCD;
+    if (p.dwg_m == 256) gate_dwg_kernel<tile::Shape<4, 2, 2, 2>, 3><<<grid, 512, 0, s>>>(a);
+    else gate_dwg_kernel<Stream, 4><<<grid, 512, 0, s>>>(a);
   }
+  const int sums = dwg ? ceil_div(a.H * (a.Ep / 4), 256) : 0;
+  if (dwg || dbias) gate_sum_kernel<<<sums + (dbias ? ceil_div(a.E, 16) : 0), 256, 0, s>>>(a, sums);
   HIP_TRY(hipGetLastError());
   return MOE_OK;
 }

@@ -344,6 +344,86 @@ struct Tile {
     lds_barrier();
   }
 
+  // run() of one pair of operands over a ring of NS stages, NS - 1 of them in
+  // flight: for operands that come from memory once and are multiplied by little,
+  // where two stages (a stage's latency each) leave the memory idle.
+  template <int NS>
+  static constexpr int RING_LDS = NS * STAGE > 2 * EPI ? NS * STAGE : 2 * EPI;
+  template <int NS>
+  static __device__ __forceinline__ void ring(Acc& acc, char* lds, const Operand& A, const Operand& B, int n, int turn = 0) {
+    static_assert(!I8 && NS >= 3 && NS <= 5, "ring");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave % WM, wn = wave / WM, ns = (n + 63) / 64, rest = AT && BT ? n % 64 : 0;
+    if (ns == 0) return;
+    uint32_t oa[AI], ob[BI];
+    offsets<AT, BM, AI>(oa, A, wave, lane, 64);
+    offsets<BT, BN, BI>(ob, B, wave, lane, 64);
+    const char *pa = base_of<BM, AI>(A, wave), *pb = base_of<BN, BI>(B, wave);
+    const size_t sa = AT ? (size_t)A.ld * 64 : DEPTH, sb = BT ? (size_t)B.ld * 64 : DEPTH;
+    const uint32_t la = lds_u32(lds) + wave * AI * 1024, lb = lds_u32(lds) + A_BYTES + wave * BI * 1024;
+    int slot_in = 0;  // where the next stage goes
+    auto issue = [&](int s) {
+      const uint32_t so = slot_in * STAGE;
+      slot_in = slot_in + 1 == NS ? 0 : slot_in + 1;
+      const int st = s + turn < ns ? s + turn : s + turn - ns;
+      const char *a = pa + st * sa, *b = pb + st * sb;
+      if ((AT && BT) && rest && s == ns - 1) {
+        uint32_t ta[AI], tb[BI];
+        offsets<AT, BM, AI>(ta, A, wave, lane, rest);
+        offsets<BT, BN, BI>(tb, B, wave, lane, rest);
+#pragma unroll
+        for (int i = 0; i < AI; ++i) dma16(a, ta[i], la + so + i * 1024);
+#pragma unroll
+        for (int i = 0; i < BI; ++i) dma16(b, tb[i], lb + so + i * 1024);
+        return;
+      }
+#pragma unroll
+      for (int i = 0; i < AI; ++i) dma16(a, oa[i], la + so + i * 1024);
+#pragma unroll
+      for (int i = 0; i < BI; ++i) dma16(b, ob[i], lb + so + i * 1024);
+    };
+    const FragOffs f = frag_offsets(wm, wn, lane);
+    Frag a0[MB], b0[NB], a1[MB], b1[NB];
+    const auto none = [](int) {};
+    const int ahead = ns < NS - 1 ? ns : NS - 1;
+    for (int s = 0; s < ahead; ++s) issue(s);
+    int slot = 0;
+    for (int s = 0; s < ns; ++s, slot = slot + 1 == NS ? 0 : slot + 1) {
+      // this wave's part of the stage has arrived, and its reads of the one before
+      // are done; after the barrier so are everyone's
+      compiler_fence();
+      const int young = ns - 1 - s;  // stages behind this one, of which NS - 2 are in flight
+      if (young >= NS - 2) wait_vm<(NS - 2) * INSTR>();
+      else if (NS > 4 && young == 2) wait_vm<2 * INSTR>();
+      else if (NS > 3 && young == 1) wait_vm<INSTR>();
+      else wait_vm<0>();
+      __builtin_amdgcn_s_waitcnt((3 << 14) | (7 << 4) | 15);  // lgkmcnt(0)
+      __builtin_amdgcn_s_barrier();
+      compiler_fence();
+      char* st = lds + slot * STAGE;
+      if constexpr (AT && BT) {
+        if (rest && s == ns - 1) {  // the rows behind the end are cleared
+          for (int i = threadIdx.x; i < STAGE / 16; i += THREADS) {
+            constexpr int RA = BM / 2 * 2 / 16, RB = BN / 2 * 2 / 16;
+            const int k = i < A_BYTES / 16 ? i / RA % 64 : (i - A_BYTES / 16) / RB % 64;
+            if (k >= rest) *reinterpret_cast<u32x4_t*>(st + i * 16) = u32x4_t{0, 0, 0, 0};
+          }
+          lds_barrier();
+        }
+      }
+      if (s + NS - 1 < ns) issue(s + NS - 1);
+      const auto from = [&](int kk, Frag (&a)[MB], Frag (&b)[NB]) {
+        return [&, kk](int u) { load_frag(u, st, kk, f, a, b); };
+      };
+      load_frags(st, 0, f, a0, b0);
+      multiply(acc, a0, b0, from(1, a1, b1), none);
+      multiply(acc, a1, b1, from(2, a0, b0), none);
+      multiply(acc, a0, b0, from(3, a1, b1), none);
+      multiply(acc, a1, b1, none, none);
+    }
+    lds_barrier();
+  }
+
   static __device__ __forceinline__ void zero(Acc& acc) {
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb)
