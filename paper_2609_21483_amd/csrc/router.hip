@@ -30,6 +30,7 @@ struct GateArgs {
   uint16_t *gate, *d;  // workspace: the gate [H][Ep] where it is copied, dlogits [T][Ep]
   float *part, *bpart;  // partial sums: of a split product, and of dbias [dbias_parts][E]
   int split, bias_parts;
+  int dx_split, dx_blocks, dwg_blocks;  // strips' parts of the rows; workgroups of dx and of dwg in one launch
 };
 
 __device__ __forceinline__ const char* bytes(const uint16_t* p) { return reinterpret_cast<const char*>(p); }
@@ -159,7 +160,7 @@ __global__ __launch_bounds__(Stream::THREADS) void gate_logits_stream_kernel(Gat
   const tile::Operand B{bytes(a.gate), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
   typename Tl::Acc acc;
   Tl::zero(acc);
-  Tl::ring<4>(acc, lds, A, B, a.H, m * a.bias_parts % (a.H / 64));
+  Tl::ring<4>(acc, lds, A, B, a.H, 1, m % (a.H / 64));
   Tl::template epilogue<false>(acc, lds, rows, [&](int i, int c, const auto& v) { put(a, 0, row + i, n0 + c, v); });
 }
 
@@ -225,17 +226,16 @@ __global__ __launch_bounds__(S::THREADS) void gate_dx_kernel(GateArgs a) {
 // consecutive; they pass through 4 KB of LDS of the wave's own and leave as whole
 // lines.
 template <int KC>
-__global__ __launch_bounds__(512, 4) void gate_dx_strip_kernel(GateArgs a) {
-  constexpr int STRIP = KC * 8192, RING = 3;
-  __shared__ __attribute__((aligned(1024))) char lds[RING * STRIP + 8 * 4096];
+__device__ __forceinline__ void dx_strips(const GateArgs& a, int block, char* lds) {
+  constexpr int STRIP = KC * 8192, RING = 3;  // and 8 * 4096 bytes behind them
   const Rows r(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int panels = ceil_div(a.H, 256), run = ceil_div(panels * a.split, NXCD);
-  const int w = blockIdx.x % NXCD * run + blockIdx.x / NXCD;
-  if ((int)blockIdx.x / NXCD >= run || w >= panels * a.split) return;
+  const int panels = ceil_div(a.H, 256), run = ceil_div(panels * a.dx_split, NXCD);
+  const int w = block % NXCD * run + block / NXCD;
+  if (block / NXCD >= run || w >= panels * a.dx_split) return;
   const int part = w / panels, n0 = w % panels * 256 + wave % 4 * 64, deep = wave / 4 * 32;
-  const int strips = ceil_div(r.e - r.b, 64), first = strips * part / a.split, last = strips * (part + 1) / a.split;
-  if (first == last) return;
+  const int strips = ceil_div(r.e - r.b, 64);  // dealt to the parts in turn
+  if (part >= strips) return;
   const bool active = n0 < a.H;
   const int half = lane >> 5, i = lane & 31;
   const auto swz = [](int row) { return (row >> 1) & 7; };
@@ -261,17 +261,17 @@ __global__ __launch_bounds__(512, 4) void gate_dx_strip_kernel(GateArgs a) {
   };
   char* mine = lds + RING * STRIP + wave * 4096;
   tile::wait_vm<0>();  // (the gate's loads: only strips and stores are counted from here)
-  issue(first);
-  if (first + 1 < last) issue(first + 1);
-  int slot = 0;
-  for (int strip = first; strip < last; ++strip, slot = slot == RING - 1 ? 0 : slot + 1) {
+  issue(part);
+  if (part + a.dx_split < strips) issue(part + a.dx_split);
+  int slot = 0, turn = 0;
+  for (int strip = part; strip < strips; strip += a.dx_split, slot = slot == RING - 1 ? 0 : slot + 1, ++turn) {
     // behind this strip's loads are the next one's and two strips' stores, 4 each
     tile::compiler_fence();
-    if (strip + 1 == last) tile::wait_vm<0>();
-    else if (active && strip >= first + 2) tile::wait_vm<KC + 8>();
+    if (strip + a.dx_split >= strips) tile::wait_vm<0>();
+    else if (active && turn >= 2) tile::wait_vm<KC + 8>();
     else tile::wait_vm<KC>();
     tile::lds_barrier();
-    if (strip + 2 < last) issue(strip + 2);
+    if (strip + 2 * a.dx_split < strips) issue(strip + 2 * a.dx_split);
     if (!active) continue;
     const char* st = lds + slot * STRIP + (deep + i) * 128;
     f32x16_t acc[2];
@@ -302,27 +302,26 @@ __global__ __launch_bounds__(512, 4) void gate_dx_strip_kernel(GateArgs a) {
   }
 }
 
-// dwg: tiles of 128 or 256 columns of x by the experts, the rows their depth.
-// Parts of the rows follow each other, so that the tiles that read the same rows of
-// dlogits run on one XCD.
-template <typename S, int NS>
-__global__ __launch_bounds__(S::THREADS) void gate_dwg_kernel(GateArgs a) {
-  using Tl = tile::Tile<S, false, true, true>;
-  __shared__ __attribute__((aligned(1024))) char lds[Tl::template RING_LDS<NS>];
+// dwg: tiles of 128 columns of x by 128 experts, the rows their depth, in stages of
+// 64 that are dealt to the parts in turn.  Tiles of one part follow each other: they
+// read the same rows of dlogits and run on one XCD.
+using DwTile = tile::Tile<Stream, false, true, true>;
+__device__ __forceinline__ void dwg_tile(const GateArgs& a, int block, char* lds) {
   const Rows r(a);
-  const int mt = ceil_div(a.H, Tl::BM), nt = ceil_div(a.E, Tl::BN), per = mt * nt, run = ceil_div(per * a.split, NXCD);
-  const int w = blockIdx.x % NXCD * run + blockIdx.x / NXCD;
-  if ((int)blockIdx.x / NXCD >= run || w >= per * a.split) return;
-  const int part = w / per, m0 = w % per % mt * Tl::BM, n0 = w % per / mt * Tl::BN;
-  const int stages = ceil_div(r.e - r.b, 64);
-  const int k0 = stages * part / a.split * 64, k1 = min(stages * (part + 1) / a.split * 64, r.e - r.b);
-  const tile::Operand A{bytes(a.x + (size_t)(r.b + k0) * a.H), nullptr, (uint32_t)a.H * 2, 0, m0, a.H};
-  const tile::Operand B{bytes(a.d + (size_t)(r.b + k0) * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
-  typename Tl::Acc acc;
-  Tl::zero(acc);
-  Tl::template ring<NS>(acc, lds, A, B, k1 - k0);
+  const int mt = ceil_div(a.H, DwTile::BM), nt = ceil_div(a.E, DwTile::BN), per = mt * nt, run = ceil_div(per * a.split, NXCD);
+  const int w = block % NXCD * run + block / NXCD;
+  if (block / NXCD >= run || w >= per * a.split) return;
+  const int part = w / per, m0 = w % per % mt * DwTile::BM, n0 = w % per / mt * DwTile::BN;
+  const int stages = ceil_div(r.e - r.b, 64), mine = stages > part ? (stages - part - 1) / a.split + 1 : 0;
+  const int depth = mine * 64 - (mine && (stages - 1) % a.split == part ? stages * 64 - (r.e - r.b) : 0);
+  const size_t row = r.b + part * 64;
+  const tile::Operand A{bytes(a.x + row * a.H), nullptr, (uint32_t)a.H * 2, 0, m0, a.H};
+  const tile::Operand B{bytes(a.d + row * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
+  typename DwTile::Acc acc;
+  DwTile::zero(acc);
+  DwTile::ring<4>(acc, lds, A, B, depth, a.split, 0);
   float* sums = a.part + (size_t)part * a.H * a.Ep;
-  Tl::template epilogue<false>(acc, lds, min(Tl::BM, a.H - m0), [&](int i, int c, const uint32_t (&v)[8]) {
+  DwTile::epilogue<false>(acc, lds, min(DwTile::BM, a.H - m0), [&](int i, int c, const uint32_t (&v)[8]) {
     c += n0;
     if (c >= a.Ep) return;
     u32x4_t* o = reinterpret_cast<u32x4_t*>(sums + (size_t)(m0 + i) * a.Ep + c);
@@ -330,6 +329,21 @@ __global__ __launch_bounds__(S::THREADS) void gate_dwg_kernel(GateArgs a) {
     o[1] = u32x4_t{v[4], v[5], v[6], v[7]};
   });
 }
+
+// dx, which is written, and dwg, for which x is read, in one launch, in turn by eight
+// workgroups (one for each XCD): either may have none.
+template <int KC>
+__global__ __launch_bounds__(512, 4) void gate_grad_kernel(GateArgs a) {
+  constexpr int LDS = std::max(DwTile::RING_LDS<4>, KC ? 3 * KC * 8192 + 8 * 4096 : 0);
+  __shared__ __attribute__((aligned(1024))) char lds[LDS];
+  const int eights = std::min(a.dx_blocks, a.dwg_blocks) / NXCD, turn = blockIdx.x / NXCD, x = blockIdx.x % NXCD;
+  const bool mixed = turn < 2 * eights;
+  const bool dx = mixed ? turn % 2 == 0 : a.dx_blocks > a.dwg_blocks;
+  const int block = (mixed ? turn / 2 : turn - eights) * NXCD + x;
+  if (KC && dx) dx_strips<KC ? KC : 1>(a, block, lds);
+  else if (!dx) dwg_tile(a, block, lds);
+}
+
 // dwg from its parts, 4 columns a thread, and behind it dbias: 16 columns a
 // workgroup, 16 threads each.
 __global__ __launch_bounds__(256) void gate_sum_kernel(GateArgs a, int dwg_blocks) {
@@ -796,7 +810,7 @@ struct GatePlan {
   bool stream;      // logits by a ring of stages; dx by strips
   tile::Plan prod;  // logits, or dx, where they are not
   int dx_split;     // parts of the rows that strips are dealt to
-  int dwg_m, dwg_n, dwg_split, bias_parts;  // dwg's tile and parts of the rows
+  int dwg_split, bias_parts;  // dwg's and dbias's parts of the rows
 };
 GatePlan logits_plan(const moe_router_config* c) {
   GatePlan p{};
@@ -814,12 +828,9 @@ GatePlan grad_plan(const moe_router_config* c) {
   p.prod = tile::plan_of(c->rows, 1, c->hidden, 1, p.Ep / 64, false);
   p.prod.split = 1;
   p.stream = p.Ep <= 128 && env("STRIP", 1);
-  p.dx_split = std::max(1, std::min(ceil_div(c->rows, 64), env("DXWG", 512) / ceil_div(c->hidden, 256)));
+  p.dx_split = std::max(1, std::min(ceil_div(c->rows, 64), env("DXWG", 256) / ceil_div(c->hidden, 256)));
   const int stages = std::max(1, ceil_div(c->rows, 64));
-  p.dwg_m = env("DWGM", 128);
-  p.dwg_n = 128;
-  const int tiles = ceil_div(c->hidden, p.dwg_m) * ceil_div(c->n_experts, p.dwg_n);
-  p.dwg_split = std::max(1, std::min(stages, 256 / tiles));
+  p.dwg_split = std::max(1, std::min(stages, 256 / (ceil_div(c->hidden, DwTile::BM) * ceil_div(c->n_experts, DwTile::BN))));
   p.bias_parts = std::max(1, std::min(512, ceil_div(c->rows, 16)));
   return p;
 }
@@ -880,7 +891,7 @@ moe_status moe_gate_logits(const moe_router_config* cfg, const uint16_t* x, cons
   GateArgs a = gate_args(cfg, seq_off, wg, false, ws);
   a.x = x, a.bias = logit_bias, a.logits = logits;
   const GatePlan p = logits_plan(cfg);
-  a.split = p.prod.split; a.bias_parts = env("TURN", 1);
+  a.split = p.prod.split;
   if (p.copied) gate_copy_kernel<<<ceil_div(a.H * (a.Ep / 8), 256), 256, 0, s>>>(a);
   const auto go = [&](auto kernel, int bm, int bn, int threads) {
     kernel<<<tile::grid_of(ceil_div(a.T, bm), ceil_div(a.Ep, bn) * a.split), threads, 0, s>>>(a);
@@ -917,25 +928,22 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   const GatePlan p = grad_plan(cfg);
   const int copies = p.copied && dx ? ceil_div(a.H * (a.Ep / 8), 256) : 0;
   gate_round_kernel<<<a.bias_parts * (a.Ep / 64) + copies, 256, 0, s>>>(a);
-  using tile::Small, tile::Wide;
-  if (dx && p.stream) {
-    a.split = p.dx_split;
-    const int grid = ceil_div(ceil_div(a.H, 256) * a.split, NXCD) * NXCD;
-    if (a.Ep == 64) gate_dx_strip_kernel<1><<<grid, 512, 0, s>>>(a);
-    else gate_dx_strip_kernel<2><<<grid, 512, 0, s>>>(a);
-  } else if (dx) {
+  if (dx && !p.stream) {
+    using tile::Small, tile::Wide;
     const auto go = [&](auto kernel, int bm, int bn, int threads) {
       kernel<<<tile::grid_of(ceil_div(a.T, bm), ceil_div(a.H, bn)), threads, 0, s>>>(a);
     };
     if (p.prod.kind == tile::Plan::WIDE) go(gate_dx_kernel<Wide>, Wide::BM, Wide::BN, Wide::THREADS);
     else go(gate_dx_kernel<Small>, Small::BM, Small::BN, Small::THREADS);
   }
-  a.split = p.dwg_split;
-  if (dwg) {
-    const int grid = ceil_div(ceil_div(a.H, p.dwg_m) * ceil_div(a.E, p.dwg_n) * a.split, NXCD) * NXCD;
-    if (p.dwg_m == 256) gate_dwg_kernel<tile::Shape<4, 2, 2, 2>, 3><<<grid, 512, 0, s>>>(a);
-    else gate_dwg_kernel<Stream, 4><<<grid, 512, 0, s>>>(a);
-  }
+  a.split = p.dwg_split, a.dx_split = p.dx_split;
+  const auto eights = [](int n) { return ceil_div(n, NXCD) * NXCD; };
+  a.dx_blocks = dx && p.stream ? eights(ceil_div(a.H, 256) * a.dx_split) : 0;
+  a.dwg_blocks = dwg ? eights(ceil_div(a.H, DwTile::BM) * ceil_div(a.E, DwTile::BN) * a.split) : 0;
+  const int grid = a.dx_blocks + a.dwg_blocks;
+  if (grid && a.dx_blocks == 0) gate_grad_kernel<0><<<grid, 512, 0, s>>>(a);
+  else if (grid && a.Ep == 64) gate_grad_kernel<1><<<grid, 512, 0, s>>>(a);
+  else if (grid) gate_grad_kernel<2><<<grid, 512, 0, s>>>(a);
   const int sums = dwg ? ceil_div(a.H * (a.Ep / 4), 256) : 0;
   if (dwg || dbias) gate_sum_kernel<<<sums + (dbias ? ceil_div(a.E, 16) : 0), 256, 0, s>>>(a, sums);
   HIP_TRY(hipGetLastError());

@@ -346,11 +346,14 @@ struct Tile {
 
   // run() of one pair of operands over a ring of NS stages, NS - 1 of them in
   // flight: for operands that come from memory once and are multiplied by little,
-  // where two stages (a stage's latency each) leave the memory idle.
+  // where two stages (a stage's latency each) leave the memory idle.  Stages lie
+  // `apart` times their length apart and are taken from `turn` on, around, so that
+  // workgroups that start together need not read from the same memory channels all
+  // along.
   template <int NS>
   static constexpr int RING_LDS = NS * STAGE > 2 * EPI ? NS * STAGE : 2 * EPI;
   template <int NS>
-  static __device__ __forceinline__ void ring(Acc& acc, char* lds, const Operand& A, const Operand& B, int n, int turn = 0) {
+  static __device__ __forceinline__ void ring(Acc& acc, char* lds, const Operand& A, const Operand& B, int n, int apart, int turn) {
     static_assert(!I8 && NS >= 3 && NS <= 5, "ring");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave % WM, wn = wave / WM, ns = (n + 63) / 64, rest = AT && BT ? n % 64 : 0;
@@ -359,7 +362,7 @@ struct Tile {
     offsets<AT, BM, AI>(oa, A, wave, lane, 64);
     offsets<BT, BN, BI>(ob, B, wave, lane, 64);
     const char *pa = base_of<BM, AI>(A, wave), *pb = base_of<BN, BI>(B, wave);
-    const size_t sa = AT ? (size_t)A.ld * 64 : DEPTH, sb = BT ? (size_t)B.ld * 64 : DEPTH;
+    const size_t sa = (AT ? (size_t)A.ld * 64 : DEPTH) * apart, sb = (BT ? (size_t)B.ld * 64 : DEPTH) * apart;
     const uint32_t la = lds_u32(lds) + wave * AI * 1024, lb = lds_u32(lds) + A_BYTES + wave * BI * 1024;
     int slot_in = 0;  // where the next stage goes
     auto issue = [&](int s) {
@@ -367,7 +370,7 @@ struct Tile {
       slot_in = slot_in + 1 == NS ? 0 : slot_in + 1;
       const int st = s + turn < ns ? s + turn : s + turn - ns;
       const char *a = pa + st * sa, *b = pb + st * sb;
-      if ((AT && BT) && rest && s == ns - 1) {
+      if ((AT && BT) && rest && st == ns - 1) {
         uint32_t ta[AI], tb[BI];
         offsets<AT, BM, AI>(ta, A, wave, lane, rest);
         offsets<BT, BN, BI>(tb, B, wave, lane, rest);
@@ -402,7 +405,7 @@ struct Tile {
       compiler_fence();
       char* st = lds + slot * STAGE;
       if constexpr (AT && BT) {
-        if (rest && s == ns - 1) {  // the rows behind the end are cleared
+        if (rest && (s + turn < ns ? s + turn : s + turn - ns) == ns - 1) {  // the rows behind the end are cleared
           for (int i = threadIdx.x; i < STAGE / 16; i += THREADS) {
             constexpr int RA = BM / 2 * 2 / 16, RB = BN / 2 * 2 / 16;
             const int k = i < A_BYTES / 16 ? i / RA % 64 : (i - A_BYTES / 16) / RB % 64;
