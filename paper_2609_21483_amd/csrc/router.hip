@@ -2,8 +2,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
-#include <string>
 #include <type_traits>
 
 #include "blocks.h"
@@ -217,7 +215,7 @@ __global__ __launch_bounds__(S::THREADS) void gate_dx_kernel(GateArgs a) {
   });
 }
 
-// dx where the depth is 64 or 128 (KC times 64): nothing but dx itself comes from or
+// dx where the depth is 64 to 256 (KC times 64): nothing but dx itself comes from or
 // goes to memory, so a wave keeps its 64 columns of the gate in registers and passes
 // over rows.  Eight waves share strips of 64 rows of dlogits, which come from the
 // caches into a ring of three in LDS (k-contiguous, granules as in tile.h), two
@@ -302,6 +300,19 @@ __device__ __forceinline__ void dx_strips(const GateArgs& a, int block, char* ld
   }
 }
 
+// A tile's sums, as one of the parts [split][H][Ep] of dwg
+template <typename Tl>
+__device__ __forceinline__ void put_dwg(const GateArgs& a, const typename Tl::Acc& acc, char* lds, int part, int m0, int n0) {
+  float* sums = a.part + (size_t)part * a.H * a.Ep;
+  Tl::template epilogue<false>(acc, lds, min(Tl::BM, a.H - m0), [&](int i, int c, const uint32_t (&v)[8]) {
+    c += n0;
+    if (c >= a.Ep) return;
+    u32x4_t* o = reinterpret_cast<u32x4_t*>(sums + (size_t)(m0 + i) * a.Ep + c);
+    o[0] = u32x4_t{v[0], v[1], v[2], v[3]};
+    o[1] = u32x4_t{v[4], v[5], v[6], v[7]};
+  });
+}
+
 // dwg: tiles of 128 columns of x by 128 experts, the rows their depth, in stages of
 // 64 that are dealt to the parts in turn.  Tiles of one part follow each other: they
 // read the same rows of dlogits and run on one XCD.
@@ -320,20 +331,33 @@ __device__ __forceinline__ void dwg_tile(const GateArgs& a, int block, char* lds
   typename DwTile::Acc acc;
   DwTile::zero(acc);
   DwTile::ring<4>(acc, lds, A, B, depth, a.split, 0);
-  float* sums = a.part + (size_t)part * a.H * a.Ep;
-  DwTile::epilogue<false>(acc, lds, min(DwTile::BM, a.H - m0), [&](int i, int c, const uint32_t (&v)[8]) {
-    c += n0;
-    if (c >= a.Ep) return;
-    u32x4_t* o = reinterpret_cast<u32x4_t*>(sums + (size_t)(m0 + i) * a.Ep + c);
-    o[0] = u32x4_t{v[0], v[1], v[2], v[3]};
-    o[1] = u32x4_t{v[4], v[5], v[6], v[7]};
-  });
+  put_dwg<DwTile>(a, acc, lds, part, m0, n0);
+}
+
+// The same on 256 x 256 tiles, whose operands come through the L2 half as often;
+// parts of the rows follow each other.
+__global__ __launch_bounds__(512) void gate_dwg_wide_kernel(GateArgs a) {
+  using Tl = tile::Tile<tile::Wide, false, true, true>;
+  __shared__ __attribute__((aligned(1024))) char lds[Tl::LDS];
+  const Rows r(a);
+  const int mt = ceil_div(a.H, Tl::BM), nt = ceil_div(a.E, Tl::BN), per = mt * nt, run = ceil_div(per * a.split, NXCD);
+  const int w = blockIdx.x % NXCD * run + blockIdx.x / NXCD;
+  if ((int)blockIdx.x / NXCD >= run || w >= per * a.split) return;
+  const int part = w / per, m0 = w % per % mt * Tl::BM, n0 = w % per / mt * Tl::BN;
+  const int stages = ceil_div(r.e - r.b, 64);
+  const int k0 = stages * part / a.split * 64, k1 = min(stages * (part + 1) / a.split * 64, r.e - r.b);
+  const tile::Operand A{bytes(a.x + (size_t)(r.b + k0) * a.H), nullptr, (uint32_t)a.H * 2, 0, m0, a.H};
+  const tile::Operand B{bytes(a.d + (size_t)(r.b + k0) * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::run(acc, lds, A, B, k1 - k0, A, B, 0);
+  put_dwg<Tl>(a, acc, lds, part, m0, n0);
 }
 
 // dx, which is written, and dwg, for which x is read, in one launch, in turn by eight
 // workgroups (one for each XCD): either may have none.
 template <int KC>
-__global__ __launch_bounds__(512, 4) void gate_grad_kernel(GateArgs a) {
+__global__ __launch_bounds__(512, 2) void gate_grad_kernel(GateArgs a) {
   constexpr int LDS = std::max(DwTile::RING_LDS<4>, KC ? 3 * KC * 8192 + 8 * 4096 : 0);
   __shared__ __attribute__((aligned(1024))) char lds[LDS];
   const int eights = std::min(a.dx_blocks, a.dwg_blocks) / NXCD, turn = blockIdx.x / NXCD, x = blockIdx.x % NXCD;
@@ -737,7 +761,6 @@ void for_row(int E, Fn&& fn) {
   else of(std::false_type());
 }
 
-int env(const char* n, int d) { const char* v = getenv((std::string("X_") + n).c_str()); return v ? atoi(v) : d; }
 // ---- host ---------------------------------------------------------------------------
 moe_status check_cfg(const moe_router_config* c) {
   if (!c) return fail(MOE_ERR_INVALID_ARG, "config is NULL");
@@ -810,6 +833,7 @@ struct GatePlan {
   bool stream;      // logits by a ring of stages; dx by strips
   tile::Plan prod;  // logits, or dx, where they are not
   int dx_split;     // parts of the rows that strips are dealt to
+  bool dwg_wide;              // dwg on 256 x 256 tiles
   int dwg_split, bias_parts;  // dwg's and dbias's parts of the rows
 };
 GatePlan logits_plan(const moe_router_config* c) {
@@ -817,7 +841,12 @@ GatePlan logits_plan(const moe_router_config* c) {
   p.Ep = ceil_div(c->n_experts, 8) * 8;
   p.copied = p.Ep != c->n_experts;
   p.prod = tile::plan_of(c->rows, 1, p.Ep, 1, c->hidden / 64, true);
-  p.stream = ceil_div(c->rows, Stream::BM) * ceil_div(p.Ep, Stream::BN) >= env("STREAM", 96);
+  // The ring of stages has one workgroup a CU, each 33 us or more at H = 4096 (64
+  // stages).  Ring against plan, us: E = 128, 12288 rows 42 : 38, 20000 46 : 60, 32768
+  // 57 : 85, 65536 117 : 134; E = 8, 32768 rows 60 : 70; E = 256, 16384 rows (256
+  // tiles) 49 : 64, 20000 (314) 79 : 69; E = 512, 32768 rows (1024) 183 : 124.
+  const int tiles = ceil_div(c->rows, Stream::BM) * ceil_div(p.Ep, Stream::BN);
+  p.stream = tiles >= 144 && (p.Ep <= Stream::BN || tiles <= 256);
   if (p.stream) p.prod.split = 1;
   return p;
 }
@@ -827,10 +856,22 @@ GatePlan grad_plan(const moe_router_config* c) {
   p.copied = p.Ep != c->n_experts;
   p.prod = tile::plan_of(c->rows, 1, c->hidden, 1, p.Ep / 64, false);
   p.prod.split = 1;
-  p.stream = p.Ep <= 128 && env("STRIP", 1);
-  p.dx_split = std::max(1, std::min(ceil_div(c->rows, 64), env("DXWG", 256) / ceil_div(c->hidden, 256)));
+  // Strips always where the gate's columns take at most 64 registers of a wave; where
+  // they take 96 or 128, in large or small batches (tiles are a launch of their own).
+  // Strips against tiles, dx alone, us: H = 4096, 32768 rows, E = 128 60 : 88, E = 256
+  // 87 : 122; all gradients, E = 256, 8192 rows 79 : 70, 2048 41 : 32, 512 27 : 36.
+  p.stream = p.Ep <= 128 || (p.Ep <= 256 && (c->rows <= 512 || (long long)c->rows * c->hidden >= 1 << 26));
+  // (256 workgroups: 512, two to a CU, took 4 to 20% longer beside dwg)
+  p.dx_split = std::max(1, std::min(ceil_div(c->rows, 64), 256 / ceil_div(c->hidden, 256)));
   const int stages = std::max(1, ceil_div(c->rows, 64));
-  p.dwg_split = std::max(1, std::min(stages, 256 / (ceil_div(c->hidden, DwTile::BM) * ceil_div(c->n_experts, DwTile::BN))));
+  // Wide tiles where each of 256 workgroups has 20 stages or more.  Wide against 128 x
+  // 128, us with the launches around them: H = 4096, 32768 rows, E = 512 (64 stages)
+  // 152 : 201, E = 300 (64) 132 : 193, E = 256 (32) 103 : 109; 8192 rows, E = 300 (16)
+  // 51 : 55, E = 512 (16) 62 : 60, E = 256 (8) 48 : 38.
+  p.dwg_wide = p.Ep > DwTile::BN &&
+               stages * ceil_div(c->hidden, tile::Wide::BM) * ceil_div(c->n_experts, tile::Wide::BN) >= 20 * 256;
+  const int bm = p.dwg_wide ? tile::Wide::BM : DwTile::BM;
+  p.dwg_split = std::max(1, std::min(stages, 256 / (ceil_div(c->hidden, bm) * ceil_div(c->n_experts, bm))));
   p.bias_parts = std::max(1, std::min(512, ceil_div(c->rows, 16)));
   return p;
 }
@@ -939,11 +980,16 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   a.split = p.dwg_split, a.dx_split = p.dx_split;
   const auto eights = [](int n) { return ceil_div(n, NXCD) * NXCD; };
   a.dx_blocks = dx && p.stream ? eights(ceil_div(a.H, 256) * a.dx_split) : 0;
-  a.dwg_blocks = dwg ? eights(ceil_div(a.H, DwTile::BM) * ceil_div(a.E, DwTile::BN) * a.split) : 0;
+  if (dwg && p.dwg_wide)
+    gate_dwg_wide_kernel<<<eights(ceil_div(a.H, tile::Wide::BM) * ceil_div(a.E, tile::Wide::BN) * a.split), 512, 0, s>>>(a);
+  else if (dwg)
+    a.dwg_blocks = eights(ceil_div(a.H, DwTile::BM) * ceil_div(a.E, DwTile::BN) * a.split);
   const int grid = a.dx_blocks + a.dwg_blocks;
   if (grid && a.dx_blocks == 0) gate_grad_kernel<0><<<grid, 512, 0, s>>>(a);
   else if (grid && a.Ep == 64) gate_grad_kernel<1><<<grid, 512, 0, s>>>(a);
-  else if (grid) gate_grad_kernel<2><<<grid, 512, 0, s>>>(a);
+  else if (grid && a.Ep == 128) gate_grad_kernel<2><<<grid, 512, 0, s>>>(a);
+  else if (grid && a.Ep == 192) gate_grad_kernel<3><<<grid, 512, 0, s>>>(a);
+  else if (grid) gate_grad_kernel<4><<<grid, 512, 0, s>>>(a);
   const int sums = dwg ? ceil_div(a.H * (a.Ep / 4), 256) : 0;
   if (dwg || dbias) gate_sum_kernel<<<sums + (dbias ? ceil_div(a.E, 16) : 0), 256, 0, s>>>(a, sums);
   HIP_TRY(hipGetLastError());
