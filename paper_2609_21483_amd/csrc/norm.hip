@@ -149,12 +149,15 @@ __global__ __launch_bounds__(group_of<THREADS>) void rms_norm_kernel(NormArgs a)
   }
 }
 
-// dx row by row, and each group of threads' part of dweight over its rows.
+// dx row by row, and each workgroup's part of dweight over its rows: bound by memory,
+// so the next row's loads are under way while a row is worked on.
 template <int THREADS, int LOADS>
 __global__ __launch_bounds__(group_of<THREADS>) void rms_norm_grad_kernel(NormGradArgs a) {
-  constexpr int PER = group_of<THREADS> / THREADS;
-  __shared__ float red_a[2][16];
-  const int t = threadIdx.x % THREADS, part = blockIdx.x * PER + threadIdx.x / THREADS;
+  constexpr int PER = group_of<THREADS> / THREADS, W = THREADS * LOADS * 8;
+  constexpr bool AHEAD = THREADS < 1024;  // (1024 threads have no registers for two rows: 222 us against 202, 8192 x 16384)
+  __shared__ float red[2][16];
+  __shared__ __attribute__((aligned(16))) float sums[PER > 1 ? PER * W : 4];
+  const int t = threadIdx.x % THREADS, group = threadIdx.x / THREADS;
   u32x4_t w[LOADS];
   float dw[LOADS][8] = {};
 #pragma unroll
@@ -162,68 +165,90 @@ __global__ __launch_bounds__(group_of<THREADS>) void rms_norm_grad_kernel(NormGr
     const int c = (t + i * THREADS) * 8;
     w[i] = c < a.H ? *reinterpret_cast<const u32x4_t*>(a.weight + c) : u32x4_t{0, 0, 0, 0};
   }
-  int turn = 0;  // two sets of slots in turn: one barrier a row
-  for (int row0 = blockIdx.x * PER; row0 < a.T; row0 += a.parts, turn ^= 1) {
-    const int row = row0 + threadIdx.x / THREADS;
+  struct Given {  // of a row: dy, s, dsum and rstd
+    u32x4_t d[LOADS], s[LOADS], more[LOADS];
+    float r;
+  };
+  const auto load = [&](Given& g, int row) {
     const bool some = row < a.T;
     const size_t at = (size_t)row * a.H;
-    const float r = some ? a.rstd[row] : 0.0f;
-    u32x4_t d[LOADS], s[LOADS], more[LOADS];
+    g.r = some ? a.rstd[row] : 0.0f;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int c = (t + i * THREADS) * 8;
       const bool in = some && c < a.H;
-      d[i] = in ? *reinterpret_cast<const u32x4_t*>(a.dy + at + c) : u32x4_t{0, 0, 0, 0};
-      s[i] = in ? *reinterpret_cast<const u32x4_t*>(a.sum + at + c) : u32x4_t{0, 0, 0, 0};
+      g.d[i] = in ? *reinterpret_cast<const u32x4_t*>(a.dy + at + c) : u32x4_t{0, 0, 0, 0};
+      g.s[i] = in ? *reinterpret_cast<const u32x4_t*>(a.sum + at + c) : u32x4_t{0, 0, 0, 0};
+      g.more[i] = in && a.dsum ? *reinterpret_cast<const u32x4_t*>(a.dsum + at + c) : u32x4_t{0, 0, 0, 0};
     }
-    if (a.dsum && a.dx)
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int c = (t + i * THREADS) * 8;
-        more[i] = some && c < a.H ? *reinterpret_cast<const u32x4_t*>(a.dsum + at + c) : u32x4_t{0, 0, 0, 0};
-      }
+  };
+  int turn = 0;  // two sets of slots in turn: one barrier a row
+  Given next;
+  if (AHEAD) load(next, blockIdx.x * PER + group);
+  for (int row0 = blockIdx.x * PER; row0 < a.T; row0 += a.parts * PER, turn ^= 1) {
+    const int row = row0 + group;
+    if (!AHEAD) load(next, row);
+    const Given g = next;
+    if (AHEAD) load(next, row + a.parts * PER);
     float dot = 0;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       float dv[8], sv[8], wv[8];
-      tile::unpack8(d[i], dv);
-      tile::unpack8(s[i], sv);
+      tile::unpack8(g.d[i], dv);
+      tile::unpack8(g.s[i], sv);
       tile::unpack8(w[i], wv);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float n = sv[j] * r;
+        const float n = sv[j] * g.r;
         dw[i][j] += dv[j] * n;
         dot += dv[j] * wv[j] * n;
       }
     }
     if (!a.dx) continue;
-    const float c0 = sum_of<THREADS>(dot, red_a[turn]) / a.H;
+    const float c0 = sum_of<THREADS>(dot, red[turn]) / a.H;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int c = (t + i * THREADS) * 8;
-      if (!some || c >= a.H) break;
+      if (row >= a.T || c >= a.H) break;
       float dv[8], sv[8], wv[8];
-      tile::unpack8(d[i], dv);
-      tile::unpack8(s[i], sv);
+      tile::unpack8(g.d[i], dv);
+      tile::unpack8(g.s[i], sv);
       tile::unpack8(w[i], wv);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) dv[j] = r * (dv[j] * wv[j] - sv[j] * r * c0);
+      for (int j = 0; j < 8; ++j) dv[j] = g.r * (dv[j] * wv[j] - sv[j] * g.r * c0);
       if (a.dsum) {
-        tile::unpack8(more[i], sv);
+        tile::unpack8(g.more[i], sv);
 #pragma unroll
         for (int j = 0; j < 8; ++j) dv[j] += sv[j];
       }
-      *reinterpret_cast<u32x4_t*>(a.dx + at + c) = tile::pack8(dv);
+      *reinterpret_cast<u32x4_t*>(a.dx + (size_t)row * a.H + c) = tile::pack8(dv);
     }
   }
   if (!a.dweight) return;
+  float* part = a.part + (size_t)blockIdx.x * a.H;
+  if constexpr (PER > 1) {  // the groups' sums first
 #pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int c = (t + i * THREADS) * 8;
-    if (c >= a.H) break;
-    f32x4_t* p = reinterpret_cast<f32x4_t*>(a.part + (size_t)part * a.H + c);
-    p[0] = f32x4_t{dw[i][0], dw[i][1], dw[i][2], dw[i][3]};
-    p[1] = f32x4_t{dw[i][4], dw[i][5], dw[i][6], dw[i][7]};
+    for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; j += 4)
+        *reinterpret_cast<f32x4_t*>(sums + group * W + (t + i * THREADS) * 8 + j) =
+            f32x4_t{dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]};
+    __syncthreads();
+    for (int c = threadIdx.x * 4; c < a.H; c += group_of<THREADS> * 4) {
+      f32x4_t v = *reinterpret_cast<const f32x4_t*>(sums + c);
+#pragma unroll
+      for (int i = 1; i < PER; ++i) v += *reinterpret_cast<const f32x4_t*>(sums + i * W + c);
+      *reinterpret_cast<f32x4_t*>(part + c) = v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int c = (t + i * THREADS) * 8;
+      if (c >= a.H) break;
+#pragma unroll
+      for (int j = 0; j < 8; j += 4)
+        *reinterpret_cast<f32x4_t*>(part + c + j) = f32x4_t{dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]};
+    }
   }
 }
 
@@ -259,11 +284,15 @@ void for_width(int H, Fn&& fn) {
   else fn(integral_constant<int, 1024>(), integral_constant<int, 2>());
 }
 
-// Parts of dweight's sum: the groups of threads that share the rows.
+// Workgroups of the backward pass, each with a part of dweight's sum: as many as
+// load 6 MB of rows at once (dy, s and dsum), 256 at least.  More cost their parts'
+// way out and back.  In 256, 512, 1024 and 2048 workgroups, us: 32768 x 4096 185, 197,
+// 221 and 220; 32768 x 2048 129, 97, 106 and 114; 65536 x 512 67, 48, 52 and 55; 262144
+// x 64 58, 39, 30 and 33.
 int grad_parts(int T, int H) {
   int per = 1;
   for_width(H, [&](auto threads, auto) { per = group_of<threads()> / threads(); });
-  return std::min(ceil_div(T, per), 1024) * per;
+  return std::min(ceil_div(T, per), std::max(256, std::min(1024, (1 << 20) / (per * H))));
 }
 
 moe_status check_cfg(const moe_rms_norm_config* c) {
@@ -331,7 +360,7 @@ moe_status moe_rms_norm_backward(const moe_rms_norm_config* cfg, const uint16_t*
   if (a.T > 0 && (dx || dweight))
     for_width(a.H, [&](auto threads, auto loads) {
       constexpr int group = group_of<threads()>;
-      rms_norm_grad_kernel<threads(), loads()><<<a.parts / (group / threads()), group, 0, s>>>(a);
+      rms_norm_grad_kernel<threads(), loads()><<<a.parts, group, 0, s>>>(a);
     });
   if (dweight) rms_norm_dweight_kernel<<<ceil_div(a.H, 32), 1024, 0, s>>>(a);
   HIP_TRY(hipGetLastError());
