@@ -677,6 +677,100 @@ __global__ __launch_bounds__(1024) void route_loss_seq_kernel(LossArgs a) {
   a.loss[1] = list.live ? z / list.rows : 0.0f;
 }
 
+// A batch whose softmax fits the LDS, by one workgroup: 333 rows of 8 experts in 12 us
+// by the two kernels above, a launch and a chain of memory latencies each.
+constexpr int SMALL_ROWS = 1024, SMALL_P = 16384, SMALL_COUNTS = 4096;
+template <typename R>
+__global__ __launch_bounds__(1024) void route_loss_small_kernel(LossArgs a) {
+  __shared__ float p[SMALL_P];  // [row][Ep]
+  __shared__ int hist[SMALL_COUNTS], start[MOE_MAX_GROUPS + 1];
+  __shared__ float vs[16], zs[16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane % R::LPR, sub = lane / R::LPR;
+  const SeqTiles list(a.off, a.S, a.T, a.bm);
+  int begin = 0;
+  if (a.off) {
+    begin = __builtin_amdgcn_readfirstlane(list.first);
+    if (wave == 0) {
+      int at = list.first;
+      for (int g = list.g0; g < list.g1; ++g) {
+        start[g] = at;
+        at = max(at, clamp_off(a.off[g + 1], a.T));
+      }
+    }
+  } else if (threadIdx.x == 0) {
+    start[0] = 0;
+  }
+  const int end = begin + list.rows;
+  if (threadIdx.x == 0) start[a.S] = end;
+  for (int i = threadIdx.x; i < a.S * a.Ep; i += 1024) hist[i] = 0;
+  float z = 0;
+  for (int base = begin + wave * R::AT_ONCE; base < end; base += 16 * R::AT_ONCE) {
+    const int row = base + sub;
+    float v[R::N], top = -__builtin_inff(), total = 0;
+    R::load(v, a.logits + (size_t)row * a.E, l, a.E, row < end);
+#pragma unroll
+    for (int i = 0; i < R::N; ++i) top = fmaxf(top, v[i]);
+#pragma unroll
+    for (int d = R::LPR / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if (top == -__builtin_inff()) top = 0;  // nothing can be chosen: every exponential is 0
+#pragma unroll
+    for (int i = 0; i < R::N; ++i) {
+      v[i] = __expf(v[i] - top);
+      total += v[i];
+    }
+    total = R::sum(total);
+    const float lse = logf(total) + top, inv = total == 0 ? 0 : 1.0f / total;
+    if (row >= end) continue;
+    if (l == 0) {
+      a.lse[row] = lse;
+      z += total == 0 ? 0 : lse * lse;
+    }
+#pragma unroll
+    for (int i = 0; i < R::N; ++i)
+      if (R::column(l, i) < a.Ep) p[(row - begin) * a.Ep + R::column(l, i)] = v[i] * inv;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < (end - begin) * a.K; i += 1024) {
+    const int e = a.idx[(size_t)begin * a.K + i], row = begin + i / a.K;
+    int g = 0;  // the last sequence that starts at or before the row (those without rows start where the next one does)
+    for (int d = 256; d; d >>= 1)
+      if (g + d < a.S && start[g + d] <= row) g += d;
+    if (e >= 0 && e < a.E) atomicAdd(&hist[g * a.Ep + e], 1);
+  }
+  __syncthreads();
+  // 8 threads a sequence and expert, each over every eighth row
+  float v = 0;
+  for (int q = threadIdx.x / 8; q < a.S * a.Ep; q += 128) {
+    const int g = q / a.Ep, e = q % a.Ep, first = start[g], rows = start[g + 1] - first;
+    float sum = 0;
+#pragma unroll 4
+    for (int row = threadIdx.x % 8; row < rows; row += 8) sum += p[(first - begin + row) * a.Ep + e];
+    if (e < a.E && threadIdx.x % 8 == 0) a.counts[(size_t)g * a.E + e] = hist[q];
+    const float n = (float)rows;
+    if (rows) v += sum * (float)hist[q] * (a.E / (a.K * n * n));
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) {
+    v += __shfl_xor(v, d);
+    z += __shfl_xor(z, d);
+  }
+  if (lane == 0) {
+    vs[wave] = v;
+    zs[wave] = z;
+  }
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int i = 1; i < 16; ++i) {
+    v += vs[i];
+    z += zs[i];
+  }
+  a.loss[0] = list.live ? v / list.live : 0.0f;
+  a.loss[1] = list.live ? z / list.rows : 0.0f;
+}
+bool is_small(const LossArgs& a) {
+  return a.T <= SMALL_ROWS && a.T * a.Ep <= SMALL_P && a.S * a.Ep <= SMALL_COUNTS;
+}
+
 __global__ __launch_bounds__(256) void route_loss_none_kernel(LossArgs a) {
   for (int i = threadIdx.x; i < a.S * a.E; i += 256) a.counts[i] = 0;
   if (threadIdx.x < 2) a.loss[threadIdx.x] = 0;
@@ -1024,6 +1118,8 @@ moe_status moe_route_loss(const moe_router_config* cfg, const float* logits, con
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (a.T == 0) {
     route_loss_none_kernel<<<1, 256, 0, s>>>(a);
+  } else if (is_small(a)) {
+    for_row(a.E, [&](auto row) { route_loss_small_kernel<decltype(row)><<<1, 1024, 0, s>>>(a); });
   } else {
     for_row(a.E, [&](auto row) { route_loss_kernel<decltype(row)><<<max_row_tiles(a.T, a.S, a.bm), 256, 0, s>>>(a); });
     route_loss_seq_kernel<<<dim3(a.S, ceil_div(a.Ep, 32)), 1024, 0, s>>>(a);

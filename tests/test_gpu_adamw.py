@@ -154,7 +154,7 @@ def test_steps_of_any_size(B, bits, mode, grads):
 @pytest.mark.parametrize("bits", [32, 8])
 def test_lists_of_any_length(B, bits):
     """More tensors than one launch takes, of all kinds, empty ones among them."""
-    for count in (1, 47, 48, 49, 97, 200):
+    for count in (1, 63, 64, 65, 66, 67, 68, 83, 84, 85, 169, 200):
         guard = Guarded()
         kinds = [("both", "fp32"), ("bf16", "bf16"), ("fp32", "fp32")]
         ts = [tensor((37 * i) % 700 if i % 11 else 0, *[kinds[i % 3][0], bits, kinds[i % 3][1]], i, 0.1, guard) for i in range(count)]

@@ -266,10 +266,17 @@ def test_losses_of_padded_batches(B, off):
     Loss(B, 256, 60, 4, off, 3, seed=2).verify()
 
 
-@pytest.mark.parametrize("S,T", [(37, 500), (64, 90), (65, 1100), (512, 700), (512, 5)])
-def test_many_sequences(B, S, T):
+@pytest.mark.parametrize("S,T", [(37, 500), (64, 90), (65, 1100), (512, 700), (512, 5), (300, 1024), (85, 341)])
+@pytest.mark.parametrize("E", [7, 8, 48])
+def test_many_sequences(B, S, T, E):
     cut = np.sort(np.random.default_rng(S).integers(0, T + 1, S - 1))
-    Loss(B, T, 48, 3, [0, *cut.tolist(), T], S, seed=3).verify()
+    Loss(B, T, E, 3, [0, *cut.tolist(), T], S, seed=3).verify()
+    Loss(B, T, E, 3, [T // 4, *np.clip(cut, T // 4, T // 2).tolist(), T // 2], S, seed=3).verify()
+
+
+@pytest.mark.parametrize("T,E,S", [(1024, 16, 1), (1025, 16, 1), (1024, 17, 1), (128, 128, 32), (128, 128, 33), (32, 512, 8), (33, 512, 8)])
+def test_losses_about_the_largest_batch_of_one_workgroup(B, T, E, S):
+    Loss(B, T, E, 4, [T * i // S for i in range(S + 1)], S, seed=11).verify()
 
 
 @pytest.mark.parametrize("kw", [dict(weights=False), dict(losses=False), dict(weights=False, losses=False)])
