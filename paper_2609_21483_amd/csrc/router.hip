@@ -33,10 +33,23 @@ struct GateArgs {
 
 __device__ __forceinline__ const char* bytes(const uint16_t* p) { return reinterpret_cast<const char*>(p); }
 
-// The rows that some sequence has, as one group's tiles.
+// The rows that some sequence has: from the first offset to the largest.
 struct Rows {
   int b, e;
-  __device__ __forceinline__ explicit Rows(const GateArgs& a) { covered_rows(a.off, a.S, a.T, &b, &e); }
+  __device__ __forceinline__ explicit Rows(const GateArgs& a) : b(0), e(a.T) {
+    if (!a.off) return;
+    const int lane = threadIdx.x & 63;
+    int first = 0, most = 0;
+    for (int i = lane; i <= a.S; i += 64) {
+      const int v = clamp_off(a.off[i], a.T);
+      if (i == 0) first = v;
+      most = max(most, v);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) most = max(most, __shfl_xor(most, d));
+    b = __builtin_amdgcn_readfirstlane(first);
+    e = __builtin_amdgcn_readfirstlane(most);
+  }
 };
 
 // Piece i of the gate's copy with rows of Ep values
@@ -944,7 +957,7 @@ GatePlan logits_plan(const moe_router_config* c) {
   if (p.stream) p.prod.split = 1;
   return p;
 }
-GatePlan grad_plan(const moe_router_config* c) {
+GatePlan grad_plan(const moe_router_config* c, bool with_dwg = true) {
   GatePlan p{};
   p.Ep = ceil_div(c->n_experts, 64) * 64;
   p.copied = p.Ep != c->n_experts;
@@ -955,8 +968,6 @@ GatePlan grad_plan(const moe_router_config* c) {
   // Strips against tiles, dx alone, us: H = 4096, 32768 rows, E = 128 60 : 88, E = 256
   // 87 : 122; all gradients, E = 256, 8192 rows 79 : 70, 2048 41 : 32, 512 27 : 36.
   p.stream = p.Ep <= 128 || (p.Ep <= 256 && (c->rows <= 512 || (long long)c->rows * c->hidden >= 1 << 26));
-  // (256 workgroups: 512, two to a CU, took 4 to 20% longer beside dwg)
-  p.dx_split = std::max(1, std::min(ceil_div(c->rows, 64), 256 / ceil_div(c->hidden, 256)));
   const int stages = std::max(1, ceil_div(c->rows, 64));
   // Wide tiles where each of 256 workgroups has 20 stages or more.  Wide against 128 x
   // 128, us with the launches around them: H = 4096, 32768 rows, E = 512 (64 stages)
@@ -964,8 +975,16 @@ GatePlan grad_plan(const moe_router_config* c) {
   // 51 : 55, E = 512 (16) 62 : 60, E = 256 (8) 48 : 38.
   p.dwg_wide = p.Ep > DwTile::BN &&
                stages * ceil_div(c->hidden, tile::Wide::BM) * ceil_div(c->n_experts, tile::Wide::BN) >= 20 * 256;
+  // One workgroup a CU: half of the CUs each where both are in one launch.  128 + 128
+  // workgroups against 256 + 256 and 64 + 128 of dx and dwg, us: H = 4096, E = 128, 32768
+  // rows 135 : 144 : 171, 4531 29 : 37 : 35; H = 2048, E = 60, 4531 rows 20 : 24 : 22.  dx
+  // alone takes them all, for its bits do not depend on its parts; dwg's do, and are
+  // the same whatever else is asked for (alone 102 where 256 parts take 75).
+  const bool together = p.stream && !p.dwg_wide;
   const int bm = p.dwg_wide ? tile::Wide::BM : DwTile::BM;
-  p.dwg_split = std::max(1, std::min(stages, 256 / (ceil_div(c->hidden, bm) * ceil_div(c->n_experts, bm))));
+  const auto parts = [&](int most, int tiles) { return std::max(1, std::min(stages, most / tiles)); };
+  p.dwg_split = parts(together ? 128 : 256, ceil_div(c->hidden, bm) * ceil_div(c->n_experts, bm));
+  p.dx_split = parts(together && with_dwg ? 128 : 256, ceil_div(c->hidden, 256));
   p.bias_parts = std::max(1, std::min(512, ceil_div(c->rows, 16)));
   return p;
 }
@@ -1060,7 +1079,7 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   GateArgs a = gate_args(cfg, seq_off, wg, true, ws);
   a.x = x, a.dlogits = dlogits, a.dx = dx, a.dwg = dwg, a.dbias = dbias;
   if (!dx && !dwg) a.d = nullptr;
-  const GatePlan p = grad_plan(cfg);
+  const GatePlan p = grad_plan(cfg, dwg != nullptr);
   const int copies = p.copied && dx ? ceil_div(a.H * (a.Ep / 8), 256) : 0;
   gate_round_kernel<<<a.bias_parts * (a.Ep / 64) + copies, 256, 0, s>>>(a);
   if (dx && !p.stream) {
