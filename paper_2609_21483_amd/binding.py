@@ -430,14 +430,16 @@ def _ws(t: Optional[torch.Tensor], dev: int):
 def _call(name: str, dev: int, stream, *args) -> None:
     """Calls on device `dev`, on the given stream of it or on its current one."""
     if stream is None:
-        stream = torch.cuda.current_stream(dev)
+        raw = torch._C._cuda_getCurrentRawStream(dev)  # current_stream(dev).cuda_stream, without its 1 us object
     elif stream.device_index != dev:
         raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{dev}")
+    else:
+        raw = stream.cuda_stream
     if torch.cuda.current_device() == dev:
-        st = getattr(_lib, name)(*args, stream.cuda_stream)
+        st = getattr(_lib, name)(*args, raw)
     else:
         with torch.cuda.device(dev):
-            st = getattr(_lib, name)(*args, stream.cuda_stream)
+            st = getattr(_lib, name)(*args, raw)
     _check(name, st)
 
 
