@@ -612,52 +612,58 @@ def moe_adamw_tensors(tensors, state_bits: int) -> AdamwTensors:
     """tensors: a dict each, of param (bf16) and/or master (fp32), grad (bf16 or fp32), m and v (fp32, or torch.float8_e4m3fn
     and torch.float8_e5m2 with the fp32 scales m_scale and v_scale of every 256 values) and weight_decay (default 0).  All
     have as many values as grad and lie on one device."""
-    names = ("param", "master", "grad", "m", "v", "m_scale", "v_scale")
     f32 = torch.float32
     if state_bits not in (8, 32):
         raise ValueError(f"state_bits must be 8 or 32, not {state_bits}")
-    kinds = dict(param=torch.bfloat16, master=f32, m=f32, v=f32, m_scale=f32, v_scale=f32)
+    kinds = dict(grad=None, param=torch.bfloat16, master=f32, m=f32, v=f32, m_scale=f32, v_scale=f32)
     if state_bits == 8:
         kinds.update(m=torch.float8_e4m3fn, v=torch.float8_e5m2)
+    known = {*kinds, "weight_decay"}
     tensors = [dict(t) for t in tensors]
     array = (moe_adamw_tensor * len(tensors))()
-    dev, spans = None, []  # spans: first and last byte, whether written, what
+    dev, spans = None, []  # spans: first and last byte, whether written, tensor and name
     for i, t in enumerate(tensors):
-        unknown = set(t) - {*names, "weight_decay"}
-        if unknown:
-            raise ValueError(f"tensor {i}: unknown {sorted(unknown)}")
+        if not t.keys() <= known:
+            raise ValueError(f"tensor {i}: unknown {sorted(t.keys() - known)}")
         grad = t.get("grad")
         dev = _device_of(f"grad of tensor {i}", grad) if dev is None else dev
         if grad is None or grad.dtype not in (torch.bfloat16, f32):
             raise ValueError(f"tensor {i}: grad must be bf16 or fp32")
         if t.get("param") is None and t.get("master") is None:
             raise ValueError(f"tensor {i}: param or master is needed")
-        n, c = grad.numel(), array[i]
+        n, c, shape = grad.numel(), array[i], grad.shape
         c.n, c.weight_decay, c.grad_fp32 = n, float(t.get("weight_decay", 0.0)), int(grad.dtype is f32)
-        c.grad = _arg(f"grad of tensor {i}", grad, grad.dtype, grad.shape, dev)
-        spans.append((c.grad or 0, (c.grad or 0) + grad.nbytes - 1, False, f"grad of tensor {i}"))
         for name, kind in kinds.items():
             v = t.get(name)
-            if name.endswith("_scale") and state_bits == 32:
-                if v is not None:
+            if name.endswith("_scale"):
+                if state_bits == 32 and v is not None:
                     raise ValueError(f"tensor {i}: states in 32 bits have no {name}")
-                continue
-            if v is None and name in ("param", "master"):
-                continue
-            want = (-(-n // MOE_ADAMW_BLOCK),) if name.endswith("_scale") else grad.shape
-            at = _arg(f"{name} of tensor {i}", v, kind, want, dev)
+                if state_bits == 32:
+                    continue
+                want = (-(-n // MOE_ADAMW_BLOCK),)
+            else:
+                if v is None and name in ("param", "master"):
+                    continue
+                want = shape
+            if name == "grad":
+                kind = grad.dtype
+            if v is None or v.dtype is not kind or v.shape != want or v.get_device() != dev or not v.is_contiguous():
+                _arg(f"{name} of tensor {i}", v, kind, want, dev)
+            at = v.data_ptr()
             setattr(c, name, at)
-            spans.append((at or 0, (at or 0) + v.nbytes - 1, True, f"{name} of tensor {i}"))
+            if n:
+                spans.append((at, at + v.nbytes - 1, name != "grad", i, name))
     # what is written is in the list once, and nobody's gradient
-    written, read = (-1, ""), (-1, "")
-    for first, last, writes, what in sorted(s for s in spans if s[1] >= s[0]):
-        for end, other in (written, read) if writes else (written,):
+    spans.sort()
+    written, read = (-1, 0, ""), (-1, 0, "")
+    for first, last, writes, i, name in spans:
+        for end, other, other_name in (written, read) if writes else (written,):
             if first <= end:
-                raise ValueError(f"{what} overlaps the {other}")
+                raise ValueError(f"{name} of tensor {i} overlaps {other_name} of tensor {other}")
         if writes:
-            written = max(written, (last, what))
+            written = max(written, (last, i, name))
         else:
-            read = max(read, (last, what))
+            read = max(read, (last, i, name))
     return AdamwTensors(array, state_bits, dev, tensors)
 
 

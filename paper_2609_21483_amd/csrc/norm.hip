@@ -324,6 +324,7 @@ moe_status moe_rms_norm_forward(const moe_rms_norm_config* cfg, const uint16_t* 
   if (cfg->rows == 0) return MOE_OK;
   if (!x || !weight) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
   if (!y && !q) return fail(MOE_ERR_INVALID_ARG, "y or q is wanted, or both");
+  if (y && y == sum) return fail(MOE_ERR_INVALID_ARG, "y and sum are the same");
   if (!q != !scale) return fail(MOE_ERR_INVALID_ARG, "q and scale are wanted both or neither");
   for (const void* p : {(const void*)x, (const void*)residual, (const void*)weight, (const void*)sum, (const void*)rstd,
                         (const void*)y, (const void*)q, (const void*)scale})

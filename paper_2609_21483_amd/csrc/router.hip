@@ -335,8 +335,9 @@ __device__ __forceinline__ void put_dwg(const GateArgs& a, const typename Tl::Ac
 
 // dwg: tiles of 128 columns of x by 128 experts, the rows their depth, in stages of
 // 64 that are dealt to the parts in turn.  Tiles of one part follow each other: they
-// read the same rows of dlogits and run on one XCD.  32768 x 4096 x 128 alone: 57 us
-// in 256 workgroups, 5 TB/s; 84 with two stages, or with parts of consecutive rows.
+// read the same rows of dlogits and run on one XCD.  32768 x 4096 x 128 in 256
+// workgroups: 57 us alone, 5 TB/s; behind dx, whose writes are still on their way to
+// memory, 78, with parts of consecutive rows 84, and on two stages of Small tiles 85.
 using DwTile = tile::Tile<Stream, false, true, true>;
 __device__ __forceinline__ void dwg_tile(const GateArgs& a, int block, char* lds) {
   const Rows r(a);

@@ -246,6 +246,8 @@ def test_binding_refuses_what_does_not_fit(B):
     with pytest.raises(B.MoeError):
         B.moe_rms_norm_forward(cfg, *good[:5], None, None, None)
     with pytest.raises(B.MoeError):
+        B.moe_rms_norm_forward(cfg, x, None, w, good[5], None, good[5], None, None)
+    with pytest.raises(B.MoeError):
         B.moe_rms_norm_forward(cfg, *good[:5], x.clone(), q, None)
     ws = torch.empty(B.moe_rms_norm_workspace_size(cfg) - 1, dtype=torch.uint8, device="cuda")
     with pytest.raises(B.MoeError):

@@ -30,6 +30,8 @@ def call(name, cfg=None, ws_bytes=1 << 30, **ptr):
     c = None if cfg == "none" else C.byref(kind(*(cfg or usual)))
     at = {**{n: AT for n in names}, "ws": AT, **ptr}
     ws = [P(at["ws"]), ws_bytes] if has_ws else []
+    if name == "moe_rms_norm_forward" and at["sum"] == at["y"] == AT:
+        at["sum"] = 2 * AT
     return getattr(B.library(), name)(c, *[P(at[n]) for n in names], *ws, P(0))
 
 
@@ -71,6 +73,7 @@ def test_other_refusals():
     assert call("moe_rms_norm_forward", y=0, q=0, scale=0) == B.MOE_ERR_INVALID_ARG
     assert call("moe_rms_norm_forward", q=0) == B.MOE_ERR_INVALID_ARG
     assert call("moe_rms_norm_forward", scale=0) == B.MOE_ERR_INVALID_ARG
+    assert call("moe_rms_norm_forward", sum=3 * AT, y=3 * AT) == B.MOE_ERR_INVALID_ARG  # outputs on top of each other
     assert call("moe_route_loss_backward", w=0) == B.MOE_ERR_INVALID_ARG
     assert call("moe_route_loss_backward", dw=0) == B.MOE_ERR_INVALID_ARG
 
@@ -103,7 +106,7 @@ def adamw(cfg=None, now=0, n=None, **t):
 
 
 @pytest.mark.parametrize("cfg", ["none", dict(lr=-1e-3), dict(lr=float("nan")), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
-                                 dict(beta2=float("nan")), dict(eps=0.0), dict(eps=float("inf")), dict(grad_scale=float("nan")),
+                                 dict(beta2=float("nan")), dict(eps=0.0), dict(eps=1e-16), dict(eps=float("inf")), dict(grad_scale=float("nan")),
                                  dict(grad_scale=float("inf")), dict(step=0), dict(step=-3), dict(state_bits=16),
                                  dict(state_bits=8)])
 def test_adamw_refuses_bad_configs(cfg):
