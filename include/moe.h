@@ -538,7 +538,7 @@ moe_status moe_gemm_i8(const moe_gemm_i8_config* cfg, const int8_t* xq, const fl
 
 /* ---- root-mean-square norm with the residual's addition ---- */
 typedef struct {
-  int32_t rows;   /* T, 0..2^22 */
+  int32_t rows;   /* T, 0..2^22 (above H = 8192: below 2^22) */
   int32_t hidden; /* H, multiple of 8, 8..16384 */
   float eps;      /* > 0, added to the mean square */
 } moe_rms_norm_config;
@@ -553,10 +553,11 @@ typedef struct {
  *   q      int8 [T][H] and scale fp32 [T] (both or neither): y in 8 bits as
  *          moe_quantize_rows_i8 would have it, from y in fp32
  * sum may be x or residual, and y may be x (the same address): a row is read
- * before it is written.  Sums are fp32: a row with magnitudes above 2^56 has an
- * infinite mean square, r = 0 and y = 0; one with an infinity or a NaN has y = NaN
- * wherever r or s is not finite, q = 0 and scale = NaN.  A row's results have the
- * same bits in any batch. */
+ * before it is written.  Sums are fp32: a row whose squares add up to more than
+ * fp32 holds (magnitudes above 2^56 may) has r = 0, y = 0 and scale = 0, but NaN where
+ * s weight passes fp32 too; one with an infinity or a NaN has y = NaN wherever r or s
+ * is not finite, q = 0 and scale = NaN.  A row's results have the same bits in any
+ * batch. */
 moe_status moe_rms_norm_forward(const moe_rms_norm_config* cfg, const uint16_t* x, const uint16_t* residual,
                                 const uint16_t* weight, uint16_t* sum, float* rstd, uint16_t* y, int8_t* q,
                                 float* scale, void* stream);
@@ -663,7 +664,7 @@ typedef struct {
  * a scale for every MOE_ADAMW_BLOCK consecutive values, m_scale and v_scale: fp32
  * [ceil(n / 256)] (NULL with 32 bits).  All zeros is the state before the first step. */
 typedef struct {
-  int64_t n; /* 0..2^40 */
+  int64_t n; /* 0..2^36 - 4096 */
   uint16_t* param;
   float* master;
   const void* grad;

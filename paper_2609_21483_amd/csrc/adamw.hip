@@ -12,10 +12,12 @@ namespace {
 
 constexpr int VALUES = 16;           // of a thread
 constexpr int CHUNK = 256 * VALUES;  // of a workgroup
+// Chunks of a launch: a launch has fewer than 2^32 threads
+constexpr int64_t MOST_CHUNKS = (1 << 24) - 1;
 // Tensors of a launch: their addresses are kernel arguments (4 KB at most), so
-// that no table has to reach the device before the step.  A tensor takes 48 bytes (8
-// bits: 56), addresses as multiples of 16: 150 small tensors in two launches, 21 us,
-// against 29 in the four that 72 bytes a tensor make.
+// that no table has to reach the device before the step.  A tensor and its end take 48
+// bytes (8 bits: 60), addresses as multiples of 16: 150 small tensors in two launches, 20
+// us, against 29 in the four that 72 bytes a tensor make.
 template <bool BITS8>
 struct Packed {
   static constexpr int N = BITS8 ? 7 : 5;  // grad, param, master, m, v, m_scale, v_scale
@@ -352,7 +354,7 @@ moe_status check(const moe_adamw_config* c, const moe_adamw_tensor* tensors, int
   if (n < 0 || (n > 0 && !tensors)) return fail(MOE_ERR_INVALID_ARG, "no list of n_tensors tensors");
   for (int32_t i = 0; i < n; ++i) {
     const moe_adamw_tensor& t = tensors[i];
-    if (t.n < 0 || t.n > (1LL << 40)) return fail(MOE_ERR_INVALID_ARG, "tensor %d: n must be in [0, 2^40]", i);
+    if (t.n < 0 || t.n > MOST_CHUNKS * CHUNK) return fail(MOE_ERR_INVALID_ARG, "tensor %d: n must be in [0, 2^36 - 4096]", i);
     if (!finite(t.weight_decay) || t.weight_decay < 0)
       return fail(MOE_ERR_INVALID_ARG, "tensor %d: weight_decay must be finite and not below 0", i);
     if (t.grad_fp32 != 0 && t.grad_fp32 != 1) return fail(MOE_ERR_INVALID_ARG, "tensor %d: grad_fp32 must be 0 or 1", i);
@@ -385,7 +387,9 @@ bool launch(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors, int32_
   for (int32_t i = 0; i < n_tensors; ++i) {
     const moe_adamw_tensor& t = tensors[i];
     if (t.n == 0) continue;
-    const int64_t before = a.count ? a.end[a.count - 1] : 0, chunks = (t.n + CHUNK - 1) / CHUNK;
+    const int64_t chunks = (t.n + CHUNK - 1) / CHUNK;
+    if (a.count == MOST<BITS8> || (a.count && a.end[a.count - 1] + chunks > MOST_CHUNKS)) go();
+    const int64_t before = a.count ? a.end[a.count - 1] : 0;
     Packed<BITS8>& p = a.t[a.count];
     p = {};
     const auto put_half = [&](int k, uint32_t v) { p.high[k / 2] |= v << (k % 2 * 16); };
@@ -400,8 +404,6 @@ bool launch(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors, int32_
     p.decay = t.weight_decay;
     p.place_and_type = (uint32_t)i << 1 | (uint32_t)t.grad_fp32;
     a.end[a.count++] = (uint32_t)(before + chunks);
-    // (2^28 chunks are the largest tensor's: a grid stays below 2^30)
-    if (a.count == MOST<BITS8> || before + chunks > (1 << 28)) go();
   }
   go();
   return any;

@@ -304,6 +304,8 @@ moe_status check_cfg(const moe_rms_norm_config* c) {
   if (c->rows < 0 || c->rows > (1 << 22)) return fail(MOE_ERR_INVALID_ARG, "rows must be in [0, 2^22]");
   if (c->hidden < 8 || c->hidden % 8 || c->hidden > 16384)
     return fail(MOE_ERR_INVALID_ARG, "hidden must be a multiple of 8 in [8, 16384]");
+  if (c->rows == 1 << 22 && c->hidden > 8192)  // (1024 threads each: a launch has fewer than 2^32)
+    return fail(MOE_ERR_INVALID_ARG, "rows must be below 2^22 where hidden is above 8192");
   if (!(c->eps > 0.0f) || !(c->eps < __builtin_inff())) return fail(MOE_ERR_INVALID_ARG, "eps must be above 0 and finite");
   return MOE_OK;
 }

@@ -1085,6 +1085,8 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   if (cfg->rows > 0 && (!dlogits || (dwg && !x) || (dx && !wg))) return fail(MOE_ERR_INVALID_ARG, "NULL argument");
   if ((st = check_off(cfg, seq_off)) != MOE_OK) return st;
   if ((st = check_tensors({dlogits, x, wg, dx, dwg, dbias})) != MOE_OK) return st;
+  if (dx && (dx == x || dx == wg)) return fail(MOE_ERR_INVALID_ARG, "dx is x or wg");
+  if (dwg && (dwg == wg || dwg == x)) return fail(MOE_ERR_INVALID_ARG, "dwg is wg or x");
   if ((st = check_ws(ws, ws_bytes, gate_ws(cfg, true))) != MOE_OK) return st;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   if (!dx && !dwg && !dbias) return MOE_OK;

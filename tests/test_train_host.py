@@ -30,8 +30,8 @@ def call(name, cfg=None, ws_bytes=1 << 30, **ptr):
     c = None if cfg == "none" else C.byref(kind(*(cfg or usual)))
     at = {**{n: AT for n in names}, "ws": AT, **ptr}
     ws = [P(at["ws"]), ws_bytes] if has_ws else []
-    if name == "moe_rms_norm_forward" and at["sum"] == at["y"] == AT:
-        at["sum"] = 2 * AT
+    for n, k in {"moe_rms_norm_forward": {"sum": 2}, "moe_gate_backward": {"dx": 2, "dwg": 3}}.get(name, {}).items():
+        at[n] = k * AT if n not in ptr else at[n]  # (outputs of their own)
     return getattr(B.library(), name)(c, *[P(at[n]) for n in names], *ws, P(0))
 
 
@@ -70,6 +70,12 @@ def test_missing_and_misaligned_tensors_are_refused(name):
 
 
 def test_other_refusals():
+    assert call("moe_rms_norm_forward", (1 << 22, 8200, 1e-6)) == B.MOE_ERR_INVALID_ARG
+    assert b"2^22" in B.library().moe_last_error()
+    assert call("moe_rms_norm_forward", sum=AT, y=AT) == B.MOE_ERR_INVALID_ARG
+    for same in (dict(dx=AT, x=AT), dict(dx=AT, wg=AT, x=4 * AT), dict(dwg=AT, wg=AT), dict(dwg=AT, x=AT, wg=4 * AT)):
+        assert call("moe_gate_backward", **same) == B.MOE_ERR_INVALID_ARG
+        assert next(iter(same)).encode() + b" is" in B.library().moe_last_error()
     assert call("moe_rms_norm_forward", y=0, q=0, scale=0) == B.MOE_ERR_INVALID_ARG
     assert call("moe_rms_norm_forward", q=0) == B.MOE_ERR_INVALID_ARG
     assert call("moe_rms_norm_forward", scale=0) == B.MOE_ERR_INVALID_ARG
@@ -114,7 +120,7 @@ def test_adamw_refuses_bad_configs(cfg):
     assert B.moe_last_error()
 
 
-@pytest.mark.parametrize("bad", [dict(n=-1), dict(n=(1 << 40) + 1), dict(param=0, master=0), dict(grad=0), dict(m=0), dict(v=0),
+@pytest.mark.parametrize("bad", [dict(n=-1), dict(n=(1 << 40) + 1), dict(n=(1 << 36) - 4095), dict(param=0, master=0), dict(grad=0), dict(m=0), dict(v=0),
                                  dict(param=AT + 8), dict(master=AT + 8), dict(grad=AT + 8), dict(m=AT + 4), dict(v=AT + 8),
                                  dict(m_scale=AT), dict(v_scale=AT), dict(weight_decay=-0.1), dict(weight_decay=float("nan")),
                                  dict(grad_fp32=2)])
