@@ -160,8 +160,8 @@ __global__ __launch_bounds__(S::THREADS) void gate_logits_kernel(GateArgs a) {
 
 using Stream = tile::Shape<4, 2, 1, 2>;  // 128 x 128, 8 waves
 
-// Large batches: x comes from memory once, the gate from the L2, three stages of 32 KB
-// under way in each CU.  A row tile starts at a stage of its own: rows are a power of
+// x comes from memory once, the gate from the L2, three stages of 32 KB under way in
+// each CU; parts of the depth where there are fewer tiles than CUs.  A row tile starts at a stage of its own: rows are a power of
 // two apart, and tiles that start together would read from the same memory channels
 // all along (32768 x 4096 x 128: 71 us so, 58 with turns, 5.0 TB/s; two stages of
 // Small tiles in two workgroups a CU, the depth in two parts, 81 + 12).
@@ -169,15 +169,17 @@ __global__ __launch_bounds__(Stream::THREADS) void gate_logits_stream_kernel(Gat
   using Tl = tile::Tile<Stream, false, false, true>;
   __shared__ __attribute__((aligned(1024))) char lds[Tl::RING_LDS<4>];
   const Rows r(a);
+  const int nt = ceil_div(a.Ep, Tl::BN), stages = a.H / 64;
   int m, n;
-  if (!tile::pick(blockIdx.x, ceil_div(r.e - r.b, Tl::BM), ceil_div(a.Ep, Tl::BN), &m, &n)) return;
-  const int n0 = n * Tl::BN, row = r.b + m * Tl::BM, rows = min(r.e - row, Tl::BM);
-  const tile::Operand A{bytes(a.x + (size_t)row * a.H), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
-  const tile::Operand B{bytes(a.gate), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
+  if (!tile::pick(blockIdx.x, ceil_div(r.e - r.b, Tl::BM), nt * a.split, &m, &n)) return;
+  const int part = n / nt, n0 = n % nt * Tl::BN, row = r.b + m * Tl::BM, rows = min(r.e - row, Tl::BM);
+  const int s0 = stages * part / a.split, s1 = stages * (part + 1) / a.split;
+  const tile::Operand A{bytes(a.x + (size_t)row * a.H + s0 * 64), nullptr, (uint32_t)a.H * 2, rows, 0, 0};
+  const tile::Operand B{bytes(a.gate + (size_t)s0 * 64 * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
   typename Tl::Acc acc;
   Tl::zero(acc);
-  Tl::ring<4>(acc, lds, A, B, a.H, 1, m % (a.H / 64));
-  Tl::template epilogue<false>(acc, lds, rows, [&](int i, int c, const auto& v) { put(a, 0, row + i, n0 + c, v); });
+  Tl::ring<4>(acc, lds, A, B, (s1 - s0) * 64, 1, m % (s1 - s0));
+  Tl::template epilogue<false>(acc, lds, rows, [&](int i, int c, const auto& v) { put(a, part, row + i, n0 + c, v); });
 }
 
 template <int NW>
@@ -951,7 +953,7 @@ struct GatePlan {
   int Ep;           // columns of the gate
   bool copied;      // the gate is copied to have them
   bool stream;      // logits by a ring of stages; dx by strips
-  tile::Plan prod;  // logits, or dx, where they are not
+  tile::Plan prod;  // the tiles of logits, or of dx, where they are not; parts of logits' depth
   int dx_split;     // parts of the rows that strips are dealt to
   bool dwg_wide;              // dwg on 256 x 256 tiles
   int dwg_split, bias_parts;  // dwg's and dbias's parts of the rows
@@ -960,14 +962,37 @@ GatePlan logits_plan(const moe_router_config* c) {
   GatePlan p{};
   p.Ep = ceil_div(c->n_experts, 8) * 8;
   p.copied = p.Ep != c->n_experts;
-  p.prod = tile::plan_of(c->rows, 1, p.Ep, 1, c->hidden / 64, true);
-  // The ring of stages has one workgroup a CU, each 33 us or more at H = 4096 (64
-  // stages).  Ring against plan, us: E = 128, 12288 rows 42 : 38, 20000 46 : 60, 32768
-  // 57 : 85, 65536 117 : 134; E = 8, 32768 rows 60 : 70; E = 256, 16384 rows (256
-  // tiles) 49 : 64, 20000 (314) 79 : 69; E = 512, 32768 rows (1024) 183 : 124.
+  // x, which is long, is what the time is spent on, so this has a rule of its own: the
+  // ring, or tiles of few rows, in the number of parts whose estimate is lowest.  us,
+  // fitted to 130 sizes (64 to 32768 rows, H = 1024 to 8192): a ring's stage 0.5; a CU's
+  // pass over a tile of few rows 0.0016 to 0.0024 for each step of the depth; x from
+  // memory as far as it passes 50 MB, overlapped better by the ring; parts a launch and
+  // their sums.  Ring : few rows, us, H = 4096: E = 128, 4096 rows 37, 20 in four parts :
+  // 14; 8192 37, 26 in four : 24; 16384 48, 42 in two : 65; 32768 58 : 122; E = 8, 32768
+  // rows 51 : 69; E = 256, 8192 rows 39, 34 in two : 42; H = 8192, E = 64, 2048 rows 67, 19
+  // in eight : 22, 14 in four.  The rule that the products over row groups have took 12
+  // and 33 for 2048 rows of that (E = 64, 512), 32 for E = 128, 8192 rows, 50 for 16384.
+  const int stages = c->hidden / 64, few = ceil_div(c->rows, 32) * ceil_div(p.Ep, 64);
   const int tiles = ceil_div(c->rows, Stream::BM) * ceil_div(p.Ep, Stream::BN);
-  p.stream = tiles >= 144 && (p.Ep <= Stream::BN || tiles <= 256);
-  if (p.stream) p.prod.split = 1;
+  const double far = std::max(0.0, 2.0 * c->rows * c->hidden - 50e6);
+  // More tiles of the ring than CUs: of one column it is the best all the same; of more,
+  // the other tiles (E = 512, 32768 rows 183 : 124; E = 256, 20000 rows 79 : 69)
+  if (tiles > 256 && p.Ep > Stream::BN) {
+    p.prod = tile::plan_of(c->rows, 1, p.Ep, 1, stages, false);
+    return p;
+  }
+  double best = 1e30;
+  const auto take = [&](bool stream, tile::Plan plan, double us) {
+    if (plan.split > 1) us += 4 + 0.25 * plan.split + 4.0 * plan.split * c->rows * p.Ep / 2.2e6;
+    if (us < best) best = us, p.stream = stream, p.prod = plan;
+  };
+  for (int s = 1; s <= tile::MAX_SPLIT && (s == 1 || 4 * s <= stages); s *= 2) {
+    if (s == 1 || tiles * s <= 256)
+      take(true, {tile::Plan::SMALL, s}, 4.5 + ceil_div(tiles * s, 256) * 0.5 * stages / s + far / 9e6);
+    if (s == 1 || few * s <= 256)
+      take(false, {few * s <= 256 ? tile::Plan::FEW8 : tile::Plan::FEW4, s},
+           4 + ceil_div(few * s, 256) * (double)c->hidden / s * (1.6e-3 + 0.8e-3 * std::min(p.Ep, 64) / 64) + far / 5e6);
+  }
   return p;
 }
 GatePlan grad_plan(const moe_router_config* c, bool with_dwg = true) {

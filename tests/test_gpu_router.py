@@ -190,6 +190,30 @@ def test_gate_of_a_long_batch(B):
     check("dx", f64(dx[-300:]), rdx, bdx)
 
 
+# (each kind of tile and number of parts that a product is computed by: logits by 1 to 16 parts of few rows or of a ring, by
+# small and wide tiles; dx by strips of 1 to 4 times 64 columns and by both kinds of tiles; dwg by both, whole and in parts)
+@pytest.mark.parametrize("T,H,E", [
+    (33, 64, 8), (33, 4096, 8), (33, 4096, 60), (33, 16384, 60), (133, 64, 190), (513, 64, 200), (517, 4096, 200), (513, 8192, 512),
+    (517, 16384, 200), (2049, 64, 200), (2051, 4096, 200), (4099, 4096, 200), (12301, 64, 200), (16403, 64, 200), (16403, 4096, 200),
+    (16403, 8192, 130), (24001, 64, 300), (32801, 1088, 300), (40001, 128, 60), (8209, 192, 128)])
+def test_gate_by_every_kind_of_tile(B, T, H, E):
+    """Whole numbers whose sums are exact: no part is lost or added twice."""
+    g = Gate(B, 8, 64, 1)
+    g.T, g.H, g.E, g.S, g.cfg = T, H, E, 2, B.moe_router_config(T, H, E, 1, 2)
+    r = torch.Generator(device="cuda").manual_seed(T)
+    x, wg, d = (torch.randint(-4, 5, n, generator=r, device="cuda") for n in ((T, H), (H, E), (T, E)))
+    g.d, g.doff = [x.to(torch.bfloat16), wg.to(torch.bfloat16), None, d.float()], dev_off([5, T // 2, T - 3])
+    inside = slice(5, T - 3)
+    l = g.logits(bias=False)
+    assert torch.equal(l[inside].double(), x[inside].double() @ wg.double())
+    assert (l[:5].view(torch.int16) == MARK).all() and (l[T - 3:].view(torch.int16) == MARK).all()
+    dx, dwg, db = g.backward()
+    assert torch.equal(dx[inside], (d[inside].double() @ wg.T.double().contiguous()).float().to(torch.bfloat16))
+    assert (dx[:5].view(torch.int16) == MARK).all() and (dx[T - 3:].view(torch.int16) == MARK).all()
+    assert torch.equal(dwg, (x[inside].T.double().contiguous() @ d[inside].double()).float().to(torch.bfloat16))
+    assert torch.equal(db.double(), d[inside].double().sum(0))
+
+
 # ---- losses ---------------------------------------------------------------------------------------------------------
 class Loss:
     def __init__(self, B, T, E, k, off=None, S=1, seed=0, scale=1.0):

@@ -209,9 +209,8 @@ def test_a_captured_step_is_the_eager_one(B, bits):
         b.close()
 
 
-def test_steps_lower_the_balance_loss_of_a_skewed_gate(B):
-    """With the balance loss alone as the objective, its gradient through the gate evens out the softmax of an expert that
-    is chosen too often: its probability's sum falls."""
+def test_the_balance_gradient_pushes_down_an_expert_that_is_chosen_too_often(B):
+    """dlogits of the balance loss alone: above 0 in sum for that expert's column, and 0 over all."""
     s = Step(B, 32, T=256, H=128, F=64, E=8, k=2, off=(0, 256))
     try:
         s.bias[3] = 2.0
