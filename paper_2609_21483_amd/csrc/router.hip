@@ -955,6 +955,7 @@ struct GatePlan {
   bool stream;      // logits by a ring of stages; dx by strips
   tile::Plan prod;  // the tiles of logits, or of dx, where they are not; parts of logits' depth
   int dx_split;     // parts of the rows that strips are dealt to
+  bool together;              // dx and dwg in one launch
   bool dwg_wide;              // dwg on 256 x 256 tiles
   int dwg_split, bias_parts;  // dwg's and dbias's parts of the rows
 };
@@ -1001,11 +1002,11 @@ GatePlan grad_plan(const moe_router_config* c, bool with_dwg = true) {
   p.copied = p.Ep != c->n_experts;
   p.prod = tile::plan_of(c->rows, 1, c->hidden, 1, p.Ep / 64, false);
   p.prod.split = 1;
-  // Strips always where the gate's columns take at most 64 registers of a wave; where
-  // they take 96 or 128, in large or small batches (tiles are a launch of their own).
-  // Strips against tiles, dx alone, us: H = 4096, 32768 rows, E = 128 60 : 88, E = 256
-  // 87 : 122; all gradients, E = 256, 8192 rows 79 : 70, 2048 41 : 32, 512 27 : 36.
-  p.stream = p.Ep <= 128 || (p.Ep <= 256 && (c->rows <= 512 || (long long)c->rows * c->hidden >= 1 << 26));
+  // Strips as far as the gate's columns fit a wave's registers (E = 256: 128 of them).
+  // Strips against tiles, us: H = 4096, 32768 rows, dx alone, E = 128 60 : 88, E = 256 87 :
+  // 122; all gradients, E = 256, 8192 rows 68 : 75, 2048 28 : 34, 512 21 : 29, H = 1024,
+  // 2048 rows 20 : 29; E = 128, 2048 21 : 28.
+  p.stream = p.Ep <= 256;
   const int stages = std::max(1, ceil_div(c->rows, 64));
   // Wide tiles where each of 256 workgroups has 20 stages or more.  Wide against 128 x
   // 128, us with the launches around them: H = 4096, 32768 rows, E = 512 (64 stages)
@@ -1018,11 +1019,15 @@ GatePlan grad_plan(const moe_router_config* c, bool with_dwg = true) {
   // rows 135 : 144 : 171, 4531 29 : 37 : 35; H = 2048, E = 60, 4531 rows 20 : 24 : 22.  dx
   // alone takes them all, for its bits do not depend on its parts; dwg's do, and are
   // the same whatever else is asked for (alone 102 where 256 parts take 75).
-  const bool together = p.stream && !p.dwg_wide;
+  // Of more than 128 experts large batches are bound by operations as much as by memory,
+  // and dx and dwg follow each other, on all CUs each.  Together against that, us: E = 256,
+  // 16384 x 4096 120 : 113, 8192 x 4096 68 : 74, 8192 x 7168 116 : 106, 4096 x 7168 64 :
+  // 67; E = 192 119 : 104, 66 : 66, 115 : 100, 63 : 62; E = 128, 16384 x 4096 73 : 84.
+  p.together = p.stream && !p.dwg_wide && (p.Ep <= 128 || (long long)c->rows * c->hidden < 3 << 24);
   const int bm = p.dwg_wide ? tile::Wide::BM : DwTile::BM;
   const auto parts = [&](int most, int tiles) { return std::max(1, std::min(stages, most / tiles)); };
-  p.dwg_split = parts(together ? 128 : 256, ceil_div(c->hidden, bm) * ceil_div(c->n_experts, bm));
-  p.dx_split = parts(together && with_dwg ? 128 : 256, ceil_div(c->hidden, 256));
+  p.dwg_split = parts(p.together ? 128 : 256, ceil_div(c->hidden, bm) * ceil_div(c->n_experts, bm));
+  p.dx_split = parts(p.together && with_dwg ? 128 : 256, ceil_div(c->hidden, 256));
   p.bias_parts = std::max(1, std::min(512, ceil_div(c->rows, 16)));
   return p;
 }
@@ -1135,14 +1140,21 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   a.dx_blocks = dx && p.stream ? eights(ceil_div(a.H, 256) * a.dx_split) : 0;
   if (dwg && p.dwg_wide)
     gate_dwg_wide_kernel<<<eights(ceil_div(a.H, tile::Wide::BM) * ceil_div(a.E, tile::Wide::BN) * a.split), 512, 0, s>>>(a);
-  else if (dwg)
-    a.dwg_blocks = eights(ceil_div(a.H, DwTile::BM) * ceil_div(a.E, DwTile::BN) * a.split);
-  const int grid = a.dx_blocks + a.dwg_blocks;
-  if (grid && a.dx_blocks == 0) gate_grad_kernel<0><<<grid, 512, 0, s>>>(a);
-  else if (grid && a.Ep == 64) gate_grad_kernel<1><<<grid, 512, 0, s>>>(a);
-  else if (grid && a.Ep == 128) gate_grad_kernel<2><<<grid, 512, 0, s>>>(a);
-  else if (grid && a.Ep == 192) gate_grad_kernel<3><<<grid, 512, 0, s>>>(a);
-  else if (grid) gate_grad_kernel<4><<<grid, 512, 0, s>>>(a);
+  const int dwg_blocks = dwg && !p.dwg_wide ? eights(ceil_div(a.H, DwTile::BM) * ceil_div(a.E, DwTile::BN) * a.split) : 0;
+  a.dwg_blocks = p.together ? dwg_blocks : 0;
+  if (a.dx_blocks) {
+    const int grid = a.dx_blocks + a.dwg_blocks;
+    switch (a.Ep) {
+      case 64: gate_grad_kernel<1><<<grid, 512, 0, s>>>(a); break;
+      case 128: gate_grad_kernel<2><<<grid, 512, 0, s>>>(a); break;
+      case 192: gate_grad_kernel<3><<<grid, 512, 0, s>>>(a); break;
+      case 256: gate_grad_kernel<4><<<grid, 512, 0, s>>>(a); break;
+    }
+  }
+  if (dwg_blocks && (!a.dx_blocks || !p.together)) {
+    a.dx_blocks = 0, a.dwg_blocks = dwg_blocks;
+    gate_grad_kernel<0><<<dwg_blocks, 512, 0, s>>>(a);
+  }
   const int sums = dwg ? ceil_div(a.H * (a.Ep / 4), 256) : 0;
   if (dwg || dbias) gate_sum_kernel<<<sums + (dbias ? ceil_div(a.E, 16) : 0), 256, 0, s>>>(a, sums);
   HIP_TRY(hipGetLastError());
