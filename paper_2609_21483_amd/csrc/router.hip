@@ -335,27 +335,32 @@ __device__ __forceinline__ void put_dwg(const GateArgs& a, const typename Tl::Ac
   });
 }
 
-// dwg: tiles of 128 columns of x by 128 experts, the rows their depth, in stages of
+// dwg: tiles of 128 columns of x by 128 or 256 experts, the rows their depth, in stages of
 // 64 that are dealt to the parts in turn.  Tiles of one part follow each other: they
 // read the same rows of dlogits and run on one XCD.  32768 x 4096 x 128 in 256
 // workgroups: 57 us alone, 5 TB/s; behind dx, whose writes are still on their way to
 // memory, 78, with parts of consecutive rows 84, and on two stages of Small tiles 85.
-using DwTile = tile::Tile<Stream, false, true, true>;
+template <bool BROAD>
+using DwTile = tile::Tile<std::conditional_t<BROAD, tile::Shape<2, 4, 2, 2>, Stream>, false, true, true>;
+template <bool BROAD>
+constexpr int DW_RING = BROAD ? 3 : 4;  // stages of 48 or 32 KB
+template <bool BROAD>
 __device__ __forceinline__ void dwg_tile(const GateArgs& a, int block, char* lds) {
+  using Tl = DwTile<BROAD>;
   const Rows r(a);
-  const int mt = ceil_div(a.H, DwTile::BM), nt = ceil_div(a.E, DwTile::BN), per = mt * nt, run = ceil_div(per * a.split, NXCD);
+  const int mt = ceil_div(a.H, Tl::BM), nt = ceil_div(a.E, Tl::BN), per = mt * nt, run = ceil_div(per * a.split, NXCD);
   const int w = block % NXCD * run + block / NXCD;
   if (block / NXCD >= run || w >= per * a.split) return;
-  const int part = w / per, m0 = w % per % mt * DwTile::BM, n0 = w % per / mt * DwTile::BN;
+  const int part = w / per, m0 = w % per % mt * Tl::BM, n0 = w % per / mt * Tl::BN;
   const int stages = ceil_div(r.e - r.b, 64), mine = stages > part ? (stages - part - 1) / a.split + 1 : 0;
   const int depth = mine * 64 - (mine && (stages - 1) % a.split == part ? stages * 64 - (r.e - r.b) : 0);
   const size_t row = r.b + part * 64;
   const tile::Operand A{bytes(a.x + row * a.H), nullptr, (uint32_t)a.H * 2, 0, m0, a.H};
   const tile::Operand B{bytes(a.d + row * a.Ep), nullptr, (uint32_t)a.Ep * 2, 0, n0, a.Ep};
-  typename DwTile::Acc acc;
-  DwTile::zero(acc);
-  DwTile::ring<4>(acc, lds, A, B, depth, a.split, 0);
-  put_dwg<DwTile>(a, acc, lds, part, m0, n0);
+  typename Tl::Acc acc;
+  Tl::zero(acc);
+  Tl::template ring<DW_RING<BROAD>>(acc, lds, A, B, depth, a.split, 0);
+  put_dwg<Tl>(a, acc, lds, part, m0, n0);
 }
 
 // The same on 256 x 256 tiles, whose operands come through the L2 half as often;
@@ -381,16 +386,16 @@ __global__ __launch_bounds__(512) void gate_dwg_wide_kernel(GateArgs a) {
 // dx, which is written, and dwg, for which x is read, in one launch, in turn by eight
 // workgroups (one for each XCD): either may have none.  32768 rows, H = 4096, E = 128:
 // 117 to 125 us for 0.55 GB, about a copy's rate; one after the other 57 + 78.
-template <int KC>
+template <int KC, bool BROAD>
 __global__ __launch_bounds__(512, 2) void gate_grad_kernel(GateArgs a) {
-  constexpr int LDS = std::max(DwTile::RING_LDS<4>, KC ? 3 * KC * 8192 + 8 * 4096 : 0);
+  constexpr int LDS = std::max(DwTile<BROAD>::template RING_LDS<DW_RING<BROAD>>, KC ? 3 * KC * 8192 + 8 * 4096 : 0);
   __shared__ __attribute__((aligned(1024))) char lds[LDS];
   const int eights = std::min(a.dx_blocks, a.dwg_blocks) / NXCD, turn = blockIdx.x / NXCD, x = blockIdx.x % NXCD;
   const bool mixed = turn < 2 * eights;
   const bool dx = mixed ? turn % 2 == 0 : a.dx_blocks > a.dwg_blocks;
   const int block = (mixed ? turn / 2 : turn - eights) * NXCD + x;
   if (KC && dx) dx_strips<KC ? KC : 1>(a, block, lds);
-  else if (!dx) dwg_tile(a, block, lds);
+  else if (!dx) dwg_tile<BROAD>(a, block, lds);
 }
 
 // dwg from its parts, 4 columns a thread, and behind it dbias: 16 columns a
@@ -955,8 +960,7 @@ struct GatePlan {
   bool stream;      // logits by a ring of stages; dx by strips
   tile::Plan prod;  // the tiles of logits, or of dx, where they are not; parts of logits' depth
   int dx_split;     // parts of the rows that strips are dealt to
-  bool together;              // dx and dwg in one launch
-  bool dwg_wide;              // dwg on 256 x 256 tiles
+  bool dwg_wide, dwg_broad;   // dwg on 256 x 256 tiles, on 128 x 256
   int dwg_split, bias_parts;  // dwg's and dbias's parts of the rows
 };
 GatePlan logits_plan(const moe_router_config* c) {
@@ -1012,22 +1016,23 @@ GatePlan grad_plan(const moe_router_config* c, bool with_dwg = true) {
   // 128, us with the launches around them: H = 4096, 32768 rows, E = 512 (64 stages)
   // 152 : 201, E = 300 (64) 132 : 193, E = 256 (32) 103 : 109; 8192 rows, E = 300 (16)
   // 51 : 55, E = 512 (16) 62 : 60, E = 256 (8) 48 : 38.
-  p.dwg_wide = p.Ep > DwTile::BN &&
+  p.dwg_wide = p.Ep > 128 &&
                stages * ceil_div(c->hidden, tile::Wide::BM) * ceil_div(c->n_experts, tile::Wide::BN) >= 20 * 256;
   // One workgroup a CU: half of the CUs each where both are in one launch.  128 + 128
   // workgroups against 256 + 256 and 64 + 128 of dx and dwg, us: H = 4096, E = 128, 32768
   // rows 135 : 144 : 171, 4531 29 : 37 : 35; H = 2048, E = 60, 4531 rows 20 : 24 : 22.  dx
   // alone takes them all, for its bits do not depend on its parts; dwg's do, and are
   // the same whatever else is asked for (alone 102 where 256 parts take 75).
-  // Of more than 128 experts large batches are bound by operations as much as by memory,
-  // and dx and dwg follow each other, on all CUs each.  Together against that, us: E = 256,
-  // 16384 x 4096 120 : 113, 8192 x 4096 68 : 74, 8192 x 7168 116 : 106, 4096 x 7168 64 :
-  // 67; E = 192 119 : 104, 66 : 66, 115 : 100, 63 : 62; E = 128, 16384 x 4096 73 : 84.
-  p.together = p.stream && !p.dwg_wide && (p.Ep <= 128 || (long long)c->rows * c->hidden < 3 << 24);
-  const int bm = p.dwg_wide ? tile::Wide::BM : DwTile::BM;
+  const bool together = p.stream && !p.dwg_wide;
+  // Broad tiles read x once, which pays where it is long; of fewer rows their parts are
+  // more, and of more experts there are too few.  Broad against 128 x 128, us: E = 256, 8192
+  // x 4096 60 : 67, 4096 x 7168 58 : 64, 32768 x 1024 68 : 73, 16384 x 1024 41 : 42, 8192 x
+  // 2048 39 : 35; E = 192 56 : 65, 54 : 63, 61 : 70, 38 : 38, 33 : 32; E = 512, 4096 x 2048 46 : 42.
+  p.dwg_broad = !p.dwg_wide && p.Ep > 128 && p.Ep <= 256 && (long long)c->rows * c->hidden >= 24 << 20;
+  const int bm = p.dwg_wide ? 256 : 128, bn = p.dwg_wide || p.dwg_broad ? 256 : 128;
   const auto parts = [&](int most, int tiles) { return std::max(1, std::min(stages, most / tiles)); };
-  p.dwg_split = parts(p.together ? 128 : 256, ceil_div(c->hidden, bm) * ceil_div(c->n_experts, bm));
-  p.dx_split = parts(p.together && with_dwg ? 128 : 256, ceil_div(c->hidden, 256));
+  p.dwg_split = parts(together ? 128 : 256, ceil_div(c->hidden, bm) * ceil_div(c->n_experts, bn));
+  p.dx_split = parts(together && with_dwg ? 128 : 256, ceil_div(c->hidden, 256));
   p.bias_parts = std::max(1, std::min(512, ceil_div(c->rows, 16)));
   return p;
 }
@@ -1140,20 +1145,17 @@ moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits,
   a.dx_blocks = dx && p.stream ? eights(ceil_div(a.H, 256) * a.dx_split) : 0;
   if (dwg && p.dwg_wide)
     gate_dwg_wide_kernel<<<eights(ceil_div(a.H, tile::Wide::BM) * ceil_div(a.E, tile::Wide::BN) * a.split), 512, 0, s>>>(a);
-  const int dwg_blocks = dwg && !p.dwg_wide ? eights(ceil_div(a.H, DwTile::BM) * ceil_div(a.E, DwTile::BN) * a.split) : 0;
-  a.dwg_blocks = p.together ? dwg_blocks : 0;
-  if (a.dx_blocks) {
-    const int grid = a.dx_blocks + a.dwg_blocks;
-    switch (a.Ep) {
-      case 64: gate_grad_kernel<1><<<grid, 512, 0, s>>>(a); break;
-      case 128: gate_grad_kernel<2><<<grid, 512, 0, s>>>(a); break;
-      case 192: gate_grad_kernel<3><<<grid, 512, 0, s>>>(a); break;
-      case 256: gate_grad_kernel<4><<<grid, 512, 0, s>>>(a); break;
-    }
-  }
-  if (dwg_blocks && (!a.dx_blocks || !p.together)) {
-    a.dx_blocks = 0, a.dwg_blocks = dwg_blocks;
-    gate_grad_kernel<0><<<dwg_blocks, 512, 0, s>>>(a);
+  else if (dwg)
+    a.dwg_blocks = eights(ceil_div(a.H, 128) * ceil_div(a.E, p.dwg_broad ? 256 : 128) * a.split);
+  const auto go = [&](auto kernel, decltype(kernel) broad = nullptr) {
+    (p.dwg_broad ? broad : kernel)<<<a.dx_blocks + a.dwg_blocks, 512, 0, s>>>(a);
+  };
+  if (a.dx_blocks + a.dwg_blocks) switch (a.dx_blocks ? a.Ep : 0) {
+    case 0: go(gate_grad_kernel<0, false>, gate_grad_kernel<0, true>); break;
+    case 64: go(gate_grad_kernel<1, false>); break;
+    case 128: go(gate_grad_kernel<2, false>); break;
+    case 192: go(gate_grad_kernel<3, false>, gate_grad_kernel<3, true>); break;
+    case 256: go(gate_grad_kernel<4, false>, gate_grad_kernel<4, true>); break;
   }
   const int sums = dwg ? ceil_div(a.H * (a.Ep / 4), 256) : 0;
   if (dwg || dbias) gate_sum_kernel<<<sums + (dbias ? ceil_div(a.E, 16) : 0), 256, 0, s>>>(a, sums);

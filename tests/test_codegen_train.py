@@ -30,8 +30,8 @@ def test_no_scratch_and_no_packed_fp32(tmp_path, source, kernels):
     assert "v_pk_fma_f32" not in asm and "v_pk_mul_f32" not in asm and "v_pk_add_f32" not in asm
     if source != "router.hip":
         return
-    for kc in (1, 2, 3, 4):
-        start = re.search(r"\n(_ZN\w*gate_grad_kernelILi%d\w*):" % kc, asm)
+    for kc, broad in ((1, 0), (2, 0), (3, 0), (3, 1), (4, 0), (4, 1)):
+        start = re.search(r"\n(_ZN\w*gate_grad_kernelILi%dELb%d\w*):" % (kc, broad), asm)
         body = asm[start.end():asm.index(".Lfunc_end", start.end())]
         # the strips' loop: from its wait for a strip behind which there are one more strip's loads and 8 stores, to its end
         loop = body[body.index(f"vmcnt({kc + 8})"):body.rindex("s_endpgm")]

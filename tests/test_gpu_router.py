@@ -191,11 +191,11 @@ def test_gate_of_a_long_batch(B):
 
 
 # (each kind of tile and number of parts that a product is computed by: logits by 1 to 16 parts of few rows or of a ring, by
-# small and wide tiles; dx by strips of 1 to 4 times 64 columns, with dwg in one launch or before it, and by both kinds of
-# tiles; dwg by both, whole and in parts)
+# small and wide tiles; dx by strips of 1 to 4 times 64 columns, with dwg in one launch or behind it, and by both kinds of
+# tiles; dwg by three, whole and in parts)
 @pytest.mark.parametrize("T,H,E", [
-    (33, 64, 8), (33, 64, 300), (1025, 64, 511), (33, 4096, 8), (33, 4096, 60), (33, 16384, 60), (133, 64, 190), (513, 64, 200), (517, 4096, 200), (513, 8192, 512),
-    (517, 16384, 200), (2049, 64, 200), (2051, 4096, 200), (4099, 4096, 200), (12301, 64, 200), (16403, 64, 200), (16403, 4096, 200),
+    (33, 64, 8), (33, 64, 300), (1025, 64, 511), (33, 4096, 8), (33, 4096, 60), (33, 16384, 60), (133, 64, 190), (513, 64, 200),
+    (517, 4096, 200), (513, 8192, 512), (6203, 4096, 190), (517, 16384, 200), (2049, 64, 200), (2051, 4096, 200), (4099, 4096, 200), (12301, 64, 200), (16403, 64, 200), (16403, 4096, 200),
     (16403, 8192, 130), (24001, 64, 300), (32801, 1088, 300), (40001, 128, 60), (8209, 192, 128)])
 def test_gate_by_every_kind_of_tile(B, T, H, E):
     """Whole numbers whose sums are exact: no part is lost or added twice."""
@@ -213,6 +213,7 @@ def test_gate_by_every_kind_of_tile(B, T, H, E):
     assert (dx[:5].view(torch.int16) == MARK).all() and (dx[T - 3:].view(torch.int16) == MARK).all()
     assert torch.equal(dwg, (x[inside].T.double().contiguous() @ d[inside].double()).float().to(torch.bfloat16))
     assert torch.equal(db.double(), d[inside].double().sum(0))
+    assert torch.equal(g.backward(("dx",))[0], dx) and torch.equal(g.backward(("dwg",))[1], dwg)
 
 
 # ---- losses ---------------------------------------------------------------------------------------------------------
