@@ -662,7 +662,8 @@ typedef struct {
  * or NULL (param alone is stepped then); at least one of them.  grad: bf16, or fp32
  * where grad_fp32 = 1.  m, v: fp32, or 8 bits each: m in e4m3, v in e5m2 (OCP), times
  * a scale for every MOE_ADAMW_BLOCK consecutive values, m_scale and v_scale: fp32
- * [ceil(n / 256)] (NULL with 32 bits).  All zeros is the state before the first step. */
+ * [ceil(n / 256)], on their values' alignment (NULL with 32 bits).  All zeros is the
+ * state before the first step. */
 typedef struct {
   int64_t n; /* 0..2^36 - 4096 */
   uint16_t* param;

@@ -16,7 +16,7 @@ constexpr int CHUNK = 256 * VALUES;  // of a workgroup
 constexpr int64_t MOST_CHUNKS = (1 << 24) - 1;
 // Tensors of a launch: their addresses are kernel arguments (4 KB at most), so
 // that no table has to reach the device before the step.  A tensor and its end take 48
-// bytes (8 bits: 60), addresses as multiples of 16: 150 small tensors in two launches, 20
+// bytes (8 bits: 60), addresses as multiples of 16 (scales': of 4): 150 small tensors in two launches, 20
 // us, against 29 in the four that 72 bytes a tensor make.
 template <bool BITS8>
 struct Packed {
@@ -28,7 +28,8 @@ struct Packed {
   uint32_t place_and_type;  // place in the caller's list * 2 + (grad is fp32)
 
   __host__ __device__ __forceinline__ uint32_t half(int i) const { return i % 2 ? high[i / 2] >> 16 : high[i / 2] & 0xffffu; }
-  __device__ __forceinline__ char* at(int i) const { return reinterpret_cast<char*>(((uint64_t)half(i) << 32 | low[i]) << 4); }
+  static __host__ __device__ __forceinline__ constexpr int unit(int i) { return i < 5 ? 4 : 2; }  // bits that are 0 in address i
+  __device__ __forceinline__ char* at(int i) const { return reinterpret_cast<char*>(((uint64_t)half(i) << 32 | low[i]) << unit(i)); }
   __device__ __forceinline__ int64_t n() const { return (int64_t)((uint64_t)half(N) << 32 | n_low); }
   __device__ __forceinline__ bool grad_fp32() const { return place_and_type & 1; }
   __device__ __forceinline__ uint32_t place() const { return place_and_type >> 1; }
@@ -362,10 +363,12 @@ moe_status check(const moe_adamw_config* c, const moe_adamw_tensor* tensors, int
     if ((!t.param && !t.master) || !t.grad || !t.m || !t.v) return fail(MOE_ERR_INVALID_ARG, "tensor %d: NULL argument", i);
     if ((!t.m_scale || !t.v_scale) != (c->state_bits == 32) || !t.m_scale != !t.v_scale)
       return fail(MOE_ERR_INVALID_ARG, "tensor %d: states in 8 bits have scales, and others none", i);
-    for (const void* p : {(const void*)t.param, (const void*)t.master, t.grad, (const void*)t.m, (const void*)t.v,
-                          (const void*)t.m_scale, (const void*)t.v_scale})
-      if (!aligned16(p) || reinterpret_cast<uint64_t>(p) >> 52)
+    for (const void* p : {(const void*)t.param, (const void*)t.master, t.grad, (const void*)t.m, (const void*)t.v})
+      if (!aligned16(p) || reinterpret_cast<uint64_t>(p) >> 50)
         return fail(MOE_ERR_INVALID_ARG, "tensor %d does not start on a 16-byte boundary", i);
+    for (const float* p : {t.m_scale, t.v_scale})
+      if (reinterpret_cast<uint64_t>(p) % 4 || reinterpret_cast<uint64_t>(p) >> 50)
+        return fail(MOE_ERR_INVALID_ARG, "tensor %d: scales are not aligned to their values", i);
   }
   return MOE_OK;
 }
@@ -395,7 +398,7 @@ bool launch(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors, int32_
     const auto put_half = [&](int k, uint32_t v) { p.high[k / 2] |= v << (k % 2 * 16); };
     const void* const at[7] = {t.grad, t.param, t.master, t.m, t.v, t.m_scale, t.v_scale};
     for (int k = 0; k < Packed<BITS8>::N; ++k) {
-      const uint64_t v = reinterpret_cast<uint64_t>(at[k]) >> 4;
+      const uint64_t v = reinterpret_cast<uint64_t>(at[k]) >> Packed<BITS8>::unit(k);
       p.low[k] = (uint32_t)v;
       put_half(k, (uint32_t)(v >> 32));
     }

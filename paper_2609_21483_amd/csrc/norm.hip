@@ -289,14 +289,15 @@ void for_width(int H, Fn&& fn) {
 }
 
 // Workgroups of the backward pass, each with a part of dweight's sum: as many as
-// load 6 MB of rows at once (dy, s and dsum), 256 at least.  More cost their parts'
+// load 6 MB of rows at once (dy, s and dsum), whole rounds of 256 CUs (32768 x 1000 in
+// 262 workgroups 69 us, in 256 51).  More cost their parts'
 // way out and back.  In 256, 512, 1024 and 2048 workgroups, us: 32768 x 4096 185, 197,
 // 221 and 220; 32768 x 2048 129, 97, 106 and 114; 65536 x 512 67, 48, 52 and 55; 262144
 // x 64 58, 39, 30 and 33.
 int grad_parts(int T, int H) {
   int per = 1;
   for_width(H, [&](auto threads, auto) { per = group_of<threads()> / threads(); });
-  return std::min(ceil_div(T, per), std::max(256, std::min(1024, (1 << 20) / (per * H))));
+  return std::min(ceil_div(T, per), std::clamp((1 << 20) / (per * H) / 256, 1, 4) * 256);
 }
 
 moe_status check_cfg(const moe_rms_norm_config* c) {

@@ -179,6 +179,36 @@ def test_any_config(B, bits, kw):
     verify(before, t, 0, c, bits, 0.1)
 
 
+@pytest.mark.parametrize("grads", ["bf16", "fp32"])
+@pytest.mark.parametrize("mode", ["both", "bf16", "fp32"])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_tensors_that_are_slices_of_one_buffer(B, bits, mode, grads):
+    """A model's tensors one behind the other, each from a block on: scales then start at any of four bytes' multiples."""
+    sizes = [300, 1, 768, 255, 257, 5000, 4096]
+    alone = [tensor(n, mode, bits, grads, seed=40) for n in sizes]
+    at = np.cumsum([0] + [-(-n // 256) for n in sizes])
+    whole, together = {}, [dict(weight_decay=t["weight_decay"]) for t in alone]
+    for k in alone[0]:
+        if k == "weight_decay":
+            continue
+        unit = 1 if k.endswith("_scale") else 256
+        whole[k] = torch.full((int(at[-1]) * unit * alone[0][k].element_size(),), MARK, dtype=torch.uint8, device="cuda").view(alone[0][k].dtype)
+        for t, u, b in zip(alone, together, at):
+            u[k] = whole[k][b * unit:b * unit + t[k].numel()]
+            u[k].copy_(t[k])
+    before = {k: w.clone() for k, w in whole.items()}
+    cfg, _ = config(B, bits)
+    for ts in (alone, together):
+        B.moe_adamw(cfg, B.moe_adamw_tensors(ts, bits))
+    torch.cuda.synchronize()
+    for k, w in whole.items():
+        unit = 1 if k.endswith("_scale") else 256
+        for t, u, b, n in zip(alone, together, at, sizes):
+            assert torch.equal(t[k].view(torch.uint8), u[k].view(torch.uint8))
+            end, e = b * unit + t[k].numel(), (b + -(-n // 256)) * unit
+            assert torch.equal(w[end:e].view(torch.uint8), before[k][end:e].view(torch.uint8))
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_first_step_from_zeros(B, bits):
     t = tensor(1000, "both", bits, "fp32", 6)

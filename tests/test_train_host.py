@@ -133,6 +133,12 @@ def test_adamw_refuses_bad_tensors(bad):
     assert st == B.MOE_ERR_INVALID_ARG and b"tensor 0" in B.library().moe_last_error()
 
 
+@pytest.mark.parametrize("bad", ["m_scale", "v_scale"])
+def test_adamw_refuses_scales_off_their_values(bad):
+    assert adamw(dict(state_bits=8), **{**dict(m_scale=AT, v_scale=AT), bad: AT + 2}) == B.MOE_ERR_INVALID_ARG
+    assert b"scales" in B.library().moe_last_error()
+
+
 def test_adamw_of_nothing():
     assert B.library().moe_adamw(C.byref(B.moe_adamw_config(*GOOD.values())), None, 0, None, None) == B.MOE_OK
     assert adamw(n=-1) == B.MOE_ERR_INVALID_ARG
