@@ -599,7 +599,7 @@ moe_status moe_gate_workspace_size(const moe_router_config* cfg, int32_t backwar
 
 /* logits[t][e] = sum_h x[t][h] wg[h][e] + logit_bias[e]: x bf16 [T][H], wg bf16
  * [H][E], logit_bias fp32 [E] or NULL, logits fp32 [T][E].  The sum is fp32, in
- * another order than moe_route's, and in large batches in one that depends on the
+ * another order than moe_route's, and in longer batches in one that depends on the
  * row's place, so the last bits may differ from the logits that moe_route compares.
  * top_k is not read. */
 moe_status moe_gate_logits(const moe_router_config* cfg, const uint16_t* x, const uint16_t* wg,
