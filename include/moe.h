@@ -625,9 +625,10 @@ moe_status moe_route_loss_workspace_size(const moe_router_config* cfg, size_t* b
  *          E / (k n^2) sum_e counts[s][e] P[s][e], n the sequence's rows and P the
  *          sums of their softmax over all experts (1 where both are even);
  *          loss[1], z: the mean of lse^2 over the rows of all sequences.
- * Without any rows both are 0.  A logit of -inf is an expert that cannot be chosen;
- * a row of nothing else has lse = -inf and adds 0 to both sums.  A row with a NaN
- * or +inf has lse = NaN, and so have the losses it enters.  hidden is not read. */
+ * Without any rows both are 0.  A logit of -inf has probability 0 (moe_route selects
+ * one only where fewer than k others are left, with weight 0; counts count it like any
+ * other); a row of nothing else has lse = -inf and adds 0 to both sums.  A row with a
+ * NaN or +inf has lse = NaN, and so have the losses it enters.  hidden is not read. */
 moe_status moe_route_loss(const moe_router_config* cfg, const float* logits, const int32_t* topk_idx,
                           const int32_t* seq_off, int32_t* counts, float* lse, float* loss, void* ws, size_t ws_bytes,
                           void* stream);
@@ -640,7 +641,8 @@ moe_status moe_route_loss(const moe_router_config* cfg, const float* logits, con
  *   dloss[0] E / (k n^2 S') p_e (c_e - sum_i c_i p_i) + dloss[1] 2 / N lse p_e
  *   + sum over j with topk_idx[j] = e of w_j (dw_j - sum_i w_i dw_i)
  * (the counts are constants; the weights are the softmax over the chosen logits).
- * counts and lse as moe_route_loss gave them.  A row of -inf alone has gradient 0.
+ * counts and lse as moe_route_loss gave them.  A row of -inf alone (lse = -inf) has
+ * gradient 0 whatever its ids and weights are (moe_route's are the k smallest and NaN).
  * dlogits may be logits (the same address). */
 moe_status moe_route_loss_backward(const moe_router_config* cfg, const float* logits, const int32_t* topk_idx,
                                    const float* topk_w, const int32_t* seq_off, const int32_t* counts,

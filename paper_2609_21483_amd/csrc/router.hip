@@ -857,11 +857,11 @@ __global__ __launch_bounds__(256) void route_loss_grad_kernel(LossArgs a) {
 #pragma unroll
     for (int i = 0; i < R::N; ++i) p[i] *= c[i] + rest;
     if (a.dtopk_w) {
-      // (choices are in the row's first 8 lanes)
+      // (choices are in the row's first 8 lanes; of a dead row routing's weights are NaN)
       float all = r.w * r.dw;
 #pragma unroll
       for (int d = 4; d; d >>= 1) all += __shfl_xor(all, d);
-      const float t = r.w * (r.dw - all);
+      const float t = dead ? 0.0f : r.w * (r.dw - all);
       for (int j = 0; j < a.K; ++j) {
         const float tj = __shfl(t, sub * R::LPR + j);
         const int ej = __shfl(r.e, sub * R::LPR + j);

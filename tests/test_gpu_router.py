@@ -340,6 +340,61 @@ def test_masked_experts_and_rows_without_any(B, E):
     g.verify()
 
 
+@pytest.mark.parametrize("E,k", [(1, 1), (8, 2), (60, 6), (128, 8), (200, 5), (300, 8), (511, 3)])
+@pytest.mark.parametrize("losses", [True, False])
+def test_rows_of_nothing_to_choose_have_no_gradient(B, E, k, losses):
+    """Rows of -inf alone, with ids and weights as routing writes them (the smallest ids, NaN) and with finite weights:
+    gradient 0 from the losses and from the weights, and the other rows as they are without them."""
+    g = Loss(B, 70, E, k, [0, 30, 69], 2, seed=12)
+    dead = [0, 7, 29, 68]
+    g.l[dead] = -np.inf
+    g.idx[dead] = np.arange(k)
+    g.update()
+    assert np.isnan(g.w[dead]).all()
+    g.w[29] = np.linspace(0.1, 0.9, k)
+    g.d["w"] = torch.from_numpy(g.w).cuda()
+    c, lse, _ = g.forward()
+    assert torch.isneginf(lse[dead]).all()
+    d = g.backward(c, lse, losses=losses)
+    assert not d[dead].any()
+    w = g.w.copy()
+    w[dead] = 0.0  # for the reference: no weights, no gradient
+    ref, bound = R.loss_grad(g.l.astype(np.float64), g.idx, w.astype(np.float64), [0, 30, 69], c.cpu().numpy(), f64(lse),
+                             g.dloss.astype(np.float64) if losses else np.zeros(2), g.dw.astype(np.float64), E, k)
+    check("dlogits", f64(d[:69]), ref[:69], bound[:69])
+
+
+@pytest.mark.parametrize("few", [True, False])
+def test_gradients_of_experts_that_routing_may_not_choose(B, few):
+    """A bias of -inf for all experts but one, or for all: routing fills its choices up with masked ones, of weight 0 (where
+    none is left: of weight NaN), and the way back through logits, losses and weights has gradient 0 there."""
+    T, H, E, k = 90, 128, 24, 3
+    g = Gate(B, T, H, E, seed=13)
+    g.d[2].fill_(float("-inf"))
+    if few:
+        g.d[2][5] = 0.5
+    idx, w = torch.empty(T, k, dtype=torch.int32, device="cuda"), torch.empty(T, k, device="cuda")
+    B.moe_route_topk_static(T, H, E, k, g.d[0], g.d[1], g.d[2], idx, w)
+    torch.cuda.synchronize()
+    want = torch.tensor([5, 0, 1] if few else [0, 1, 2], device="cuda")
+    assert (idx == want).all()
+    assert torch.equal(w, torch.tensor([1.0, 0, 0], device="cuda").expand(T, k)) if few else torch.isnan(w).all()
+    l = g.logits()
+    q = Loss(B, T, E, k)
+    q.d.update(l=l, idx=idx, w=w)
+    c, lse, loss = q.forward()
+    assert (c[0, want.long()] == T).all() and int(c.sum()) == k * T
+    # (one expert left has probability 1, exactly, and is chosen by every row; 16 roundings at most in each value)
+    assert float(loss[0]) == pytest.approx(E / k if few else 0.0, rel=16 * R.F32)
+    d = q.backward(c, lse)
+    # by the one logit that is left: z 2 lse / T, the weights none, the balance loss the rounding of c - c
+    rest = torch.zeros_like(d)
+    if few:
+        rest[:, 5] = 2 * 0.02 / T * lse
+    torch.testing.assert_close(d, rest, rtol=16 * R.F32, atol=4 * R.F32 * 0.7 * E / (k * T))
+    assert not d[:, torch.arange(E) != 5].any()
+
+
 def test_a_nan_row_is_its_sequences(B):
     g = Loss(B, 90, 60, 4, [0, 40, 90], 2, seed=7)
     c0, lse0, _ = g.forward()
