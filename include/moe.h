@@ -685,8 +685,9 @@ typedef struct {
  *   w -= lr (weight_decay w + (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
  * in fp32, from m and v before they are rounded.  now: NULL, or device memory with
  * three fp32 values, lr, grad_scale and step, in place of the config's (a captured
- * step reads them at each replay; a step below 1 counts as 1).  A grad_scale there
- * that is NaN leaves every tensor as it was: a step to be skipped.
+ * step reads them at each replay; a step below 1 counts as 1, and above 2^24 fp32
+ * holds no more every step: steps there share random bits, and adding 1 stands still).
+ * A grad_scale there that is NaN leaves every tensor as it was: a step to be skipped.
  *
  * master's rounded value goes to param; param alone, and states in 8 bits, are
  * rounded up or down at random, with the probabilities that keep their means (to

@@ -40,7 +40,8 @@ constexpr int MOST = BITS8 ? 67 : 84;
 template <bool BITS8>
 struct AdamArgs {
   const float* now;
-  float lr, scale, step, log_b1, log_b2, b1, b2, rest1, rest2, eps;  // rest: 1 - beta
+  float lr, scale, log_b1, log_b2, b1, b2, rest1, rest2, eps;  // rest: 1 - beta
+  int32_t step;
   uint32_t seed;
   int count;                  // tensors of this launch
   uint32_t end[MOST<BITS8>];  // chunks of the tensors up to and with each
@@ -141,14 +142,16 @@ __device__ __forceinline__ void step_chunk(const AdamArgs<BITS8>& a, const Packe
   constexpr int GROUP = BITS8 ? 16 : 4, GROUPS = VALUES / GROUP;
   const int lane = threadIdx.x & 63;
   const int inside = (int)min((int64_t)CHUNK, t.n() - chunk);  // values of this chunk
-  float lr = a.lr, gs = a.scale, step = a.step;
+  float lr = a.lr, gs = a.scale, step = (float)a.step;
+  uint32_t count = (uint32_t)a.step;  // of the random bits: fp32 would give neighbouring steps from 2^24 on the same
   if (a.now) {
     lr = a.now[0], gs = a.now[1], step = a.now[2];
     if (gs != gs) return;
     step = step >= 1.0f ? step : 1.0f;
+    count = (uint32_t)fminf(step, 0x1.fffffep31f);
   }
   const float c1 = 1.0f / -expm1f(step * a.log_b1), c2 = 1.0f / -expm1f(step * a.log_b2);
-  const uint32_t key = mixed(mixed(a.seed + (uint32_t)step * 0xD22CD251u) + t.place() * 0xA5375919u);
+  const uint32_t key = mixed(mixed(a.seed + count * 0xD22CD251u) + t.place() * 0xA5375919u);
   const float* grad_f = reinterpret_cast<const float*>(t.at(0)) + chunk;
   const uint16_t* grad_h = reinterpret_cast<const uint16_t*>(t.at(0)) + chunk;
   uint16_t* param = reinterpret_cast<uint16_t*>(t.at(1)) + chunk;
@@ -376,7 +379,7 @@ moe_status check(const moe_adamw_config* c, const moe_adamw_tensor* tensors, int
 template <bool BITS8>
 bool launch(const moe_adamw_config* cfg, const moe_adamw_tensor* tensors, int32_t n_tensors, const float* now, hipStream_t s) {
   AdamArgs<BITS8> a{};
-  a.now = now, a.lr = (float)cfg->lr, a.scale = (float)cfg->grad_scale, a.step = (float)cfg->step;
+  a.now = now, a.lr = (float)cfg->lr, a.scale = (float)cfg->grad_scale, a.step = cfg->step;
   a.b1 = (float)cfg->beta1, a.b2 = (float)cfg->beta2, a.eps = (float)cfg->eps, a.seed = cfg->seed;
   a.rest1 = (float)(1 - cfg->beta1), a.rest2 = (float)(1 - cfg->beta2);
   a.log_b1 = (float)std::log(cfg->beta1), a.log_b2 = (float)std::log(cfg->beta2);

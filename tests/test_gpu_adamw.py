@@ -322,6 +322,17 @@ def test_replays_of_a_captured_step(B, bits):
         assert equal(ts, eager), turn
 
 
+@pytest.mark.parametrize("step", [(1 << 24) + 1, (1 << 24) + 3, (1 << 30) + 65, (1 << 31) - 1])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_random_bits_of_steps_that_fp32_does_not_hold(B, bits, step):
+    """Every step has random bits of its own, of 32-bit states' bf16 weights and of 8-bit states."""
+    t = tensor(9000, "bf16", bits, "fp32", 21)
+    before = values(t, bits)
+    cfg, c = config(B, bits, step=step)
+    B.moe_adamw(cfg, B.moe_adamw_tensors([t], bits))
+    verify(before, t, 0, c, bits, 0.1)
+
+
 def test_another_stream_and_a_second_run(B):
     ts = [tensor(n, "bf16", 8, "bf16", 11) for n in (700, 90000)]
     a, b = clones(ts), clones(ts)
