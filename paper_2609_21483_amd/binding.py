@@ -427,10 +427,18 @@ def _ws(t: Optional[torch.Tensor], dev: int):
     return _arg("ws", t, t.dtype, t.shape, dev), t.nbytes
 
 
+def _current_stream(dev: int) -> int:
+    """The handle of the device's current stream."""
+    try:
+        return torch._C._cuda_getCurrentRawStream(dev)  # without the object that torch.cuda makes, 1 us of a call's 6
+    except AttributeError:  # (torch promises only the object)
+        return torch.cuda.current_stream(dev).cuda_stream
+
+
 def _call(name: str, dev: int, stream, *args) -> None:
     """Calls on device `dev`, on the given stream of it or on its current one."""
     if stream is None:
-        raw = torch._C._cuda_getCurrentRawStream(dev)  # current_stream(dev).cuda_stream, without its 1 us object
+        raw = _current_stream(dev)
     elif stream.device_index != dev:
         raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{dev}")
     else:

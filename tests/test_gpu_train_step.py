@@ -252,6 +252,16 @@ def test_8_bit_rows_feed_the_8_bit_product(B):
         assert int((q.int() - q2.int()).abs().max()) <= 1
 
 
+def test_current_stream_handles(B, monkeypatch):
+    s = torch.cuda.Stream()
+    dev = torch.cuda.current_device()
+    for _ in range(2):  # by torch's shortcut, and without it
+        assert B._current_stream(dev) == torch.cuda.current_stream(dev).cuda_stream
+        with torch.cuda.stream(s):
+            assert B._current_stream(dev) == s.cuda_stream
+        monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+
+
 def test_two_batches_at_once_on_two_streams(B):
     """Two batches at once on two streams, each with its own workspace, give what they give alone."""
     one, two = Step(B, 32, seed=3), Step(B, 32, seed=4)

@@ -166,6 +166,18 @@ def test_binding_refuses_cpu_tensors():
         B.moe_adamw_tensors([], 16)
 
 
+def test_calls_take_the_current_stream_without_torchs_own_shortcut(monkeypatch):
+    """A torch that lacks the shortcut to the current stream's handle is asked for the stream itself."""
+    import types
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev: types.SimpleNamespace(cuda_stream=0x1230 + dev))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    taken = []
+    monkeypatch.setattr(B, "_lib", types.SimpleNamespace(some_call=lambda *a: taken.append(a) or B.MOE_OK))
+    B._call("some_call", 3, None, 7)
+    assert taken == [(7, 0x1233)]
+
+
 # ---- the reference -----------------------------------------------------------------------------------------------------
 def difference(f, x, d, h=1e-5):
     return (f(x + h * d) - f(x - h * d)) / (2 * h)
