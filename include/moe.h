@@ -467,7 +467,11 @@ typedef enum {
   MOE_TILES_FEW4 = 0,  /* 32 rows x 64 columns, 4 waves that share the depth */
   MOE_TILES_FEW8 = 1,  /* the same, 8 waves */
   MOE_TILES_SMALL = 2, /* 128 x 128 */
-  MOE_TILES_WIDE = 3   /* 256 x 256 */
+  MOE_TILES_WIDE = 3,  /* 256 x 256 */
+  /* of the gate's products alone: */
+  MOE_TILES_RING = 4,  /* 128 x 128, a ring of four stages */
+  MOE_TILES_BROAD = 5, /* 128 x 256, a ring of three */
+  MOE_TILES_STRIPS = 6 /* 64 rows at a time x 256 columns, whose gate stays in registers */
 } moe_tiles;
 
 typedef struct {
@@ -596,6 +600,15 @@ typedef struct {
 
 /* Workspace of moe_gate_logits (backward = 0) or moe_gate_backward (1). */
 moe_status moe_gate_workspace_size(const moe_router_config* cfg, int32_t backward, size_t* bytes);
+
+/* Which tiles the gate's products are computed by (on the host; no device is
+ * touched): logits in parts of the depth H, dwg in parts of the rows, dx (with dwg
+ * wanted too) in parts that strips of rows are dealt to, whole where it takes tiles. */
+typedef struct {
+  moe_product_plan logits, dx, dwg;
+} moe_gate_plan;
+
+moe_status moe_gate_plan_host(const moe_router_config* cfg, moe_gate_plan* out);
 
 /* logits[t][e] = sum_h x[t][h] wg[h][e] + logit_bias[e]: x bf16 [T][H], wg bf16
  * [H][E], logit_bias fp32 [E] or NULL, logits fp32 [T][E].  The sum is fp32, in

@@ -106,7 +106,7 @@ class moe_adamw_tensor(C.Structure):
         ("weight_decay", C.c_float), ("grad_fp32", C.c_int32)]
 
 
-MOE_TILES = ("few4", "few8", "small", "wide")
+MOE_TILES = ("few4", "few8", "small", "wide", "ring", "broad", "strips")
 
 
 class moe_product_plan(C.Structure):
@@ -118,6 +118,10 @@ class moe_product_plan(C.Structure):
 
 class moe_ffn_plan(C.Structure):
     _fields_ = [(n, moe_product_plan) for n in ("up", "down", "dh", "dx", "dw")]
+
+
+class moe_gate_plan(C.Structure):
+    _fields_ = [(n, moe_product_plan) for n in ("logits", "dx", "dwg")]
 
 
 class MoeError(RuntimeError):
@@ -170,6 +174,7 @@ _SIGS = {
     "moe_rms_norm_workspace_size": ([C.POINTER(moe_rms_norm_config), C.POINTER(C.c_size_t)], C.c_int),
     "moe_rms_norm_backward": ([C.POINTER(moe_rms_norm_config)] + [_P] * 8 + [C.c_size_t, _P], C.c_int),
     "moe_gate_workspace_size": ([C.POINTER(moe_router_config), C.c_int32, C.POINTER(C.c_size_t)], C.c_int),
+    "moe_gate_plan_host": ([C.POINTER(moe_router_config), C.POINTER(moe_gate_plan)], C.c_int),
     "moe_gate_logits": ([C.POINTER(moe_router_config)] + [_P] * 6 + [C.c_size_t, _P], C.c_int),
     "moe_gate_backward": ([C.POINTER(moe_router_config)] + [_P] * 8 + [C.c_size_t, _P], C.c_int),
     "moe_route_loss_workspace_size": ([C.POINTER(moe_router_config), C.POINTER(C.c_size_t)], C.c_int),
@@ -558,6 +563,12 @@ def moe_rms_norm_backward(cfg: moe_rms_norm_config, dy, dsum, sum, weight, rstd,
 
 def moe_gate_workspace_size(cfg: moe_router_config, backward: bool = False) -> int:
     return _size("moe_gate_workspace_size", cfg, int(backward))
+
+
+def moe_gate_plan_host(cfg: moe_router_config) -> moe_gate_plan:
+    p = moe_gate_plan()
+    _check("moe_gate_plan_host", _lib.moe_gate_plan_host(C.byref(cfg), C.byref(p)))
+    return p
 
 
 def moe_gate_logits(cfg: moe_router_config, x, wg, logit_bias, seq_off, logits, ws, stream=None) -> None:

@@ -1082,6 +1082,17 @@ moe_status moe_gate_workspace_size(const moe_router_config* cfg, int32_t backwar
   return MOE_OK;
 }
 
+moe_status moe_gate_plan_host(const moe_router_config* cfg, moe_gate_plan* out) {
+  moe_status st = check_gate(cfg);
+  if (st != MOE_OK) return st;
+  if (!out) return fail(MOE_ERR_INVALID_ARG, "out is NULL");
+  const GatePlan l = logits_plan(cfg), g = grad_plan(cfg);
+  out->logits = {l.stream ? (int)MOE_TILES_RING : (int)l.prod.kind, l.prod.split};
+  out->dx = {g.stream ? (int)MOE_TILES_STRIPS : (int)g.prod.kind, g.stream ? g.dx_split : 1};
+  out->dwg = {g.dwg_wide ? MOE_TILES_WIDE : g.dwg_broad ? MOE_TILES_BROAD : MOE_TILES_RING, g.dwg_split};
+  return MOE_OK;
+}
+
 moe_status moe_gate_logits(const moe_router_config* cfg, const uint16_t* x, const uint16_t* wg,
                            const float* logit_bias, const int32_t* seq_off, float* logits, void* ws, size_t ws_bytes,
                            void* stream) {

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests import gate_plans as GP
 from tests import train_ref as R
 from tests.blocks import check
 
@@ -214,6 +215,38 @@ def test_gate_by_every_kind_of_tile(B, T, H, E):
     assert torch.equal(dwg, (x[inside].T.double().contiguous() @ d[inside].double()).float().to(torch.bfloat16))
     assert torch.equal(db.double(), d[inside].double().sum(0))
     assert torch.equal(g.backward(("dx",))[0], dx) and torch.equal(g.backward(("dwg",))[1], dwg)
+
+
+@pytest.mark.parametrize("T,H,E,plan", GP.GATE, ids=lambda v: str(v)[:24])
+def test_gate_in_its_steady_state(B, T, H, E, plan):
+    """The same at sizes whose rings and strips go round several times."""
+    p = B.moe_gate_plan_host(B.moe_router_config(T, H, E, 1, 2))
+    assert {n: getattr(p, n).as_tuple() for n in plan} == plan
+    test_gate_by_every_kind_of_tile(B, T, H, E)
+
+
+@pytest.mark.parametrize("T,H,E", [((1 << 21) + 37, 1088, 60), ((1 << 21) + 37, 1088, 300), (1 << 22, 64, 256)])
+def test_gate_elements_past_32_bits(B, T, H, E):
+    """More than 2^31 elements (2^32 bytes) of x and dx by every kind of product, and the largest batch of 256 experts,
+    whose dlogits in bf16 are 2^31 bytes: whole numbers whose sums are exact, compared in all rows."""
+    r = torch.Generator(device="cuda").manual_seed(E)
+    whole = lambda *n: torch.randint(-4, 5, n, generator=r, device="cuda", dtype=torch.int8)  # noqa: E731
+    x, wg, d = whole(T, H).to(torch.bfloat16), whole(H, E).to(torch.bfloat16), whole(T, E).float()
+    cfg = B.moe_router_config(T, H, E, 1, 1)
+    ws = torch.empty(max(B.moe_gate_workspace_size(cfg), B.moe_gate_workspace_size(cfg, True)), dtype=torch.uint8, device="cuda")
+    l, dx = torch.empty(T, E, device="cuda"), torch.empty_like(x)
+    dwg, db = torch.empty_like(wg), torch.empty(E, device="cuda")
+    B.moe_gate_logits(cfg, x, wg, None, None, l, ws)
+    B.moe_gate_backward(cfg, d, x, wg, None, dx, dwg, db, ws)
+    w, sums = wg.double(), torch.zeros(H, E, dtype=torch.float64, device="cuda")
+    wt = w.T.contiguous()
+    for at in range(0, T, 1 << 18):
+        rows = slice(at, min(at + (1 << 18), T))
+        xd, dd = x[rows].double(), d[rows].double()
+        assert torch.equal(l[rows].double(), xd @ w), at
+        assert torch.equal(dx[rows], (dd @ wt).float().to(torch.bfloat16)), at
+        sums += xd.T.contiguous() @ dd
+    assert torch.equal(dwg, sums.float().to(torch.bfloat16)) and torch.equal(db.double(), d.double().sum(0))
 
 
 # ---- losses ---------------------------------------------------------------------------------------------------------

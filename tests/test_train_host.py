@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 import torch
 
+from tests import gate_plans as GP
 from tests import train_ref as R
 
 B = pytest.importorskip("paper_2609_21483_amd.binding", reason="libmoe.so not built")
@@ -176,6 +177,53 @@ def test_calls_take_the_current_stream_without_torchs_own_shortcut(monkeypatch):
     monkeypatch.setattr(B, "_lib", types.SimpleNamespace(some_call=lambda *a: taken.append(a) or B.MOE_OK))
     B._call("some_call", 3, None, 7)
     assert taken == [(7, 0x1233)]
+
+
+# ---- the gate's tiles ----------------------------------------------------------------------------------------------
+def gate_plan(T, H, E):
+    p = B.moe_gate_plan_host(B.moe_router_config(T, H, E, 1, 1))
+    return {n: getattr(p, n).as_tuple() for n in ("logits", "dx", "dwg")}
+
+
+def test_the_gates_plan_query_refuses_bad_arguments():
+    lib, out = B.library(), B.moe_gate_plan()
+    assert lib.moe_gate_plan_host(None, C.byref(out)) == B.MOE_ERR_INVALID_ARG
+    assert lib.moe_gate_plan_host(C.byref(B.moe_router_config(8, 64, 4, 1, 1)), None) == B.MOE_ERR_INVALID_ARG
+    for cfg in [(-1, 64, 4, 2, 1), (8, 32, 4, 2, 1), (8, 64, 513, 2, 1), (8, 64, 4, 2, 0)]:
+        assert lib.moe_gate_plan_host(C.byref(B.moe_router_config(*cfg)), C.byref(out)) == B.MOE_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("T,H,E,plan", GP.GATE, ids=lambda v: str(v)[:24])
+def test_gate_sizes_take_their_plan(T, H, E, plan):
+    assert gate_plan(T, H, E) == plan
+
+
+def test_gate_sizes_cover_every_kind_of_tile_in_its_steady_state():
+    """A ring's steady state is reached from its fifth stage on (it holds up to four), a strip's waits from the third
+    strip of a part on, and every kind is covered whole and in parts where it has any."""
+    from tests import test_gpu_router as G
+    known = next(m.args[1] for m in G.test_gate_by_every_kind_of_tile.pytestmark if m.name == "parametrize")
+    sizes = sorted({(T, H, E) for T, H, E, *_ in [*known, *GP.GATE]})
+    logits, dx, dwg = set(), set(), set()
+    for T, H, E in sizes:
+        p = gate_plan(T, H, E)
+        rows = T - 8  # (of the tests' sequences)
+        stages = -(-rows // 64)
+        tiles, parts = p["logits"]
+        if tiles != "ring" or H // 64 // parts >= 5:
+            logits.add((tiles, parts > 1))
+        tiles, parts = p["dx"]
+        if tiles != "strips":
+            dx.add(tiles)
+        elif -(-stages // parts) >= 4:
+            dx.add((-(-E // 64), p["dwg"][0]))
+        tiles, parts = p["dwg"]
+        if stages // parts >= 5:
+            dwg.add((tiles, parts > 1))
+    assert logits >= {("few8", False), ("few8", True), ("few4", False), ("ring", False), ("ring", True), ("small", False), ("small", True),
+                      ("wide", False)}
+    assert dx >= {"small", "wide", (1, "ring"), (2, "ring"), (3, "ring"), (3, "broad"), (4, "ring"), (4, "broad"), (3, "wide"), (4, "wide")}
+    assert dwg >= {("ring", False), ("ring", True), ("broad", True), ("wide", True)}
 
 
 # ---- the reference -----------------------------------------------------------------------------------------------------
