@@ -164,6 +164,25 @@ def test_backward(B, T, H, stream):
     check("dweight", f64(dw), rdw, bdw)
 
 
+# at least three passes of the workgroups over the rows, the last one ragged, at every number of threads and loads of a row
+LONG = [(40001, 64), (16403, 128), (9001, 512), (3501, 1000), (1801, 2048), (801, 4096), (799, 8192), (601, 16384)]
+
+
+@pytest.mark.parametrize("T,H", LONG)
+def test_backward_over_several_passes(B, T, H):
+    test_backward(B, T, H, True)
+
+
+@pytest.mark.parametrize("T,H", LONG)
+def test_rows_of_later_passes_have_the_same_bits_alone(B, T, H):
+    dy, dsum, s, w = normal(1, T, H, std=0.01).cuda(), normal(2, T, H, std=0.01).cuda(), normal(3, T, H).cuda(), normal(4, H).cuda()
+    r = torch.rand(T, device="cuda") + 0.5
+    dx, _ = backward(B, dy, dsum, s, w, r)
+    for a, b in ((T // 2 - 3, T // 2 + 4), (T - 7, T)):
+        at = slice(a, b)
+        assert torch.equal(dx[at], backward(B, dy[at], dsum[at], s[at], w, r[at].clone())[0])
+
+
 def test_gradients_that_are_not_wanted(B):
     s, w, dy, r = normal(1, 70, 1000).cuda(), normal(2, 1000).cuda(), normal(3, 70, 1000).cuda(), torch.rand(70, device="cuda")
     dx, dw = backward(B, dy, None, s, w, r)
