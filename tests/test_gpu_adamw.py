@@ -449,3 +449,41 @@ def test_values_past_32_bits(B, bits):
     else:
         check("m", f64(big["m"][first:]), m1, em)
     assert not big["param"][:100000].any() and not big["param"][n // 2:n // 2 + 100000].any()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_past_32_bits(B, bits):
+    """The states and scales of the last blocks of a tensor of 2^32 + 1000 values in 8 bits, of 2^31 + 1000 in 32, value by
+    value; the gradients of the others are 0, and so their states stay."""
+    n = (1 << (32 if bits == 8 else 31)) + 1000
+    blocks = -(-n // 256)
+    first = (blocks - 5) * 256
+    src = tensor(n - first, "bf16", bits, "fp32", 18)
+    big = dict(weight_decay=0.1)
+    for k in ("param", "grad", "m", "v") + (("m_scale", "v_scale") if bits == 8 else ()):
+        size = blocks if k.endswith("_scale") else n
+        whole = torch.zeros(size * src[k].element_size(), dtype=torch.uint8, device="cuda")
+        whole[-src[k].nbytes:] = src[k].view(torch.uint8)
+        big[k] = whole.view(src[k].dtype)
+    before = values(src, bits)
+    cfg, c = config(B, bits)
+    B.moe_adamw(cfg, B.moe_adamw_tensors([big], bits))
+    torch.cuda.synchronize()
+    _, (m1, em), (v1, ev) = R.adamw(*before, c, np.float64(np.float32(0.1)))
+    random = R.random_bits(c["seed"], c["step"], 0, n - first, first)
+    for name, x, err, u, mant, least, most in (("m", m1, em, random[0], 3, -6, 448.0), ("v", v1, ev, random[1], 2, -14, 57344.0)):
+        got = f64(big[name][first:])
+        if bits == 32:
+            check(name, got, x, err)
+        else:
+            scale = R.block_max(x) / most
+            check(name + "_scale", f64(big[name + "_scale"][-5:]), scale, 12 * R.F32 * scale)
+            want, unit = R.rounded_at_random(x, scale, u, mant, least, most, name == "v")
+            # the reference's neighbour but where an error crosses one of 2^16 thresholds of a step, and never further than a step
+            rep = np.repeat(scale, 256)[:n - first]
+            odds = np.minimum(1.0, 2 * (err + 8 * R.F32 * np.abs(x)) / (unit * rep)).sum()
+            assert (got != want).sum() <= odds + 6 * odds ** 0.5 + 3
+            check(name, got, want, unit)
+            assert not big[name + "_scale"][:-5].any()
+        for at in range(0, first, 1 << 30):
+            assert not big[name][at:min(at + (1 << 30), first)].view(torch.uint8).any()
