@@ -621,8 +621,12 @@ moe_status moe_gate_logits(const moe_router_config* cfg, const uint16_t* x, cons
 
 /* The gradients of moe_gate_logits from dlogits (fp32 [T][E]): dx bf16 [T][H] =
  * dlogits wg^T, dwg bf16 [H][E] = x^T dlogits, dbias fp32 [E] = sum_t dlogits; each
- * may be NULL.  dlogits are rounded to bf16 once for the two products (dbias adds
- * them unrounded); sums are fp32.  Without rows dwg and dbias are 0. */
+ * may be NULL.  dlogits are rounded to bf16 once for the two products, as every
+ * operand of the matrix instructions is, so each of their terms is off by up to 2^-8 of
+ * itself (dbias adds them unrounded); sums are fp32.  Where terms cancel and that is
+ * too much, two calls have the products of dlogits to 2^-16 of a term: of dlogits
+ * rounded to bf16 and of what that left, their results added in fp32.  Without rows
+ * dwg and dbias are 0. */
 moe_status moe_gate_backward(const moe_router_config* cfg, const float* dlogits, const uint16_t* x,
                              const uint16_t* wg, const int32_t* seq_off, uint16_t* dx, uint16_t* dwg, float* dbias,
                              void* ws, size_t ws_bytes, void* stream);

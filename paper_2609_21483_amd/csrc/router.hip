@@ -16,7 +16,11 @@ namespace {
 // groups, over the rows that some sequence has.  The tiles want whole 16 bytes, so
 // a gate whose rows are none is copied with zeros behind each row; dlogits are
 // rounded to bf16 for both products that take them, with zeros up to a multiple of
-// 64, the depth of a stage.
+// 64, the depth of a stage.  The matrix instructions multiply bf16 by bf16, as x and
+// the gate are: dlogits as two bf16 terms would be the products of twice the experts
+// (32768 x 4096, E = 128 : 256, all gradients 133 : 195 us).  One term puts each of a
+// sum's terms off by up to 2^-8: dx and dwg by 2.3e-3 of their 2-norm where nothing
+// cancels, 1.7e-3 of it their own rounding.  A caller has both terms by two calls.
 struct GateArgs {
   int T, H, E, S;
   int Ep;  // columns of the gate as the product reads it

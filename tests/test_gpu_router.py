@@ -5,7 +5,7 @@ import torch
 
 from tests import gate_plans as GP
 from tests import train_ref as R
-from tests.blocks import check
+from tests.blocks import BF, check
 
 pytestmark = pytest.mark.gpu
 MARK = 0x4B4B
@@ -247,6 +247,36 @@ def test_gate_elements_past_32_bits(B, T, H, E):
         assert torch.equal(dx[rows], (dd @ wt).float().to(torch.bfloat16)), at
         sums += xd.T.contiguous() @ dd
     assert torch.equal(dwg, sums.float().to(torch.bfloat16)) and torch.equal(db.double(), d.double().sum(0))
+
+
+@pytest.mark.parametrize("T,H,E", [(300, 192, 60), (1000, 1088, 128), (700, 256, 300)])
+def test_products_of_unrounded_dlogits_by_two_calls(B, T, H, E):
+    """dlogits of rows that add up to 0, as a softmax's do, and a gate with a part that all experts share, which cancels: the
+    products of dlogits rounded to bf16 and of what that left, added, are those of dlogits to 2^-16 of the terms, where
+    one call is off by up to 2^-8 of them."""
+    g = Gate(B, T, H, E, seed=14)
+    g.wg = (g.wg.float() + 4.0).to(torch.bfloat16)
+    g.dl = g.dl - g.dl.mean(1, keepdim=True)
+    g.d[1] = g.wg.cuda()
+    high = g.dl.to(torch.bfloat16).float()
+    parts = []
+    for d in (high, g.dl - high):
+        g.d[3] = d.cuda()
+        parts.append([f64(t) for t in g.backward()])
+    g.d[3] = g.dl.cuda()
+    one = [f64(t) for t in g.backward()]
+    d, x, wg = g.dl.numpy().astype(np.float64), f64(g.x), f64(g.wg)
+    for name, exact, terms, n, a, b, c in zip(("dx", "dwg"), (d @ wg.T, x.T @ d), (np.abs(d) @ np.abs(wg).T, np.abs(x).T @ np.abs(d)),
+                                              (E, T), *parts, one):
+        # each product is rounded to bf16, what is left of the rest is 2^-16 of a term at most, sums are fp32
+        check(name, a + b, exact, BF * (np.abs(a) + np.abs(b)) + (2.0 ** -16 + 4 * n * R.F32) * terms + 2 * R.TINY)
+        check(name + " by one call", c, exact, BF * np.abs(c) + (BF + 2 * n * R.F32) * terms + R.TINY)
+    off = lambda v: np.linalg.norm(v - d @ wg.T) / np.linalg.norm(d @ wg.T)  # noqa: E731
+    # evenly spread roundings, 2^-8 / sqrt(3) of a norm at most, of the second product, whose norm is a sixth of dx's or less,
+    # and of the first, which is dx but for it: sqrt(1 + 2 / 36) of that of dx
+    assert off(parts[0][0] + parts[1][0]) < BF / 3 ** 0.5 * 1.2 < off(one[0])
+    db = parts[0][2] + parts[1][2]
+    check("dbias", db, d.sum(0), 4 * T * R.F32 * np.abs(d).sum(0))
 
 
 # ---- losses ---------------------------------------------------------------------------------------------------------
