@@ -618,7 +618,8 @@ def moe_route_loss_backward(cfg: moe_router_config, logits, topk_idx, topk_w, se
 
 
 class AdamwTensors:
-    """The list that moe_adamw takes, checked and laid out once; it keeps the tensors alive."""
+    """The list that moe_adamw takes, checked and laid out once, at 4 to 5 us a tensor; it keeps the tensors alive and goes by
+    their addresses, so gradients are written where they were: one that is allocated anew needs a new list."""
 
     def __init__(self, array, state_bits: int, device: Optional[int], tensors):
         self.array, self.state_bits, self.device, self.tensors = array, state_bits, device, tensors

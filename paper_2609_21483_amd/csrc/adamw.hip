@@ -16,8 +16,8 @@ constexpr int CHUNK = 256 * VALUES;  // of a workgroup
 constexpr int64_t MOST_CHUNKS = (1 << 24) - 1;
 // Tensors of a launch: their addresses are kernel arguments (4 KB at most), so
 // that no table has to reach the device before the step.  A tensor and its end take 48
-// bytes (8 bits: 60), addresses as multiples of 16 (scales': of 4): 150 small tensors in two launches, 20
-// us, against 29 in the four that 72 bytes a tensor make.
+// bytes (8 bits: 60), addresses as multiples of 16 (scales': of 4): 150 small tensors in
+// two launches, 20 us, against 29 in four of 48 tensors.
 template <bool BITS8>
 struct Packed {
   static constexpr int N = BITS8 ? 7 : 5;  // grad, param, master, m, v, m_scale, v_scale
@@ -134,8 +134,8 @@ __device__ __forceinline__ float bf16_of(const Raw<GROUP>& r, int j) {
 // One workgroup steps CHUNK values of a tensor, in groups of GROUP consecutive
 // ones a thread: 16 where states have 8 bits (one 16-byte load of each, a block's
 // scale from 16 threads), 4 where they have 32.  Bound by memory: 604 million values,
-// 8-bit states and bf16 weights and gradients, 1183 to 1213 us, 5.1 TB/s; 134 million with
-// 32-bit states, master weights and fp32 gradients 770, 5.2.
+// 8-bit states and bf16 weights and gradients, 1183 to 1262 us, 4.8 to 5.1 TB/s; 134 million
+// with 32-bit states, master weights and fp32 gradients 744 to 770, 5.2 to 5.4.
 // GRAD32: gradients in fp32; MASTER, PARAM: which weights there are.
 template <bool BITS8, bool GRAD32, bool MASTER, bool PARAM>
 __device__ __forceinline__ void step_chunk(const AdamArgs<BITS8>& a, const Packed<BITS8>& t, int64_t chunk) {

@@ -153,8 +153,8 @@ __global__ __launch_bounds__(group_of<THREADS>) void rms_norm_kernel(NormArgs a)
 
 // dx row by row, and each workgroup's part of dweight over its rows: bound by memory,
 // so the next row's loads are under way while a row is worked on.  32768 x 4096 with
-// dsum 181 to 204 us, 5.3 to 5.9 TB/s (without the next row's loads 200 to 215), and 5
-// for the parts' sum; 333 x 1000 3.5 and 3.1.
+// dsum 179 to 212 us by a trace, 186 with the next kernel's 5 in a row of calls, 5.8 TB/s
+// (without the next row's loads 200 to 215 by a trace); 333 x 1000 3.5 and 3.0.
 template <int THREADS, int LOADS>
 __global__ __launch_bounds__(group_of<THREADS>) void rms_norm_grad_kernel(NormGradArgs a) {
   constexpr int PER = group_of<THREADS> / THREADS, W = THREADS * LOADS * 8;

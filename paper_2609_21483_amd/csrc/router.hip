@@ -18,7 +18,7 @@ namespace {
 // rounded to bf16 for both products that take them, with zeros up to a multiple of
 // 64, the depth of a stage.  The matrix instructions multiply bf16 by bf16, as x and
 // the gate are: dlogits as two bf16 terms would be the products of twice the experts
-// (32768 x 4096, E = 128 : 256, all gradients 133 : 195 us).  One term puts each of a
+// (32768 x 4096, E = 128 : 256, all gradients 135 : 200 us).  One term puts each of a
 // sum's terms off by up to 2^-8: dx and dwg by 2.3e-3 of their 2-norm where nothing
 // cancels, 1.7e-3 of it their own rounding.  A caller has both terms by two calls.
 struct GateArgs {
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(512) void gate_dwg_wide_kernel(GateArgs a) {
 
 // dx, which is written, and dwg, for which x is read, in one launch, in turn by eight
 // workgroups (one for each XCD): either may have none.  32768 rows, H = 4096, E = 128:
-// 117 to 125 us for 0.55 GB, about a copy's rate; one after the other 57 + 78.
+// 117 to 136 us for 0.55 GB, about a copy's rate; one after the other 57 + 78.
 template <int KC, bool BROAD>
 __global__ __launch_bounds__(512, 2) void gate_grad_kernel(GateArgs a) {
   constexpr int LDS = std::max(DwTile<BROAD>::template RING_LDS<DW_RING<BROAD>>, KC ? 3 * KC * 8192 + 8 * 4096 : 0);
